@@ -434,6 +434,134 @@ int lstm_bench_exchange(int hidden, int waves, int steps, int iters, int coopera
 int lstm_bench_group_exchange(int slots, int members, int groups, int placed, int workgroup_stores, int steps, int iters,
                               int cooperative, double* avg_us_per_round, int* groups_verified, void* stream);
 
+/* ---- operators around the cells -----------------------------------------------------------------------------------------
+ * What a recurrent language model runs beside the stacks above: a recurrence that is linear in its state (for long sequences
+ * and for training), the norm between layers, products of 8-bit operands and the draw of the next token.  They have no
+ * handle.  All data pointers are DEVICE and the caller's, `dtype` and `out_dtype` are LSTM_F32 or LSTM_BF16 (raw 16-bit
+ * patterns), lengths `*_ld` and strides are in elements.  Every call is asynchronous on `stream`, allocates nothing, keeps
+ * nothing and may be recorded into a graph; two calls may run at the same time if their outputs and workspaces are different
+ * ones.  A workspace is 16-byte aligned and need not be initialised.  Errors: LSTM_ERR_ARG (NULL where required, a size, type,
+ * stride or alignment outside what is named), LSTM_ERR_NOMEM (workspace too small), LSTM_ERR_LAUNCH; the text is what
+ * lstm_last_error(NULL) returns.  Nothing is launched by a call that returns an error of an argument.
+ */
+
+/*
+ * Gated linear recurrence: the conventional cell with gates that read the input only,
+ *
+ *     f, i, o = sigmoid(P_f, P_i, P_o)     g = tanh(P_g)     c_t = f (x) c_{t-1} + i (x) g     h_t = o (x) tanh(c_t)
+ *
+ *   P [T, B, 4H] of dtype: the pre-activations W x_t + b in the library's gate order (f, i, o, g, H values each), row (t, b)
+ *     at P + t*P_t + b*P_b.  The strides are >= 0; so P may be part of a wider array, or [B, T, 4H].
+ *   reverse = 1: each sequence runs from its last step to its first (h_t stays at the position of its input).
+ *   lengths [B] int32 or NULL (all T): steps of each sequence, counted from t = 0 and taken into [0, T].  What P holds behind
+ *     a sequence's end is not read into any result; h is 0 there, and the state is that of the last step (c0 for length 0).
+ *   c0 [B, H] fp32 or NULL = zeros; cT [B, H] fp32 or NULL, the final state; it may be c0 itself.
+ *   h [T, B, H] of dtype, strides h_t and h_b (at least H where there is more than one row).
+ *   states: NULL, or fp32 [ceil(T / LSTM_SCAN_STEPS), B, H], what lstm_scan_backward needs: the state in front of every
+ *     LSTM_SCAN_STEPS-th step.
+ *   workspace: at least lstm_scan_workspace_bytes(T, B, H) bytes.
+ * T = 0 moves c0 to cT; B = 0 does nothing.  State and gates are fp32; h alone is rounded to dtype.  T = 1 is the form for
+ * serving: one launch, c0 = cT in place.
+ */
+enum { LSTM_SCAN_STEPS = 16 };
+size_t lstm_scan_workspace_bytes(int T, int B, int H);
+int lstm_scan_forward(int T, int B, int H, int dtype, int reverse, const void* P, int64_t P_t, int64_t P_b,
+                      const int32_t* lengths, const float* c0, void* h, int64_t h_t, int64_t h_b, float* cT, float* states,
+                      void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Its gradient.  T, B, H, dtype, reverse, P, lengths as in the forward that left `states`.
+ *   dh [T, B, H] of dtype, strides dh_t, dh_b (>= 0): gradient of h; what it holds behind a sequence's end is not read.
+ *   dcT [B, H] fp32 or NULL = zeros: gradient of the final state.
+ *   dP [T, B, 4H] of dtype, strides dP_t, dP_b (at least 4H where there is more than one row): gradient of P, 0 behind the
+ *     end of a sequence.  dc0 [B, H] fp32 or NULL: gradient of c0; it may be dcT itself.
+ */
+int lstm_scan_backward(int T, int B, int H, int dtype, int reverse, const void* P, int64_t P_t, int64_t P_b,
+                       const int32_t* lengths, const float* states, const void* dh, int64_t dh_t, int64_t dh_b,
+                       const float* dcT, void* dP, int64_t dP_t, int64_t dP_b, float* dc0, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/*
+ * Root-mean-square norm of M rows of N columns (N <= 16384), with the residual's addition in front and 8-bit values behind:
+ *
+ *     s = round(x + residual)     rstd = (sum_n s^2 / N + eps)^(-1/2)     y = s rstd weight
+ *     y8_scale[m, n / 128] = max over the 128 columns of |y| / 448, at least 2^-126     y8 = e4m3(y / scale)
+ *
+ *   x, residual (NULL: s = x), sum (NULL: not wanted; may be residual or x), y (NULL: not wanted; may be x or residual) of
+ *     dtype.  s is rounded to dtype before the norm, whether or not it is stored.
+ *   weight [N] fp32 or NULL = ones; rstd [M] fp32 or NULL, for the backward pass.
+ *   y8 uint8 (e4m3, no infinities, largest value 448) and y8_scale fp32 [M, ceil(N / 128)]: both or neither.  y8 is 16-byte
+ *     aligned and y8_ld a multiple of 16, as lstm_matmul_fp8 takes it; columns behind N are left as they are.
+ *   eps >= 0.
+ * A NaN or an infinity in a row makes that row's results NaN or 0 as the formula does; rows do not see each other.
+ */
+int lstm_rmsnorm_forward(int M, int N, int dtype, const void* x, int64_t x_ld, const void* residual, int64_t residual_ld,
+                         const float* weight, float eps, void* sum, int64_t sum_ld, void* y, int64_t y_ld, uint8_t* y8,
+                         int64_t y8_ld, float* y8_scale, int64_t y8_scale_ld, float* rstd, void* stream);
+/*
+ * Its gradient, with respect to s (and so to x and to the residual alike) and to the weight:
+ *
+ *     g = dy weight     xhat = s rstd     dx = rstd (g - xhat sum_n(g xhat) / N) + dsum     dweight = sum_m dy xhat
+ *
+ *   sum: s as the forward stored it (x where there was no residual); rstd as the forward stored it.  dy: gradient of y; where
+ *   y8 alone was made, that of the values it stands for.  dsum: what reaches s from elsewhere (the residual's next use), or
+ *   NULL; dx may be dsum or dy itself.  dweight [N] fp32 or NULL.  workspace: at least lstm_rmsnorm_workspace_bytes(M, N).  M = 0: dweight
+ *   becomes 0.  The rows' sums are added in one order: the same call gives the same bits.
+ */
+size_t lstm_rmsnorm_workspace_bytes(int M, int N);
+int lstm_rmsnorm_backward(int M, int N, int dtype, const void* sum, int64_t sum_ld, const float* weight, const float* rstd,
+                          const void* dy, int64_t dy_ld, const void* dsum, int64_t dsum_ld, void* dx, int64_t dx_ld,
+                          float* dweight, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * x [M, N] of dtype as e4m3 values q and scales: scale = max |x| / 448 (at least 2^-126) over 128 columns and block_rows rows,
+ * q = e4m3(x / scale), nearest-even.  block_rows = 1: scale [M, ceil(N / 128)], for activations; block_rows = 128: scale
+ * [ceil(M / 128), ceil(N / 128)], for weights (the transpose of such a matrix has the transposed scales).  q is 16-byte
+ * aligned, q_ld a multiple of 16; columns behind N are left as they are.  An infinity becomes 448 and counts as the largest finite
+ * value for its block's scale; a NaN stays NaN and does not count.
+ */
+int lstm_quantize_fp8(int M, int N, int dtype, int block_rows, const void* x, int64_t x_ld, uint8_t* q, int64_t q_ld,
+                      float* scale, int64_t scale_ld, void* stream);
+
+/*
+ * Product of e4m3 operands with a scale for every 128 columns:
+ *
+ *     C[m, n] = sum_kb a_scale[m, kb] w_scale[n / w_block_rows, kb] ( sum over the 128 columns k of kb of A[m, k] W[n, k] ) + bias[n]
+ *
+ *   A [M, K], W [N, K] uint8 (e4m3): 16-byte aligned, a_ld and w_ld multiples of 16 and at least K.  A row is read up to the
+ *     next multiple of 16 columns; what stands behind column K does not enter.
+ *   a_scale [M, ceil(K / 128)], w_scale [ceil(N / w_block_rows), ceil(K / 128)] fp32; w_block_rows 1 or 128.
+ *   bias [N] fp32 or NULL.  C [M, N] of out_dtype.  workspace: at least lstm_matmul_fp8_workspace_bytes(M, N, K).
+ * Both gradients are the same call: dA = dC . W with dC quantized along N and W transposed; dW = dC^T . A with both
+ * transposed and quantized along M (w_block_rows = 1).  K = 0 gives the bias.  The same call gives the same bits.
+ */
+size_t lstm_matmul_fp8_workspace_bytes(int M, int N, int K);
+int lstm_matmul_fp8(int M, int N, int K, const uint8_t* A, int64_t a_ld, const float* a_scale, int64_t a_scale_ld,
+                    const uint8_t* W, int64_t w_ld, const float* w_scale, int64_t w_scale_ld, int w_block_rows,
+                    const float* bias, int out_dtype, void* C, int64_t c_ld, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
+ * One token for each of M rows of logits [M, V] (dtype; V <= 2^20) from given random numbers.  With w_j = exp((l_j - max l) / temperature)
+ * and the tokens ordered by logit, the largest first, equal ones by index:
+ *   allowed uint8 [M, V] (allowed_ld = 0: one row for all) or NULL: tokens whose byte is 0 do not exist, whatever their
+ *     logit holds; neither do tokens whose logit is NaN or minus infinity.  Plus infinity takes all mass.
+ *   temperature [M] or NULL = 1; at or below 0 (or NaN) the first token of the order is taken.
+ *   top_k [M] int32 or NULL: the first top_k tokens of the order stay; 0 or less keeps all.
+ *   top_p [M] or NULL: of those, a token stays while the mass in front of it is less than top_p times their whole mass; the
+ *     first always stays; 1 or more keeps all.
+ *   min_p [M] or NULL = 0: of those, tokens with w_j >= min_p (taken to at most 1) stay.
+ *   u [M] fp32 in [0, 1): the token is the first by index at which the running sum of w over the tokens that stayed exceeds u
+ *     times their sum.
+ *   token [M] int32, -1 for a row without tokens; prob [M] fp32 or NULL: w of the token over the sum, 0 for such a row;
+ *   kept [M] int32 or NULL: how many tokens stayed.  workspace: at least lstm_sample_workspace_bytes(M, V).
+ * Weights are evaluated in fp64 and summed as whole multiples of 2^-S, S = 62 - ceil(log2 V): what is drawn does not depend
+ * on how the work is cut.
+ */
+size_t lstm_sample_workspace_bytes(int M, int V);
+int lstm_sample(int M, int V, int dtype, const void* logits, int64_t ld, const uint8_t* allowed, int64_t allowed_ld,
+                const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+                int32_t* token, float* prob, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,7 @@ LSTM_OK = 0
 LSTM_ERR_ARG, LSTM_ERR_SHAPE, LSTM_ERR_STATE, LSTM_ERR_NOMEM, LSTM_ERR_LAUNCH, LSTM_ERR_TIMEOUT = -1, -2, -3, -4, -5, -6
 LSTM_FMT_AUTO, LSTM_FMT_DENSE_MASKED, LSTM_FMT_ROW_COMPRESSED = 0, 1, 2
 LSTM_PLAN_AUTO, LSTM_PLAN_STEPWISE, LSTM_PLAN_PERSISTENT = 0, 1, 2
+LSTM_SCAN_STEPS = 16
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liblstm355.so")
 
@@ -28,6 +29,9 @@ EXPORTS = [
     "lstm_forward", "lstm_check", "lstm_set_plan", "lstm_set_launch_mode", "lstm_set_default_launch_mode", "lstm_set_profiling", "lstm_get_profile", "lstm_describe_plan", "lstm_get_compressed",
     "lstm_latency_sweep", "lstm_latency_sweep_model", "lstm_find_lhp", "lstm_grow_to_lhp", "lstm_prune_weights", "lstm_prune_rows_cols", "lstm_prune_rows_cols_static",
     "lstm_compact_rows_cols",
+    "lstm_scan_workspace_bytes", "lstm_scan_forward", "lstm_scan_backward", "lstm_rmsnorm_workspace_bytes", "lstm_rmsnorm_forward",
+    "lstm_rmsnorm_backward", "lstm_quantize_fp8", "lstm_matmul_fp8_workspace_bytes", "lstm_matmul_fp8",
+    "lstm_sample_workspace_bytes", "lstm_sample",
     "lstm_bench_copy", "lstm_bench_matmul", "lstm_bench_mfma", "lstm_bench_barrier", "lstm_bench_exchange", "lstm_bench_group_exchange",
 ]
 
@@ -116,6 +120,21 @@ def load(build_if_missing: bool = True):
     lib.lstm_bench_exchange.argtypes = [ci, ci, ci, ci, ci, c.POINTER(c.c_double), vp]
     lib.lstm_bench_group_exchange.restype = ci
     lib.lstm_bench_group_exchange.argtypes = [ci, ci, ci, ci, ci, ci, ci, ci, c.POINTER(c.c_double), c.POINTER(ci), vp]
+    i64, sz = c.c_int64, c.c_size_t
+    for name, types in (
+            ("lstm_scan", [ci] * 3), ("lstm_rmsnorm", [ci] * 2), ("lstm_matmul_fp8", [ci] * 3), ("lstm_sample", [ci] * 2)):
+        fn = getattr(lib, name + "_workspace_bytes")
+        fn.restype, fn.argtypes = sz, types
+    for name, types in (
+            ("lstm_scan_forward", [ci] * 5 + [vp, i64, i64, vp, vp, vp, i64, i64, vp, vp, vp, sz, vp]),
+            ("lstm_scan_backward", [ci] * 5 + [vp, i64, i64, vp, vp, vp, i64, i64, vp, vp, i64, i64, vp, vp, sz, vp]),
+            ("lstm_rmsnorm_forward", [ci] * 3 + [vp, i64, vp, i64, vp, c.c_float] + [vp, i64] * 4 + [vp, vp]),
+            ("lstm_rmsnorm_backward", [ci] * 3 + [vp, i64, vp, vp] + [vp, i64] * 3 + [vp, vp, sz, vp]),
+            ("lstm_quantize_fp8", [ci] * 4 + [vp, i64] * 3 + [vp]),
+            ("lstm_matmul_fp8", [ci] * 3 + [vp, i64] * 4 + [ci, vp, ci, vp, i64, vp, sz, vp]),
+            ("lstm_sample", [ci] * 3 + [vp, i64, vp, i64] + [vp] * 9 + [sz, vp])):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = ci, types
     _lib = lib
     return lib
 
@@ -393,6 +412,64 @@ def lstm_bench_exchange(hidden: int, waves: int = 0, steps: int = 200, iters: in
 # ------------------------------------------------------------------------------------------------------------
 # Convenience wrapper for tests and the benchmark: owns a handle plus torch device buffers.
 # ------------------------------------------------------------------------------------------------------------
+# ---- operators around the cells: device pointers as addresses, as the header describes them; None is NULL
+
+def lstm_scan_workspace_bytes(T: int, B: int, H: int) -> int:
+    return load().lstm_scan_workspace_bytes(T, B, H)
+
+
+def lstm_scan_forward(T, B, H, dtype, reverse, P_ptr, P_t, P_b, lengths_ptr, c0_ptr, h_ptr, h_t, h_b, cT_ptr, states_ptr, ws_ptr,
+                      ws_bytes, stream=None) -> None:
+    _check(load().lstm_scan_forward(T, B, H, dtype, reverse, P_ptr, P_t, P_b, lengths_ptr, c0_ptr, h_ptr, h_t, h_b, cT_ptr, states_ptr,
+                                    ws_ptr, ws_bytes, stream))
+
+
+def lstm_scan_backward(T, B, H, dtype, reverse, P_ptr, P_t, P_b, lengths_ptr, states_ptr, dh_ptr, dh_t, dh_b, dcT_ptr, dP_ptr, dP_t,
+                       dP_b, dc0_ptr, ws_ptr, ws_bytes, stream=None) -> None:
+    _check(load().lstm_scan_backward(T, B, H, dtype, reverse, P_ptr, P_t, P_b, lengths_ptr, states_ptr, dh_ptr, dh_t, dh_b, dcT_ptr,
+                                     dP_ptr, dP_t, dP_b, dc0_ptr, ws_ptr, ws_bytes, stream))
+
+
+def lstm_rmsnorm_workspace_bytes(M: int, N: int) -> int:
+    return load().lstm_rmsnorm_workspace_bytes(M, N)
+
+
+def lstm_rmsnorm_forward(M, N, dtype, x_ptr, x_ld, residual_ptr, residual_ld, weight_ptr, eps, sum_ptr, sum_ld, y_ptr, y_ld, y8_ptr,
+                         y8_ld, y8_scale_ptr, y8_scale_ld, rstd_ptr, stream=None) -> None:
+    _check(load().lstm_rmsnorm_forward(M, N, dtype, x_ptr, x_ld, residual_ptr, residual_ld, weight_ptr, eps, sum_ptr, sum_ld, y_ptr,
+                                       y_ld, y8_ptr, y8_ld, y8_scale_ptr, y8_scale_ld, rstd_ptr, stream))
+
+
+def lstm_rmsnorm_backward(M, N, dtype, sum_ptr, sum_ld, weight_ptr, rstd_ptr, dy_ptr, dy_ld, dsum_ptr, dsum_ld, dx_ptr, dx_ld,
+                          dweight_ptr, ws_ptr, ws_bytes, stream=None) -> None:
+    _check(load().lstm_rmsnorm_backward(M, N, dtype, sum_ptr, sum_ld, weight_ptr, rstd_ptr, dy_ptr, dy_ld, dsum_ptr, dsum_ld, dx_ptr,
+                                        dx_ld, dweight_ptr, ws_ptr, ws_bytes, stream))
+
+
+def lstm_quantize_fp8(M, N, dtype, block_rows, x_ptr, x_ld, q_ptr, q_ld, scale_ptr, scale_ld, stream=None) -> None:
+    _check(load().lstm_quantize_fp8(M, N, dtype, block_rows, x_ptr, x_ld, q_ptr, q_ld, scale_ptr, scale_ld, stream))
+
+
+def lstm_matmul_fp8_workspace_bytes(M: int, N: int, K: int) -> int:
+    return load().lstm_matmul_fp8_workspace_bytes(M, N, K)
+
+
+def lstm_matmul_fp8(M, N, K, A_ptr, a_ld, a_scale_ptr, a_scale_ld, W_ptr, w_ld, w_scale_ptr, w_scale_ld, w_block_rows, bias_ptr,
+                    out_dtype, C_ptr, c_ld, ws_ptr, ws_bytes, stream=None) -> None:
+    _check(load().lstm_matmul_fp8(M, N, K, A_ptr, a_ld, a_scale_ptr, a_scale_ld, W_ptr, w_ld, w_scale_ptr, w_scale_ld, w_block_rows,
+                                  bias_ptr, out_dtype, C_ptr, c_ld, ws_ptr, ws_bytes, stream))
+
+
+def lstm_sample_workspace_bytes(M: int, V: int) -> int:
+    return load().lstm_sample_workspace_bytes(M, V)
+
+
+def lstm_sample(M, V, dtype, logits_ptr, ld, allowed_ptr, allowed_ld, temperature_ptr, top_k_ptr, top_p_ptr, min_p_ptr, u_ptr,
+                token_ptr, prob_ptr, kept_ptr, ws_ptr, ws_bytes, stream=None) -> None:
+    _check(load().lstm_sample(M, V, dtype, logits_ptr, ld, allowed_ptr, allowed_ld, temperature_ptr, top_k_ptr, top_p_ptr, min_p_ptr,
+                              u_ptr, token_ptr, prob_ptr, kept_ptr, ws_ptr, ws_bytes, stream))
+
+
 class Lstm:
     """hidden (and gate_hidden) may be one width for all layers or one per layer.  With per-layer widths the states are
     flat tensors: block n = l * ndir + d holds [B, hidden[l]] values, the blocks follow each other in that order."""

@@ -79,6 +79,16 @@ static int fail(const lstm_t* m, int code, const std::string& msg)
     if (m) m->err = msg; else g_create_error = msg;
     return code;
 }
+namespace l355 {
+int op_error(int code, const char* msg) noexcept
+{
+    try {
+        g_create_error = msg;
+    } catch (...) {     // no memory for the text: the code says it
+    }
+    return code;
+}
+}  // namespace l355
 static int fail_hip(const lstm_t* m, hipError_t e, const char* what)
 {
     return fail(m, e == hipErrorOutOfMemory ? LSTM_ERR_NOMEM : LSTM_ERR_LAUNCH,
