@@ -216,7 +216,11 @@ int lstm_matmul_fp8(int M, int N, int K, const uint8_t* A, int64_t a_ld, const f
     if (!workspace) return bad(entry, kNull);
     if (!aligned(workspace, 16)) return bad(entry, "the workspace is not 16-byte aligned");
     const MatmulFp8Args a = {M, N, K, w_block_rows, out_dtype == LSTM_BF16, A, a_ld, a_scale, a_scale_ld, W, w_ld, w_scale, w_scale_ld, bias, C, c_ld, (float*)workspace};
-    return launched(entry, launch_matmul_fp8(a, (hipStream_t)stream));
+    try {
+        return launched(entry, launch_matmul_fp8(a, (hipStream_t)stream));
+    } catch (...) {     // the table of kernels with their LDS sizes allocates
+        return op_error(LSTM_ERR_NOMEM, "lstm_matmul_fp8: host allocation failed");
+    }
 }
 
 static bool sample_fits(int M, int V) { return M >= 0 && M < (1 << 22) && V >= 1 && V <= kSampleMaxVocabulary; }

@@ -114,11 +114,18 @@ __global__ __launch_bounds__(64 * kRowsWaves) void matmul_fp8_rows_kernel(Matmul
     }
 }
 
-// Many rows.  A workgroup of WN x WM waves takes a tile of W's rows by A's, each wave 64 by 16 TM of it.  The rows of a
-// block of 128 columns are copied to LDS without passing through registers, NST - 1 blocks ahead (what a copy takes, one to
-// two microseconds, is several blocks' products), a wave reads its fragments of a block at once, and while it waits for
-// them the other wave of its SIMD multiplies.  Sixteen-byte chunk c of row r stands at chunk c ^ key(r), and lanes (r, g) read
-// chunks g and g + 4, so that the lanes that are served together meet different banks.
+// Many rows.  A workgroup of four waves takes a tile of 128 rows of W by 32 TM of A, each wave 64 by 16 TM of it.  The rows
+// of a block of 128 columns are copied to LDS without passing through registers while the block before is multiplied, and a
+// wave reads its fragments of a block at once; two to three workgroups on a compute unit fill each other's waits.
+// Sixteen-byte chunk c of row r stands at chunk c ^ key(r), and lanes (r, g) read chunks g and g + 4, so that the lanes that
+// are served together meet different banks (chunks 2 g and 2 g + 1 cost twice the reads).
+//
+// Bound: the path from L2 to LDS.  16384 x 8192 x 2048 to bf16 takes 343 us, 1.6 PFLOP/s; without its copies it would take 230,
+// without copies and reads 185, the matrix instructions alone 152 (they sustain 3.6 PFLOP/s), the copies alone about as long.
+// Tiles of 256 by 128 copy a quarter less, but one workgroup of eight waves waits for itself: no faster with two or three
+// blocks in flight, 355 with its waves reading and multiplying in turns; 256 by 256: 380.  The copies are issued in front of the
+// reads in the large tiles (behind them: 365, in between the products: 371), in between the products in the small ones, whose
+// compute units hold one or two workgroups (700 x 6000 x 1500 with its quantization 21.7 us, in front of the reads 22.7).
 //
 // The instruction's rows are rows of W in an order that leaves a lane with sixteen neighbouring n of one m (n_of), so that C
 // is written in wide pieces; one scale per lane and 16 rows of A covers them where W's scales are those of 128 rows.
@@ -136,12 +143,6 @@ __device__ __forceinline__ int key_w(int row) { return ((row >> 1) & 1) | ((row 
 __device__ __forceinline__ i32x8 both(const u32x4v (&f)[2])
 {
     return (i32x8){(int)f[0][0], (int)f[0][1], (int)f[0][2], (int)f[0][3], (int)f[1][0], (int)f[1][1], (int)f[1][2], (int)f[1][3]};
-}
-template <int N>
-__device__ __forceinline__ void wait_vmcnt()
-{
-    static_assert(N >= 0 && N < 64, "six-bit counter");
-    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 // A wave's fragments and scales of a block, all of them there when it returns.  (Written out because in front of a read that
 // it knows of the compiler waits until every copy to LDS under way has ended.)  w, a: addresses of the lower chunks, w1, a1: of
@@ -202,10 +203,10 @@ __device__ __forceinline__ void read_block(u32x4v (&fw)[4][2], u32x4v (&fa)[2][2
 #undef L355_READ_W
 #undef L355_W_OUT
 
-template <int WN, int WM, int TM, int NST, bool EXACT, bool ROW_SCALES>
-__global__ __launch_bounds__(64 * WN * WM, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a, int tiles_n, int tiles_m)
+template <int TM, bool EXACT, bool ROW_SCALES>
+__global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a, int tiles_n, int tiles_m)
 {
-    constexpr int BN = 64 * WN, BM = 16 * TM * WM, TILE = (BN + BM) * 128, STAGE = TILE + 256 * (WN + WM), WAVES = WN * WM;
+    constexpr int WN = 2, WM = 2, BN = 64 * WN, BM = 16 * TM * WM, TILE = (BN + BM) * 128, STAGE = TILE + 256 * (WN + WM), WAVES = WN * WM;
     constexpr int LW = BN / 8 / WAVES, LA = BM / 8 / WAVES;      // a wave's copies of eight rows of W and of A
     constexpr int COPIES = LW + LA + 1;                          // and one of scales
     static_assert(LW >= 1 && LA >= 1 && WAVES == WN + WM && (TM == 2 || TM == 4), "");
@@ -239,20 +240,19 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void matmul_fp8_tile_kernel(Matmul
                                                           4u * (unsigned)((end_row - first_row) * scale_ld + blocks), kBufferWord3);
     const unsigned scale_at = 4u * (unsigned)((scale_row - first_row) * scale_ld);
     const unsigned lds0 = (unsigned)(uintptr_t)(InLds)smem;
-    auto copy = [&](int kb) {
-        uint8_t* const to = smem + kb % NST * STAGE;
+    // piece i of a block's copies
+    auto copy = [&](int kb, int i) {
+        uint8_t* const to = smem + (kb & 1) * STAGE;
         const unsigned k = (unsigned)(kb * kScaleCols);
-#pragma unroll
-        for (int i = 0; i < LW; ++i) {
+        if (i < LW) {
             const int x = wave * LW + i, c = c8 ^ ((l8 >> 1) & 1) ^ (((x >> 1) & 3) << 1);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rows, (InLds)(to + x * 1024), 16, (unsigned)(8 * x + l8) * w_ld + (unsigned)(16 * c) + k, 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < LA; ++i) {
-            const int x = wave * LA + i, c = c8 ^ (l8 >> 1) ^ ((x & 1) << 2);
+        } else if (i < LW + LA) {
+            const int x = wave * LA + i - LW, c = c8 ^ (l8 >> 1) ^ ((x & 1) << 2);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rows, (InLds)(to + BN * 128 + x * 1024), 16, (unsigned)(8 * x + l8) * a_ld + (unsigned)(16 * c) + k, 0, 0, 0);
+        } else {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (InLds)(to + TILE + wave * 256), 4, scale_at + 4u * (unsigned)kb, 0, 0, 0);
         }
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (InLds)(to + TILE + wave * 256), 4, scale_at + 4u * (unsigned)kb, 0, 0, 0);
     };
 
     // where this lane finds row r of its first fragments; the others follow at whole multiples of what the keys go by
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void matmul_fp8_tile_kernel(Matmul
     std::conditional_t<ROW_SCALES, f32x4v[4], float[1][4]> ws;
     std::conditional_t<TM == 4, f32x4v, f32x2v> s;
     auto read = [&](int kb) {
-        const unsigned stage = (unsigned)(kb % NST * STAGE);
+        const unsigned stage = (unsigned)((kb & 1) * STAGE);
         read_block(fw, fa, ws, s, Addresses{first.w + stage, first.w1 + stage, first.a + stage, first.a1 + stage, first.ws + stage, first.as + stage});
         if constexpr (!ROW_SCALES) s *= ws[0][0];
         if ((kb + 1) * kScaleCols > a.K) {  // zeros behind column K, in both operands: there may be NaN codes
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void matmul_fp8_tile_kernel(Matmul
                 }
         }
     };
-    auto multiply = [&]() {
+    auto multiply = [&](int next) {         // small tiles copy block `next` in between, if there is one
         // a product's sums are used three products later, so that the matrix unit does not wait for them
         constexpr int kAhead = EXACT ? 1 : 3, kAll = kTN * TM;
         f32x4v d[kAhead + 1];
@@ -327,14 +327,9 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void matmul_fp8_tile_kernel(Matmul
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[j][t][i] = fmaf(ROW_SCALES ? v[i] * ws[ROW_SCALES ? j : 0][i] : v[i], s[t], acc[j][t][i]);
             }
+            if (TM == 2 && p < COPIES && next < blocks) copy(next, p);
             __builtin_amdgcn_sched_barrier(0);
         }
-    };
-    // the wave's copies of a block have arrived once only those of `younger` blocks can be under way
-    auto arrived = [&](int younger) {
-        if (NST > 3 && younger >= 2) wait_vmcnt<(NST > 3 ? 2 * COPIES : 0)>();
-        else if (NST > 2 && younger >= 1) wait_vmcnt<(NST > 2 ? COPIES : 0)>();
-        else wait_vmcnt<0>();
     };
     auto barrier = []() {                   // bare: with the fence of __syncthreads() it would wait for the copies under way
         asm volatile("" : : : "memory");
@@ -342,16 +337,17 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void matmul_fp8_tile_kernel(Matmul
         asm volatile("" : : : "memory");
     };
 
-    // the other workgroups of the compute unit multiply while this one reads
+    if (blocks > 0)
 #pragma unroll
-    for (int k = 0; k < NST - 1; ++k)
-        if (k < blocks) copy(k);
+        for (int i = 0; i < COPIES; ++i) copy(0, i);
     for (int kb = 0; kb < blocks; ++kb) {
-        arrived(min(blocks - 1 - kb, NST - 2));
-        barrier();                      // everybody's have, and nobody reads the block before any more
-        if (kb + NST - 1 < blocks) copy(kb + NST - 1);
+        __builtin_amdgcn_s_waitcnt(0x0F70);         // vmcnt(0): this wave's copies of the block have arrived
+        barrier();                          // everybody's have, and nobody reads the block before any more
+        if (TM == 4 && kb + 1 < blocks)
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) copy(kb + 1, i);
         read(kb);
-        multiply();
+        multiply(kb + 1);
     }
 
     // a lane has sixteen neighbouring n: 32 or 64 bytes of a row of C
@@ -394,24 +390,22 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void matmul_fp8_tile_kernel(Matmul
     }
 }
 
-template <int WN, int WM, int TM, int NST, bool EXACT, bool ROW_SCALES>
+template <int TM, bool EXACT, bool ROW_SCALES>
 hipError_t tiles(const MatmulFp8Args& a, hipStream_t s)
 {
-    constexpr int BN = 64 * WN, BM = 16 * TM * WM;
-    constexpr size_t lds = (size_t)NST * ((BN + BM) * 128 + 256 * (WN + WM));     // tiles and scales
-    static_assert(lds <= 160 * 1024, "");
+    constexpr int BN = 128, BM = 32 * TM;
+    constexpr size_t lds = 2 * (size_t)((BN + BM) * 128 + 4 * 256);     // two blocks, with their scales
     const int tn = (a.N + BN - 1) / BN, tm = (a.M + BM - 1) / BM;
-    const hipError_t e = allow_dynamic_lds((const void*)matmul_fp8_tile_kernel<WN, WM, TM, NST, EXACT, ROW_SCALES>, lds);
+    const hipError_t e = allow_dynamic_lds((const void*)matmul_fp8_tile_kernel<TM, EXACT, ROW_SCALES>, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((matmul_fp8_tile_kernel<WN, WM, TM, NST, EXACT, ROW_SCALES>), dim3(tn * tm), dim3(64 * WN * WM), lds, s, a, tn, tm);
+    hipLaunchKernelGGL((matmul_fp8_tile_kernel<TM, EXACT, ROW_SCALES>), dim3(tn * tm), dim3(256), lds, s, a, tn, tm);
     return hipGetLastError();
 }
-
 template <int TM>
 hipError_t tiles_of(const MatmulFp8Args& a, hipStream_t s)
 {
-    if (a.out_bf16) return a.w_block_rows == 1 ? tiles<2, 2, TM, 2, false, true>(a, s) : tiles<2, 2, TM, 2, false, false>(a, s);
-    return a.w_block_rows == 1 ? tiles<2, 2, TM, 2, true, true>(a, s) : tiles<2, 2, TM, 2, true, false>(a, s);
+    if (a.out_bf16) return a.w_block_rows == 1 ? tiles<TM, false, true>(a, s) : tiles<TM, false, false>(a, s);
+    return a.w_block_rows == 1 ? tiles<TM, true, true>(a, s) : tiles<TM, true, false>(a, s);
 }
 
 // Tiles of 128 by 128 from so many of them on (two to a compute unit), else of 128 by 64.  4800 x 4096 x 800 (1216 tiles): 35
