@@ -6,24 +6,42 @@
 //     gradient: e_t = f_t delta_t (what reaches c_{t-1}),  delta_t = dh_t o_t (1 - tanh^2 c_t) + e_{t+1}
 //               a run of steps maps the e behind it to  A e + U  with the same A
 //
-// One thread takes kScanSteps consecutive steps of one or two neighbouring units with all of their pre-activations in
-// registers; the waves of a workgroup take consecutive runs of steps of the same units (a tile), pass (A, S) through LDS and
-// go on to the next tile with the state in registers.  Where batch and width alone give too few workgroups, time is also cut
-// into segments: a first launch leaves every segment's (A, S) in the workspace, the second starts each segment from the
-// product of those in front of it.
+// One thread takes a run of consecutive steps of one or two neighbouring units with their pre-activations in registers;
+// the waves of a workgroup take consecutive runs of the same units (a tile), pass (A, S) through LDS and go on to the next
+// tile with the state in registers.  Where batch and width alone give too few workgroups, time is also cut into segments: a
+// first launch leaves every segment's (A, S) in the workspace, the second starts each segment from the product of those in
+// front of it.
 #include "device_math.h"
 #include "elem.h"
 #include "lm_ops.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace l355 {
 
 namespace {
 
-constexpr int kScanWaves = 4;                               // waves of a workgroup
-constexpr int kTileSteps = kScanSteps * kScanWaves;         // steps of a tile
-constexpr int kScanTarget = 1024;                           // workgroups aimed at: four on each compute unit
+constexpr int kScanWaves = 4;                       // waves of a workgroup
+constexpr int kRun = 8;                             // steps of a thread in the forward pass; the gradient's are kScanSteps
+constexpr int kScanWhole = 512;                     // so many workgroups without cutting time are enough
+constexpr int kScanTarget = 1024;                   // workgroups aimed at where time is cut: four on each compute unit
+
+// one or two neighbouring elements as loaded
+template <class E, int UPT>
+using Raw = std::conditional_t<UPT == 2, uint32_t, typename E::T>;
+template <class E, int UPT>
+__device__ __forceinline__ void unpack(Raw<E, UPT> r, float (&v)[UPT])
+{
+    if constexpr (UPT == 2) {
+        v[0] = bf16_lo(r);
+        v[1] = bf16_hi(r);
+    } else if constexpr (E::kBytes == 2) {
+        v[0] = __uint_as_float((uint32_t)r << 16);
+    } else {
+        v[0] = r;
+    }
+}
 
 // What one workgroup works on, the same in all of its threads but for the unit
 struct Place {
@@ -50,79 +68,134 @@ __device__ __forceinline__ Place place_of(const ScanArgs& a, int groups, int til
 }
 
 // position in memory of step s < len
-__device__ __forceinline__ int64_t at_step(const ScanArgs& a, int len, int s) { return a.reverse ? len - 1 - s : s; }
+__device__ __forceinline__ int at_step(const ScanArgs& a, int len, int s) { return a.reverse ? len - 1 - s : s; }
 
-// State in front of a segment, or gradient behind it: the (A, S) of the segments in between applied to `v`.
-// ws: [segments][B][H][2]
+// State in front of a segment, or gradient behind it: the (A, S) of `n` segments (first, first + step, ..) applied to `v`.
+// Each wave joins a part of them, eight requested at a time (one after the other their loads took longer than the segment);
+// the parts meet in LDS.  ws: [segments][B][H][2].  Called by the whole workgroup.
 template <int UPT>
-__device__ __forceinline__ void through_segments(const ScanArgs& a, const Place& p, int from, int to, int step, float (&v)[UPT])
+__device__ __forceinline__ void through_segments(const ScanArgs& a, const Place& p, int first, int n, int step, float (&part_a)[kScanWaves][64 * UPT],
+                                                 float (&part_s)[kScanWaves][64 * UPT], float (&v)[UPT])
 {
-    for (int s = from; s != to; s += step) {
-        const float* const w = a.ws + (((int64_t)s * a.B + p.b) * a.H + p.unit) * 2;
+    if (n <= 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int k0 = n * wave / kScanWaves, k1 = n * (wave + 1) / kScanWaves;
+    float A[UPT], S[UPT];
 #pragma unroll
-        for (int u = 0; u < UPT; ++u) v[u] = fmaf(w[2 * u], v[u], w[2 * u + 1]);
+    for (int u = 0; u < UPT; ++u) {
+        A[u] = 1.f;
+        S[u] = 0.f;
     }
+    for (int k = k0; k < k1; k += 8) {
+        float w[8][2 * UPT];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float* const q = a.ws + (((int64_t)(first + min(k + i, k1 - 1) * step) * a.B + p.b) * a.H + p.unit) * 2;
+#pragma unroll
+            for (int u = 0; u < 2 * UPT; ++u) w[i][u] = q[u];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (k + i >= k1) break;
+#pragma unroll
+            for (int u = 0; u < UPT; ++u) {
+                S[u] = fmaf(w[i][2 * u], S[u], w[i][2 * u + 1]);
+                A[u] *= w[i][2 * u];
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < UPT; ++u) {
+        part_a[wave][u * 64 + lane] = A[u];
+        part_s[wave][u * 64 + lane] = S[u];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kScanWaves; ++w)
+#pragma unroll
+        for (int u = 0; u < UPT; ++u) v[u] = fmaf(part_a[w][u * 64 + lane], v[u], part_s[w][u * 64 + lane]);
 }
 
+// Forward.  The next tile is requested as soon as this one's pre-activations have become gates, so that its way from memory
+// is covered by the runs' joining, the second half of the arithmetic and the stores.
 // SUMMARY: only the segment's (A, S), into the workspace.
 template <class E, int UPT, bool SUMMARY>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_forward_kernel(ScanArgs a, int groups, int tiles, int tiles_per_seg)
 {
+    using T = typename E::T;
+    using R = Raw<E, UPT>;
+    constexpr int kTile = kRun * kScanWaves;
     __shared__ float run_a[2][kScanWaves][64 * UPT], run_s[2][kScanWaves][64 * UPT];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place p = place_of<UPT>(a, groups, tiles, tiles_per_seg);
-    const typename E::T* const P = (const typename E::T*)a.P + (int64_t)p.b * a.P_b + p.unit;
-    typename E::T* const h = (typename E::T*)a.h + (int64_t)p.b * a.h_b + p.unit;
+    const T* const P = (const T*)a.P + (int64_t)p.b * a.P_b;        // the same in all lanes; a lane adds its unit
+    T* const h = (T*)a.h + (int64_t)p.b * a.h_b;
+    const int64_t P_step = a.reverse ? -a.P_t : a.P_t, h_step = a.reverse ? -a.h_t : a.h_t;
     float carry[UPT], whole[UPT];
 #pragma unroll
     for (int u = 0; u < UPT; ++u) {
         carry[u] = !SUMMARY && a.c0 ? a.c0[(int64_t)p.b * a.H + p.unit + u] : 0.f;
         whole[u] = 1.f;
     }
-    if (!SUMMARY) through_segments<UPT>(a, p, 0, p.seg, 1, carry);
+    R pf[kRun], pi[kRun], pg[kRun], po[kRun];
+    auto request = [&](int tile) {
+        const int s0 = tile * kTile + wave * kRun, on = min(p.len - s0, kRun);
+        if (tile >= p.tile1 || on <= 0) return;
+        const T* q = P + at_step(a, p.len, s0) * a.P_t;
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) {               // steps behind the end read the last one again: no branch between loads
+            pf[j] = *(const R*)(q + p.unit);
+            pi[j] = *(const R*)(q + a.H + p.unit);
+            pg[j] = *(const R*)(q + 3 * (int64_t)a.H + p.unit);
+            if (!SUMMARY) po[j] = *(const R*)(q + 2 * (int64_t)a.H + p.unit);
+            q += j + 1 < on ? P_step : 0;
+        }
+    };
+    request(p.tile0);
+    if (!SUMMARY) through_segments<UPT>(a, p, 0, p.seg, 1, run_a[1], run_s[1], carry);
     int turn = 0;
     for (int tile = p.tile0; tile < p.tile1; ++tile, turn ^= 1) {
-        const int s0 = tile * kTileSteps + wave * kScanSteps;
-        float f[kScanSteps][UPT], b[kScanSteps][UPT], o[kScanSteps][UPT];
-        const bool any = s0 < p.len;
-        if (any) {
-#pragma unroll
-            for (int j = 0; j < kScanSteps; ++j) {     // steps behind the end read the last one again: no branch between loads
-                const typename E::T* const q = P + at_step(a, p.len, min(s0 + j, p.len - 1)) * a.P_t;
-                float i[UPT], g[UPT];
-                load_n<E, UPT>(q, f[j]);
-                load_n<E, UPT>(q + a.H, i);
-                if (!SUMMARY) load_n<E, UPT>(q + 2 * (int64_t)a.H, o[j]);
-                load_n<E, UPT>(q + 3 * (int64_t)a.H, g);
-                const bool on = s0 + j < p.len;
-#pragma unroll
-                for (int u = 0; u < UPT; ++u) {
-                    f[j][u] = on ? sigmoidf_fast(f[j][u]) : 1.f;
-                    b[j][u] = on ? sigmoidf_fast(i[u]) * tanhf_exact(g[u]) : 0.f;
-                }
-            }
-        }
-        float A[UPT], S[UPT];
+        const int s0 = tile * kTile + wave * kRun;
+        const int on = min(max(p.len - s0, 0), kRun);               // steps of the run that the sequence has
+        float f[kRun][UPT], b[kRun][UPT], o[kRun][UPT], A[UPT], S[UPT];
 #pragma unroll
         for (int u = 0; u < UPT; ++u) {
             A[u] = 1.f;
             S[u] = 0.f;
         }
-        if (any) {
+        // FULL: a run without a branch, which all but the last of a sequence are
+        auto gates = [&](auto full) {
 #pragma unroll
-            for (int j = 0; j < kScanSteps; ++j)
+            for (int j = 0; j < kRun; ++j) {
+                if (!decltype(full)::value && j >= on) continue;
+                float i[UPT], g[UPT];
+                unpack<E, UPT>(pf[j], f[j]);
+                unpack<E, UPT>(pi[j], i);
+                unpack<E, UPT>(pg[j], g);
+                if (!SUMMARY) unpack<E, UPT>(po[j], o[j]);
 #pragma unroll
                 for (int u = 0; u < UPT; ++u) {
+                    f[j][u] = sigmoidf_fast(f[j][u]);
+                    b[j][u] = sigmoidf_fast(i[u]) * tanhf_exact(g[u]);
+                    if (!SUMMARY) o[j][u] = sigmoidf_fast(o[j][u]);
                     S[u] = fmaf(f[j][u], S[u], b[j][u]);
                     A[u] *= f[j][u];
                 }
-        }
+            }
+        };
+        if (on == kRun) gates(std::true_type());
+        else gates(std::false_type());
+        request(tile + 1);
 #pragma unroll
         for (int u = 0; u < UPT; ++u) {
             run_a[turn][wave][u * 64 + lane] = A[u];
             run_s[turn][wave][u * 64 + lane] = S[u];
         }
-        __syncthreads();        // one is enough: the other buffer is written next, and everybody has read it in front of this one
+        // One barrier is enough (the other buffer is written next, and everybody has read it in front of this one), and a bare
+        // one: that of __syncthreads() waits for the loads under way too.
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
         float in[UPT];
 #pragma unroll
         for (int w = 0; w < kScanWaves; ++w)
@@ -133,26 +206,32 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_forward_kernel(ScanArgs 
                 if (SUMMARY) whole[u] *= run_a[turn][w][u * 64 + lane];
             }
         if (SUMMARY) continue;
-        if (a.states && s0 < a.T && p.live)
+        if (a.states && s0 % kScanSteps == 0 && s0 < a.T && p.live)
 #pragma unroll
             for (int u = 0; u < UPT; ++u)
                 a.states[((int64_t)(s0 / kScanSteps) * a.B + p.b) * a.H + p.unit + u] = in[u];
+        auto outputs = [&](auto full) {
+            T* q = h + at_step(a, p.len, s0) * a.h_t + p.unit;
 #pragma unroll
-        for (int j = 0; j < kScanSteps; ++j) {
-            const int s = s0 + j;
-            if (s >= a.T) break;
-            float out[UPT];
-            const bool on = s < p.len;
+            for (int j = 0; j < kRun; ++j) {
+                float out[UPT];
+                if (decltype(full)::value || j < on) {
 #pragma unroll
-            for (int u = 0; u < UPT; ++u) {
-                out[u] = 0.f;
-                if (on) {
-                    in[u] = fmaf(f[j][u], in[u], b[j][u]);
-                    out[u] = sigmoidf_fast(o[j][u]) * tanhf_exact(in[u]);
+                    for (int u = 0; u < UPT; ++u) {
+                        in[u] = fmaf(f[j][u], in[u], b[j][u]);
+                        out[u] = o[j][u] * tanhf_exact(in[u]);
+                    }
+                    if (p.live) store_n<E, UPT>(q, out);
+                    q += h_step;
+                } else if (s0 + j < a.T) {
+#pragma unroll
+                    for (int u = 0; u < UPT; ++u) out[u] = 0.f;
+                    if (p.live) store_n<E, UPT>(h + (s0 + j) * a.h_t + p.unit, out);
                 }
             }
-            if (p.live) store_n<E, UPT>(h + (on ? at_step(a, p.len, s) : (int64_t)s) * a.h_t, out);
-        }
+        };
+        if (on == kRun) outputs(std::true_type());
+        else outputs(std::false_type());
     }
     if (wave != 0 || !p.live) return;
 #pragma unroll
@@ -168,58 +247,72 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_forward_kernel(ScanArgs 
 }
 
 // Gradient: tiles from the last to the first.  The states inside a run of kScanSteps steps are computed again from the one
-// the forward kept in front of it.
+// the forward kept in front of it.  What does not depend on the gradient behind the run - that of the output gate, and
+// dh o (1 - tanh^2 c) - is finished (the first: stored) before the runs are joined, so that five values a step wait in registers.
 template <class E, bool SUMMARY>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_backward_kernel(ScanArgs a, int groups, int tiles, int tiles_per_seg, int segs)
 {
+    using T = typename E::T;
     __shared__ float run_a[2][kScanWaves][64], run_s[2][kScanWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place p = place_of<1>(a, groups, tiles, tiles_per_seg);
-    const typename E::T* const P = (const typename E::T*)a.P + (int64_t)p.b * a.P_b + p.unit;
-    const typename E::T* const dh = (const typename E::T*)a.dh + (int64_t)p.b * a.dh_b + p.unit;
-    typename E::T* const dP = (typename E::T*)a.dP + (int64_t)p.b * a.dP_b + p.unit;
-    const int64_t H = a.H;
+    const T* const P = (const T*)a.P + (int64_t)p.b * a.P_b;
+    const T* const dh = (const T*)a.dh + (int64_t)p.b * a.dh_b;
+    T* const dP = (T*)a.dP + (int64_t)p.b * a.dP_b;
+    const int64_t H = a.H, P_step = a.reverse ? -a.P_t : a.P_t, dh_step = a.reverse ? -a.dh_t : a.dh_t, dP_step = a.reverse ? -a.dP_t : a.dP_t;
     float carry[1] = {!SUMMARY && a.dcT ? a.dcT[(int64_t)p.b * a.H + p.unit] : 0.f}, whole = 1.f;
-    if (!SUMMARY) through_segments<1>(a, p, segs - 1, p.seg, -1, carry);
+    if (!SUMMARY) through_segments<1>(a, p, segs - 1, segs - 1 - p.seg, -1, run_a[1], run_s[1], carry);
     int turn = 0;
     for (int tile = p.tile1 - 1; tile >= p.tile0; --tile, turn ^= 1) {
-        const int s0 = tile * kTileSteps + wave * kScanSteps;
-        float f[kScanSteps], i[kScanSteps], o[kScanSteps], g[kScanSteps], d[kScanSteps], c[kScanSteps];
-        const bool any = s0 < p.len;
+        const int s0 = (tile * kScanWaves + wave) * kScanSteps;
+        const int on = min(max(p.len - s0, 0), kScanSteps);
+        float f[kScanSteps], i[kScanSteps], g[kScanSteps], c[kScanSteps], u[kScanSteps];
         float A = 1.f, U = 0.f;
-        if (any) {
+        // FULL: a run without a branch, which all but the last of a sequence are
+        auto load_run = [&](auto full) {
+            constexpr bool FULL = decltype(full)::value;
+            float o[kScanSteps], d[kScanSteps];
             float state = a.states[((int64_t)(s0 / kScanSteps) * a.B + p.b) * H + p.unit];
+            const int first = at_step(a, p.len, s0);
+            const T *q = P + first * a.P_t, *r = dh + first * a.dh_t;
 #pragma unroll
             for (int j = 0; j < kScanSteps; ++j) {
-                const int64_t pos = at_step(a, p.len, min(s0 + j, p.len - 1));
-                const typename E::T* const q = P + pos * a.P_t;
-                f[j] = E::load(q);
-                i[j] = E::load(q + H);
-                o[j] = E::load(q + 2 * H);
-                g[j] = E::load(q + 3 * H);
-                d[j] = E::load(dh + pos * a.dh_t);
+                f[j] = E::load(q + p.unit);
+                i[j] = E::load(q + H + p.unit);
+                g[j] = E::load(q + 3 * H + p.unit);
+                o[j] = E::load(q + 2 * H + p.unit);
+                d[j] = E::load(r + p.unit);
+                if (FULL || j + 1 < on) {
+                    q += P_step;
+                    r += dh_step;
+                }
             }
+            T* to = dP + first * a.dP_t + 2 * H + p.unit;
 #pragma unroll
             for (int j = 0; j < kScanSteps; ++j) {
+                if (!FULL && j >= on) continue;
                 f[j] = sigmoidf_fast(f[j]);
                 i[j] = sigmoidf_fast(i[j]);
-                o[j] = sigmoidf_fast(o[j]);
                 g[j] = tanhf_exact(g[j]);
                 c[j] = state;       // in front of the step
                 state = fmaf(f[j], state, i[j] * g[j]);
+                const float og = sigmoidf_fast(o[j]), t = tanhf_exact(state), through = d[j] * og;
+                u[j] = through * fmaf(-t, t, 1.f);
+                if (!SUMMARY && p.live) E::store(to, through * t * (1.f - og));
+                to += dP_step;
             }
 #pragma unroll
             for (int j = kScanSteps - 1; j >= 0; --j) {
-                if (s0 + j < p.len) {
-                    const float t = tanhf_exact(fmaf(f[j], c[j], i[j] * g[j]));
-                    U = f[j] * fmaf(d[j] * o[j], fmaf(-t, t, 1.f), U);
-                    A *= f[j];
-                }
+                if (!FULL && j >= on) continue;
+                U = f[j] * (u[j] + U);
+                A *= f[j];
             }
-        }
+        };
+        if (on == kScanSteps) load_run(std::true_type());
+        else if (on > 0) load_run(std::false_type());
         run_a[turn][wave][lane] = A;
         run_s[turn][wave][lane] = U;
-        __syncthreads();
+        __syncthreads();        // one is enough: the other buffer is written next, and everybody has read it in front of this one
         float e = 0.f;
 #pragma unroll
         for (int w = kScanWaves - 1; w >= 0; --w) {
@@ -228,29 +321,28 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_backward_kernel(ScanArgs
             if (SUMMARY) whole *= run_a[turn][w][lane];
         }
         if (SUMMARY) continue;
+        auto store_run = [&](auto full) {
+            constexpr bool FULL = decltype(full)::value;
+            T* q = dP + at_step(a, p.len, s0 + (FULL ? kScanSteps : on) - 1) * a.dP_t + p.unit;
 #pragma unroll
-        for (int j = kScanSteps - 1; j >= 0; --j) {
-            const int s = s0 + j;
-            if (s >= a.T) continue;
-            float df = 0.f, di = 0.f, dout = 0.f, dg = 0.f;
-            const bool on = s < p.len;
-            if (on) {
-                const float t = tanhf_exact(fmaf(f[j], c[j], i[j] * g[j]));
-                const float delta = fmaf(d[j] * o[j], fmaf(-t, t, 1.f), e);
-                e = f[j] * delta;
-                df = e * c[j] * (1.f - f[j]);
-                di = delta * g[j] * i[j] * (1.f - i[j]);
-                dout = d[j] * t * o[j] * (1.f - o[j]);
-                dg = delta * i[j] * fmaf(-g[j], g[j], 1.f);
+            for (int j = kScanSteps - 1; j >= 0; --j) {
+                if (FULL || j < on) {
+                    const float delta = u[j] + e, di = delta * i[j];
+                    e = f[j] * delta;
+                    if (p.live) {
+                        E::store(q, e * c[j] * (1.f - f[j]));
+                        E::store(q + H, di * g[j] * (1.f - i[j]));
+                        E::store(q + 3 * H, di * fmaf(-g[j], g[j], 1.f));
+                    }
+                    q -= dP_step;
+                } else if (s0 + j < a.T && p.live) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) E::store(dP + (s0 + j) * a.dP_t + k * H + p.unit, 0.f);
+                }
             }
-            if (p.live) {
-                typename E::T* const q = dP + (on ? at_step(a, p.len, s) : (int64_t)s) * a.dP_t;
-                E::store(q, df);
-                E::store(q + H, di);
-                E::store(q + 2 * H, dout);
-                E::store(q + 3 * H, dg);
-            }
-        }
+        };
+        if (on == kScanSteps) store_run(std::true_type());
+        else store_run(std::false_type());
     }
     if (wave != 0 || !p.live) return;
     if (SUMMARY) {
@@ -284,39 +376,42 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a)
 struct Cut {
     int groups, tiles, per_seg, segs;
 };
-// How a layer of `H` units with `upt` of them per thread is cut
-Cut cut_of(int T, int B, int H, int upt)
+// How a layer of `H` units with `upt` of them per thread, and tiles of `steps` steps, is cut.  Time is cut only where that leaves
+// compute units idle otherwise: the summary reads three quarters of the pre-activations once more.
+Cut cut_of(int T, int B, int H, int upt, int steps)
 {
     Cut c;
     c.groups = (H + 64 * upt - 1) / (64 * upt);
-    c.tiles = (T + kTileSteps - 1) / kTileSteps;
+    c.tiles = (T + steps - 1) / steps;
     const int64_t wgs = std::max<int64_t>(1, (int64_t)c.groups * B);
-    int segs = (int)std::min<int64_t>(std::max<int64_t>(1, kScanTarget / wgs), std::max(1, c.tiles));
+    const int segs = wgs >= kScanWhole ? 1 : (int)std::min<int64_t>(std::max<int64_t>(1, kScanTarget / wgs), std::max(1, c.tiles));
     c.per_seg = std::max(1, (c.tiles + segs - 1) / segs);
     c.segs = std::max(1, (c.tiles + c.per_seg - 1) / c.per_seg);
     return c;
 }
+Cut forward_cut(int T, int B, int H, int upt) { return cut_of(T, B, H, upt, kRun * kScanWaves); }
+Cut backward_cut(int T, int B, int H) { return cut_of(T, B, H, 1, kScanSteps * kScanWaves); }
 
 }  // namespace
 
-// the larger of the two cuts: one or two units per thread
+// the largest of the cuts: one or two units per thread, forward or back
 size_t scan_workspace_bytes(int T, int B, int H)
 {
-    const int segs = std::max(cut_of(T, B, H, 1).segs, cut_of(T, B, H, 2).segs);
+    const int segs = std::max(std::max(forward_cut(T, B, H, 1).segs, forward_cut(T, B, H, 2).segs), backward_cut(T, B, H).segs);
     return segs < 2 ? 256 : (size_t)segs * B * H * 2 * sizeof(float);
 }
 
 // a grid's threads have to stay under 2^32
 bool scan_fits(int T, int B, int H)
 {
-    const Cut c = cut_of(T, B, H, 1);
+    const Cut c = forward_cut(T, B, H, 1);
     return (int64_t)c.groups * B * c.segs < (1 << 24);
 }
 
 template <class E, int UPT>
 static void forward(const ScanArgs& a, hipStream_t s)
 {
-    const Cut c = cut_of(a.T, a.B, a.H, UPT);
+    const Cut c = forward_cut(a.T, a.B, a.H, UPT);
     const dim3 grid((unsigned)c.groups * a.B * c.segs), block(64 * kScanWaves);
     if (c.segs > 1) hipLaunchKernelGGL((scan_forward_kernel<E, UPT, true>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg);
     hipLaunchKernelGGL((scan_forward_kernel<E, UPT, false>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg);
@@ -340,7 +435,7 @@ hipError_t launch_scan_forward(const ScanArgs& a, hipStream_t s)
 
 hipError_t launch_scan_backward(const ScanArgs& a, hipStream_t s)
 {
-    const Cut c = cut_of(a.T, a.B, a.H, 1);
+    const Cut c = backward_cut(a.T, a.B, a.H);
     const dim3 grid((unsigned)c.groups * a.B * c.segs), block(64 * kScanWaves);
     if (a.bf16) {
         if (c.segs > 1) hipLaunchKernelGGL((scan_backward_kernel<Bf16, true>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
