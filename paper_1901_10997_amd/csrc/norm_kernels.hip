@@ -161,15 +161,16 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_forward_kernel(NormArgs 
     }
 }
 
-// A team of WPR waves takes every teams-th row and keeps the sums of its columns' dw in registers; they go to ws [teams][N].
+// A team of WPR waves takes every teams-th row and keeps its sums of dw in registers; those of a workgroup's teams meet in LDS
+// and go to ws [workgroups][N].
 template <class E, int VEC, int WPR, int IT>
-__global__ __launch_bounds__(kNormThreads) void rmsnorm_backward_kernel(NormGradArgs a, int teams)
+__global__ __launch_bounds__(kNormThreads) void rmsnorm_backward_kernel(NormGradArgs a)
 {
     __shared__ float part[2][4];
+    __shared__ float met[WPR == 1 ? 3 : 1][WPR == 1 ? 512 * IT : 1];
     using T = typename E::T;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int team = blockIdx.x * (4 / WPR) + wave / WPR;
-    if (team >= teams) return;
+    const int team = blockIdx.x * (4 / WPR) + wave / WPR, teams = gridDim.x * (4 / WPR);
     const int col0 = ((wave % WPR) * 64 + lane) * kGranule;
     float dw[IT][kGranule];
 #pragma unroll
@@ -220,28 +221,59 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_backward_kernel(NormGrad
         }
     }
     if (!a.dweight) return;
+    if constexpr (WPR == 1) {
+        // column i of the granules of step k stands at (k * 8 + i) * 64 + lane: every wave's lanes meet different banks
+        if (wave > 0)
+#pragma unroll
+            for (int k = 0; k < IT; ++k)
+#pragma unroll
+                for (int i = 0; i < kGranule; ++i) met[wave - 1][(k * kGranule + i) * 64 + lane] = dw[k][i];
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int w = 0; w < 3; ++w)
+#pragma unroll
+            for (int k = 0; k < IT; ++k)
+#pragma unroll
+                for (int i = 0; i < kGranule; ++i) dw[k][i] += met[w][(k * kGranule + i) * 64 + lane];
+    }
+    float* const to = a.ws + (int64_t)blockIdx.x * a.N;
 #pragma unroll
     for (int k = 0; k < IT; ++k) {
         const int col = col0 + k * WPR * 512;
+        if (VEC > 1) {
+            store_granule<F32, (VEC > 1 ? 4 : 1)>(to, col, a.N, dw[k]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < kGranule; ++i)
-            if (col + i < a.N) a.ws[(int64_t)team * a.N + col + i] = dw[k][i];
+            for (int i = 0; i < kGranule; ++i)
+                if (col + i < a.N) to[col + i] = dw[k][i];
+        }
     }
 }
 
-// dw = sum of the teams' rows, in their order: 32 columns per workgroup, eight threads of each column
-__global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict__ ws, int teams, int N, float* __restrict__ dw)
+// dw = sum of the rows of ws, in their order: 16 columns per workgroup, sixteen threads of each column
+__global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict__ ws, int rows, int N, float* __restrict__ dw)
 {
-    __shared__ float part[8][32];
-    const int c = threadIdx.x & 31, k = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+    __shared__ float part[16][16];
+    const int c = threadIdx.x & 15, k = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
     float sum = 0.f;
-    if (col < N)
-        for (int t = k; t < teams; t += 8) sum += ws[(int64_t)t * N + col];
+    if (col < N) {
+        const float* const p = ws + col;
+        int t = k;
+        for (; t + 112 < rows; t += 128) {      // eight loads under way
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = p[(int64_t)(t + 16 * i) * N];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+        for (; t < rows; t += 16) sum += p[(int64_t)t * N];
+    }
     part[k][c] = sum;
     __syncthreads();
     if (k == 0 && col < N) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) sum += part[i][c];
+        for (int i = 1; i < 16; ++i) sum += part[i][c];
         dw[col] = sum;
     }
 }
@@ -345,7 +377,13 @@ void with_elements(bool bf16, int vec, F f)
     }
 }
 
-int grad_teams(int M) { return std::min(M, 1024); }
+// Workgroups of the gradient for `rows` rows at a time in each: at most kGradGroups, and all with the same number of turns
+constexpr int kGradGroups = 512;
+int grad_groups(int M, int rows)
+{
+    const int all = (M + rows - 1) / rows, turns = (all + kGradGroups - 1) / kGradGroups;
+    return turns < 1 ? 0 : (all + turns - 1) / turns;
+}
 
 }  // namespace
 
@@ -362,20 +400,20 @@ hipError_t launch_rmsnorm_forward(const NormArgs& a, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t rmsnorm_workspace_bytes(int M, int N) { return (size_t)grad_teams(M) * N * sizeof(float); }
+size_t rmsnorm_workspace_bytes(int M, int N) { return (size_t)std::min(M, kGradGroups) * N * sizeof(float); }
 
 hipError_t launch_rmsnorm_backward(const NormGradArgs& a, hipStream_t s)
 {
     const int vec = widest(a.bf16, a.N, {{a.sum, a.sum_ld}, {a.dy, a.dy_ld}, {a.dsum, a.dsum_ld}, {a.dx, a.dx_ld}}, a.weight);
-    const int teams = grad_teams(a.M);
-    if (teams > 0) with_elements(a.bf16, vec, [&](auto e, auto v) {
+    int groups = 0;
+    if (a.M > 0) with_elements(a.bf16, vec, [&](auto e, auto v) {
         with_row_shape(a.M, a.N, [&](auto wpr, auto it) {
             constexpr int kWaves = decltype(wpr)::value;
-            const dim3 grid((teams + 4 / kWaves - 1) / (4 / kWaves)), block(kNormThreads);
-            hipLaunchKernelGGL((rmsnorm_backward_kernel<decltype(e), decltype(v)::value, kWaves, decltype(it)::value>), grid, block, 0, s, a, teams);
+            groups = grad_groups(a.M, 4 / kWaves);
+            hipLaunchKernelGGL((rmsnorm_backward_kernel<decltype(e), decltype(v)::value, kWaves, decltype(it)::value>), dim3(groups), dim3(kNormThreads), 0, s, a);
         });
     });
-    if (a.dweight) hipLaunchKernelGGL(column_sum_kernel, dim3((a.N + 31) / 32), dim3(256), 0, s, a.ws, teams, a.N, a.dweight);
+    if (a.dweight) hipLaunchKernelGGL(column_sum_kernel, dim3((a.N + 15) / 16), dim3(256), 0, s, a.ws, groups, a.N, a.dweight);
     return hipGetLastError();
 }
 
