@@ -9,11 +9,13 @@
 // the cut of the work do not change who is drawn.
 //
 // A workgroup per row; each wave has a run of neighbouring tokens, 256 at a time (four to a lane), which every step reads again
-// from the caches (kept in registers, 32 a lane, the unrolled steps spilled).  A border is found by a histogram over 2048 bins of the logit's distance to the
-// largest one - of counts for top_k, of masses for top_p - and the tokens of the bin in which it lies are compared one by one
-// (kList of them; more than that, in rows of equal or of very far logits, by the digits of the logit's bit pattern).
+// from the caches (kept in registers, 32 a lane, the unrolled steps spilled).  A border is found by a histogram over 2048 bins
+// of the logit's distance to the largest one - of counts for top_k, of masses for top_p - and the tokens of the bin in which it
+// lies are compared one by one (kList of them; more than that, in rows of equal or of very far logits, by the digits of the
+// logit's bit pattern).  The token is found in two steps: the wave in whose run the sum is passed, then that run cut over
+// all threads.
 //
-// Bound: the vector units' 64-bit arithmetic (about 17 instructions a weight) and the barriers between the steps.
+// Bound: the vector units of the row's compute unit, about 25 instructions a weight, and the barriers between the steps.
 #include "elem.h"
 #include "lm_ops.h"
 
@@ -24,14 +26,16 @@ namespace {
 typedef unsigned long long u64;
 constexpr int kBins = 2048, kList = 512, kTable = 1024;
 constexpr int kChunk = 256;         // tokens of a wave at a time
+constexpr int kAhead = 2;           // ... and of these so many are requested at once
+constexpr float kInf = __builtin_inff();
 
-// Bits of a value in ascending order; both zeros are one value.  Every number above minus infinity has a key above 0.
+// Bits of a value in ascending order; both zeros are one value
 __device__ __forceinline__ uint32_t key_of(float v)
 {
     const uint32_t b = __float_as_uint(v + 0.f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
+    return b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key ^ ((uint32_t)((int)~key >> 31) | 0x80000000u)); }
 
 struct Shared {
     union {
@@ -39,13 +43,13 @@ struct Shared {
         unsigned count[kBins];
     };
     double table[kTable];           // 2^(k / 1024)
-    u64 list_weight[kList];
-    uint32_t list_key[kList];
+    u64 list_weight[kList], list_front[kList];
+    float list_value[kList];
     int list_index[kList];
     u64 part[16];
     u64 found_before;
-    unsigned found_digit, listed;
-    uint32_t border_key;
+    unsigned found_bin, listed;
+    float border_value;
     int border_index;
 };
 
@@ -53,24 +57,37 @@ struct Shared {
 // 2^(n / 1024) by table and exponent, 2^(r / 1024) by its series to the third power (r at most a half: 6e-16).
 struct Weights {
     const double* table;
-    double top, scale;
-    uint32_t top_key;
+    double scale, shift;            // y = l scale + shift
+    float top;
     int bits;                       // S, at most 51: adding 2^52 rounds to a whole number in the low bits
-    bool infinite;                  // the largest logit is plus infinity and has all mass
-    __device__ __forceinline__ u64 whole(uint32_t key) const
+    // No branch in here: the chains of several tokens run side by side.  Of minus infinity or NaN it is anything.
+    __device__ __forceinline__ u64 whole(float v) const
     {
-        if (infinite) return key == top_key ? 1ull << bits : 0ull;
-        const double y = fmax(((double)value_of(key) - top) * scale, -1024.0 * 1074.0);
-        const double n = rint(y), r = y - n;
-        const int i = (int)n;
+        const double y = fma((double)v, scale, shift), n = rint(y), r = y - n;
+        int i;                      // the instruction's own saturation: a weight too far down becomes 0
+        asm("v_cvt_i32_f64 %0, %1" : "=v"(i) : "v"(n));
         constexpr double c1 = 6.769015435155716e-4 /* ln 2 / 1024 */, c2 = c1 * c1 / 2, c3 = c1 * c1 * c1 / 6;
         const double p = fma(fma(fma(c3, r, c2), r, c1), r, 1.0);
-        const double v = __builtin_amdgcn_ldexp(table[i & (kTable - 1)] * p, (i >> 10) + bits);
-        return (u64)__double_as_longlong(v + 0x1p52) & 0xfffffffffffffull;
+        const double x = __builtin_amdgcn_ldexp(table[i & (kTable - 1)] * p, (i >> 10) + bits);
+        const u64 w = (u64)__double_as_longlong(x + 0x1p52) & 0xfffffffffffffull;
+        return v == top ? 1ull << bits : w;     // exactly one, plus infinity among them
+    }
+    // of those of four tokens that `wanted` has, 0 of the others
+    __device__ __forceinline__ void whole4(const float (&l)[4], const bool (&wanted)[4], u64 (&v)[4]) const
+    {
+        if (__any(wanted[0] || wanted[1] || wanted[2] || wanted[3])) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = whole(l[e]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = wanted[e] ? v[e] : 0ull;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = 0ull;
+        }
     }
 };
 
-// One row as a workgroup of WAVES waves sees it
+// One row as a workgroup sees it.  A token that is masked (what it holds is not looked at), NaN or behind the row is minus infinity.
 template <class E, int VEC>
 struct Row {
     const typename E::T* logits;
@@ -78,59 +95,73 @@ struct Row {
     int V, first, chunks, lane;     // first: of the wave's tokens
 
     __device__ __forceinline__ int index(int chunk, int e) const { return first + chunk * kChunk + lane * 4 + e; }
-    // keys of four neighbouring tokens; 0: masked (what it holds is not looked at), NaN, minus infinity or behind the row
-    __device__ __forceinline__ void load(int chunk, uint32_t (&k)[4]) const
+    __device__ __forceinline__ float one(int j) const
+    {
+        return j < V && (!allowed || allowed[j]) ? fmaxf(E::load(logits + j), -kInf) : -kInf;
+    }
+    __device__ __forceinline__ void load(int chunk, float (&v)[4]) const
     {
         const int j = index(chunk, 0);
-        float v[4];
-        uint32_t mask = 0x01010101u;
         if (VEC == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = -kInf;
             if (j < V) {            // V is a multiple of four
                 load_n<E, 4>(logits + j, v);
-                if (allowed) mask = *(const uint32_t*)(allowed + j);
-            } else {
-                mask = 0;
+                if (allowed) {
+                    const uint32_t mask = *(const uint32_t*)(allowed + j);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = mask >> (8 * e) & 255u ? v[e] : -kInf;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = fmaxf(v[e], -kInf);      // NaN gives way
             }
         } else {
-            mask = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (j + e < V) {
-                    v[e] = E::load(logits + j + e);
-                    mask |= (allowed ? (uint32_t)allowed[j + e] : 1u) << (8 * e);
-                }
+            for (int e = 0; e < 4; ++e) v[e] = one(j + e);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) k[e] = (mask >> (8 * e) & 255u) && v[e] > -__builtin_inff() ? key_of(v[e]) : 0u;
     }
-    // f(chunk, keys) for the wave's tokens in their order
+    // f(chunk, values) for the wave's tokens in their order
     template <class F>
     __device__ __forceinline__ void each(F f) const
     {
-#pragma unroll 2
-        for (int c = 0; c < chunks; ++c) {
-            uint32_t k[4];
-            load(c, k);
-            f(c, k);
+        for (int c0 = 0; c0 < chunks; c0 += kAhead) {
+            float v[kAhead][4];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) load(c0 + i < chunks ? c0 + i : 1 << 21, v[i]);    // (behind every row: nothing is read)
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) f(c0 + i, v[i]);
         }
     }
 };
 
+template <int CTRL>
+__device__ __forceinline__ u64 moved(u64 v)     // by register moves between lanes; 0 where none comes from
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, 0xF, 0xF, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, 0xF, 0xF, true);
+    return (u64)hi << 32 | lo;
+}
+__device__ __forceinline__ u64 of_lane(u64 v, int lane)
+{
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+// Sum over the lanes up to this one; *total: over all (rows of sixteen lanes by shifts of 1, 2, 4 and 8, then the rows)
+__device__ __forceinline__ u64 wave_scan(u64 v, u64* total)
+{
+    v += moved<0x111>(v);
+    v += moved<0x112>(v);
+    v += moved<0x114>(v);
+    v += moved<0x118>(v);
+    const u64 r0 = of_lane(v, 15), r1 = r0 + of_lane(v, 31), r2 = r1 + of_lane(v, 47);
+    *total = r2 + of_lane(v, 63);
+    const int lane = threadIdx.x & 63;
+    return v + (lane < 16 ? 0ull : lane < 32 ? r0 : lane < 48 ? r1 : r2);
+}
 __device__ __forceinline__ u64 wave_total(u64 v)
 {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
-}
-__device__ __forceinline__ u64 wave_front(u64 v, int lane)     // sum over the lanes in front
-{
-    u64 incl = v;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const u64 up = __shfl_up(incl, off, 64);
-        if (lane >= off) incl += up;
-    }
-    return incl - v;
+    u64 total;
+    wave_scan(v, &total);
+    return total;
 }
 // Sum over the waves in front of this one and over all of them, of a value that every lane of a wave has
 template <int WAVES>
@@ -151,8 +182,8 @@ __device__ __forceinline__ u64 join(u64 v, Shared& sh, u64* total)
     return front;
 }
 
-// The first bin from `last` down to 0 or, DOWN = false, from 0 up, at which base + the sum so far reaches `want`, and the sum in
-// front of it.  Behind a barrier; all threads.
+// The first bin from 0 up (DOWN: from the last down) at which base + the sum so far reaches `want`, and the sum in front of it.
+// Behind a barrier; all threads.
 template <int WAVES, bool MASS, bool DOWN>
 __device__ __forceinline__ void crossing(Shared& sh, u64 base, double want, unsigned* bin, u64* before)
 {
@@ -164,75 +195,69 @@ __device__ __forceinline__ void crossing(Shared& sh, u64 base, double want, unsi
         v[i] = MASS ? sh.mass[b] : sh.count[b];
         sum += v[i];
     }
-    const int lane = threadIdx.x & 63;
-    const u64 inside = wave_front(sum, lane);
-    u64 total;
-    u64 front = base + join<WAVES>(__shfl(inside + sum, 63, 64), sh, &total) + inside;
+    u64 mine, total;
+    const u64 inside = wave_scan(sum, &mine) - sum;
+    u64 front = base + join<WAVES>(mine, sh, &total) + inside;
     if ((double)front < want && (double)(front + sum) >= want) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             if ((double)front < want && (double)(front + v[i]) >= want) {
                 const int at = threadIdx.x * kEach + i;
-                sh.found_digit = DOWN ? kBins - 1 - at : at;
+                sh.found_bin = DOWN ? kBins - 1 - at : at;
                 sh.found_before = front;
             }
             front += v[i];
         }
     }
     __syncthreads();
-    *bin = sh.found_digit;
+    *bin = sh.found_bin;
     *before = sh.found_before;
 }
 
-// The first token in index order at which the running sum of weight(key, index) exceeds `past` (counts: reaches past + 1), given
-// each wave's sum.  One wave finds it and calls found(index, key).
+// The first token in index order at which the running sum of weight(value, index) exceeds `past`, given each wave's sum over its
+// run: found(index, weight) is called by the thread that has it.  All threads.
 template <int WAVES, class R, class W, class F>
-__device__ __forceinline__ void in_order(const R& row, u64 front, u64 mine, double past, W weight, F found)
+__device__ __forceinline__ void in_order(const R& row, Shared& sh, u64 front, u64 mine, double past, W weight, F found)
 {
-    if (!((double)front <= past && (double)(front + mine) > past)) return;
-    bool done = false;
-    row.each([&](int c, const uint32_t (&k)[4]) {
-        if (done) return;
-        u64 w[4], sum = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            w[e] = weight(k[e], row.index(c, e));
-            sum += w[e];
+    if ((double)front <= past && (double)(front + mine) > past && row.lane == 0) {
+        sh.border_index = row.first;
+        sh.found_bin = row.chunks * kChunk;
+        sh.found_before = front;
+    }
+    __syncthreads();
+    const int each = sh.found_bin / (64 * WAVES), j0 = sh.border_index + threadIdx.x * each;     // (a run is whole chunks: no rest)
+    u64 run = sh.found_before, sum = 0, wave_sum, total;
+    for (int i = 0; i < each; ++i) sum += weight(row.one(j0 + i), j0 + i);
+    const u64 upto = wave_scan(sum, &wave_sum);
+    run += join<WAVES>(wave_sum, sh, &total) + upto - sum;
+    if ((double)run <= past && (double)(run + sum) > past)
+        for (int i = 0; i < each; ++i) {
+            const u64 w = weight(row.one(j0 + i), j0 + i);
+            if ((double)run <= past && (double)(run + w) > past) found(j0 + i, w);
+            run += w;
         }
-        const u64 chunk = wave_total(sum);
-        if ((double)(front + chunk) > past) {
-            u64 run = front + wave_front(sum, row.lane);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if ((double)run <= past && (double)(run + w[e]) > past) found(row.index(c, e), k[e]);
-                run += w[e];
-            }
-            done = true;
-        }
-        front += chunk;
-    });
 }
 
 constexpr int kDigitShift[3] = {21, 10, 0};
 constexpr unsigned kDigitMask[3] = {2047u, 2047u, 1023u};
 
-// What stays is every token in front of (key, index) in the order, and that token
+// What stays is every token in front of (value, index) in the order, and that token
 struct Border {
-    uint32_t key;
+    float value;
     int index;
-    __device__ __forceinline__ bool keeps(uint32_t k, int j) const { return k > key || (k == key && j <= index); }
+    __device__ __forceinline__ bool keeps(float v, int j) const { return v > value || (v == value && j <= index); }
 };
 
 // The border among the tokens that `old` keeps: the first token at which the sum of their counts or masses reaches `want`
 // (MASS: share * the sum of all, at least 1).
 template <int WAVES, bool MASS, class R>
-__device__ __forceinline__ Border find_border(const R& row, const Weights& w, Shared& sh, float top, float bins_per_unit, const Border& old, double want)
+__device__ __forceinline__ Border find_border(const R& row, const Weights& w, Shared& sh, float bins_per_unit, const Border& old, double want)
 {
     constexpr int kThreads = 64 * WAVES;
     const int tid = threadIdx.x;
-    auto weight = [&](uint32_t k) -> u64 { return MASS ? w.whole(k) : 1ull; };
-    // a larger distance never has a smaller bin: difference, product and conversion are monotone
-    auto bin_of = [&](uint32_t k) -> unsigned { return k == w.top_key ? 0u : (unsigned)fminf((top - value_of(k)) * bins_per_unit, (float)(kBins - 1)); };
+    auto weight = [&](float v) -> u64 { return MASS ? w.whole(v) : 1ull; };
+    // a larger distance never has a smaller bin: difference, product and conversion are monotone (infinity less itself has bin 0)
+    auto bin_of = [&](float v) -> unsigned { return (unsigned)fminf(fmaxf((w.top - v) * bins_per_unit, 0.f), (float)(kBins - 1)); };
     auto clear = [&]() {
         for (int i = tid; i < kBins; i += kThreads) {
             if (MASS) sh.mass[i] = 0;
@@ -240,17 +265,21 @@ __device__ __forceinline__ Border find_border(const R& row, const Weights& w, Sh
         }
         if (tid == 0) sh.listed = 0;
     };
-    auto add = [&](unsigned b, uint32_t k) {
-        if (MASS) atomicAdd(&sh.mass[b], weight(k));
-        else atomicAdd(&sh.count[b], 1u);
-    };
     __syncthreads();
     clear();
     __syncthreads();
-    row.each([&](int c, const uint32_t (&k)[4]) {
+    row.each([&](int c, const float (&l)[4]) {
+        bool mine[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine[e] = old.keeps(l[e], row.index(c, e));
+        u64 v[4];
+        if (MASS) w.whole4(l, mine, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (k[e] && old.keeps(k[e], row.index(c, e))) add(bin_of(k[e]), k[e]);
+            if (mine[e]) {
+                if (MASS) atomicAdd(&sh.mass[bin_of(l[e])], v[e]);
+                else atomicAdd(&sh.count[bin_of(l[e])], 1u);
+            }
     });
     __syncthreads();
     if (MASS) {
@@ -263,68 +292,91 @@ __device__ __forceinline__ Border find_border(const R& row, const Weights& w, Sh
     u64 before;
     crossing<WAVES, MASS, false>(sh, 0, want, &bin, &before);
     // the tokens of that bin
-    row.each([&](int c, const uint32_t (&k)[4]) {
+    row.each([&](int c, const float (&l)[4]) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int j = row.index(c, e);
-            if (k[e] && old.keeps(k[e], j) && bin_of(k[e]) == bin) {
+            if (bin_of(l[e]) == bin && old.keeps(l[e], j)) {
                 const unsigned at = atomicAdd(&sh.listed, 1u);
                 if (at < kList) {
-                    sh.list_key[at] = k[e];
+                    sh.list_value[at] = l[e];
                     sh.list_index[at] = j;
-                    sh.list_weight[at] = weight(k[e]);
+                    sh.list_weight[at] = weight(l[e]);
+                    sh.list_front[at] = before;
                 }
             }
         }
     });
     __syncthreads();
-    const unsigned listed = sh.listed;
+    const int listed = (int)min(sh.listed, (unsigned)kList + 1);
     if (listed <= kList) {
-        // each against all: the sum in front of it in the order
-        for (unsigned i = tid; i < listed; i += kThreads) {
-            const uint32_t k = sh.list_key[i];
-            const int j = sh.list_index[i];
-            u64 front = before;
-            for (unsigned o = 0; o < listed; ++o) {
-                const uint32_t ko = sh.list_key[o];
-                if (ko > k || (ko == k && sh.list_index[o] < j)) front += sh.list_weight[o];
-            }
-            if ((double)front < want && (double)(front + sh.list_weight[i]) >= want) {
-                sh.border_key = k;
-                sh.border_index = j;
+        // each against all, several threads to each: the sum in front of it in the order
+        const int parts = kThreads / max(listed, 1), i = tid / max(parts, 1), part = tid % max(parts, 1);
+        const int step = max(parts, 1), rounds = parts > 0 ? 1 : (listed + kThreads - 1) / kThreads;
+        for (int k = 0; k < rounds; ++k) {
+            const int me = i + k * kThreads;
+            if (me < listed) {
+                const float v = sh.list_value[me];
+                const int j = sh.list_index[me];
+                u64 front = 0;
+                for (int o = part; o < listed; o += step) {
+                    const float vo = sh.list_value[o];
+                    const u64 wo = sh.list_weight[o];
+                    front += vo > v || (vo == v && sh.list_index[o] < j) ? wo : 0ull;
+                }
+                if (front) atomicAdd(&sh.list_front[me], front);
             }
         }
         __syncthreads();
-        return Border{sh.border_key, sh.border_index};
+        for (int k = tid; k < listed; k += kThreads) {
+            const u64 front = sh.list_front[k];
+            if ((double)front < want && (double)(front + sh.list_weight[k]) >= want) {
+                sh.border_value = sh.list_value[k];
+                sh.border_index = sh.list_index[k];
+            }
+        }
+        __syncthreads();
+        const Border found = {sh.border_value, sh.border_index};
+        __syncthreads();
+        return found;
     }
-    // many: digit by digit of the key, then by index among equal ones
+    // many: digit by digit of the bit pattern, then by index among equal ones
     uint32_t prefix = 0;
     for (int d = 0; d < 3; ++d) {
         __syncthreads();
         clear();
         __syncthreads();
-        row.each([&](int c, const uint32_t (&k)[4]) {
+        row.each([&](int c, const float (&l)[4]) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (k[e] && old.keeps(k[e], row.index(c, e)) && bin_of(k[e]) == bin && (d == 0 || k[e] >> kDigitShift[d - 1] == prefix >> kDigitShift[d - 1]))
-                    add((k[e] >> kDigitShift[d]) & kDigitMask[d], k[e]);
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t k = key_of(l[e]);
+                if (bin_of(l[e]) == bin && old.keeps(l[e], row.index(c, e)) && (d == 0 || k >> kDigitShift[d - 1] == prefix >> kDigitShift[d - 1])) {
+                    const unsigned b = (k >> kDigitShift[d]) & kDigitMask[d];
+                    if (MASS) atomicAdd(&sh.mass[b], weight(l[e]));
+                    else atomicAdd(&sh.count[b], 1u);
+                }
+            }
         });
         __syncthreads();
         unsigned digit;
         crossing<WAVES, MASS, true>(sh, before, want, &digit, &before);
         prefix |= digit << kDigitShift[d];
     }
-    const double nth = ceil((want - (double)before) / (double)weight(prefix));      // 1: the first of the equal ones
-    auto equal = [&](uint32_t k, int j) -> u64 { return k == prefix && old.keeps(k, j); };
+    const float value = value_of(prefix);
+    const double nth = ceil((want - (double)before) / (double)weight(value));       // 1: the first of the equal ones
+    auto equal = [&](float v, int j) -> u64 { return v == value && old.keeps(v, j); };
     u64 count = 0, total;
-    row.each([&](int c, const uint32_t (&k)[4]) {
+    row.each([&](int c, const float (&l)[4]) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) count += equal(k[e], row.index(c, e));
+        for (int e = 0; e < 4; ++e) count += equal(l[e], row.index(c, e));
     });
     const u64 mine = wave_total(count), front = join<WAVES>(mine, sh, &total);
-    in_order<WAVES>(row, front, mine, fmin(nth, (double)total) - 1.0, equal, [&](int j, uint32_t) { sh.border_index = j; });
+    int* const at = (int*)sh.list_index;
+    in_order<WAVES>(row, sh, front, mine, fmin(nth, (double)total) - 1.0, equal, [&](int j, u64) { at[0] = j; });
     __syncthreads();
-    return Border{prefix, sh.border_index};
+    const Border found = {value, at[0]};
+    __syncthreads();
+    return found;
 }
 
 template <class E, int WAVES, int VEC>
@@ -337,100 +389,110 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a, int bi
     row.allowed = a.allowed ? a.allowed + (int64_t)m * a.allowed_ld : nullptr;
     row.V = a.V;
     row.lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), all_chunks = (a.V + kChunk - 1) / kChunk, each = (all_chunks + WAVES - 1) / WAVES;
+    // runs of as many chunks for every wave, of at least four, so that in_order cuts a run without a rest
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), all_chunks = (a.V + kChunk - 1) / kChunk;
+    constexpr int kLeast = 64 * WAVES > kChunk ? 64 * WAVES / kChunk : 1;
+    const int each = ((all_chunks + WAVES - 1) / WAVES + kLeast - 1) / kLeast * kLeast;
     row.first = wave * each * kChunk;
-    row.chunks = max(0, min(each, all_chunks - wave * each));
+    row.chunks = each;
     const float heat = a.temperature ? a.temperature[m] : 1.f;
     const bool greedy = !(heat > 0.f);
     const int top_k = a.top_k ? a.top_k[m] : 0;
     const double top_p = a.top_p ? (double)a.top_p[m] : 1.0, min_p = a.min_p ? fmin((double)a.min_p[m], 1.0) : 0.0;
     for (int i = tid; i < kTable; i += 64 * WAVES) sh.table[i] = exp2((double)i / kTable);
 
-    // largest key, the first token that has it, and how many tokens there are
-    u64 best = 0;                   // key, then the index from the back
-    unsigned there = 0;
-    row.each([&](int c, const uint32_t (&k)[4]) {
+    // the largest logit, and how many tokens there are
+    float best = -kInf;
+    int there = 0;
+    row.each([&](int, const float (&l)[4]) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const u64 v = (u64)k[e] << 32 | (unsigned)(0x7fffffff - row.index(c, e));
-            best = k[e] && v > best ? v : best;
-            there += k[e] != 0;
+            best = fmaxf(best, l[e]);
+            there += __popcll(__ballot(l[e] > -kInf));
         }
     });
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        const u64 o = __shfl_xor(best, off, 64);
-        best = o > best ? o : best;
-        there += __shfl_xor(there, off, 64);
-    }
-    if (row.lane == 0) {
-        sh.part[wave] = best;
-        sh.list_weight[wave] = there;
-    }
+    for (int off = 32; off >= 1; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
+    if (row.lane == 0) sh.part[wave] = (u64)__float_as_uint(best) << 32 | (unsigned)there;
     __syncthreads();
-    u64 tokens = 0;
+    int tokens = 0;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
-        best = sh.part[i] > best ? sh.part[i] : best;
-        tokens += sh.list_weight[i];
+        const u64 p = sh.part[i];
+        best = fmaxf(best, __uint_as_float((uint32_t)(p >> 32)));
+        tokens += (int)(unsigned)p;
     }
-    if (tokens == 0 || greedy) {
+    if (tokens == 0) {
         if (tid == 0) {
-            a.token[m] = tokens ? 0x7fffffff - (int)(unsigned)best : -1;
-            if (a.prob) a.prob[m] = tokens ? 1.f : 0.f;
-            if (a.kept) a.kept[m] = tokens ? 1 : 0;
+            a.token[m] = -1;
+            if (a.prob) a.prob[m] = 0.f;
+            if (a.kept) a.kept[m] = 0;
         }
         return;
     }
-    const float top = value_of((uint32_t)(best >> 32));
+    if (greedy) {
+        int first = 0x7fffffff;
+        row.each([&](int c, const float (&l)[4]) {
+#pragma unroll
+            for (int e = 3; e >= 0; --e)
+                if (l[e] == best) first = min(first, row.index(c, e));
+        });
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) first = min(first, __shfl_xor(first, off, 64));
+        __syncthreads();
+        if (row.lane == 0) sh.list_index[wave] = first;
+        __syncthreads();
+        if (tid == 0) {
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) first = min(first, sh.list_index[i]);
+            a.token[m] = first;
+            if (a.prob) a.prob[m] = 1.f;
+            if (a.kept) a.kept[m] = 1;
+        }
+        return;
+    }
     Weights w;
     w.table = sh.table;
-    w.top = (double)top;
+    w.top = best;
     w.scale = 1024.0 * 1.4426950408889634 / (double)heat;
-    w.top_key = (uint32_t)(best >> 32);
+    w.shift = best == kInf ? -0x1p1000 : -(double)best * w.scale;      // plus infinity: everything else is far below
     w.bits = bits;
-    w.infinite = top == __builtin_inff();
-    const double one = (double)(1ull << bits);
     // 64 bins to a factor of e, over 32 of them; a weight behind that is below 2^-46
     const float bins_per_unit = fminf(64.f / heat, 0x1p100f);
 
-    Border border = {0u, -1};       // all
-    if (top_k > 0 && (u64)top_k < tokens) border = find_border<WAVES, false>(row, w, sh, top, bins_per_unit, border, (double)top_k);
-    if (top_p < 1.0) border = find_border<WAVES, true>(row, w, sh, top, bins_per_unit, border, top_p);
+    Border border = {-kInf, -1};    // all
+    if (top_k > 0 && top_k < tokens) border = find_border<WAVES, false>(row, w, sh, bins_per_unit, border, (double)top_k);
+    if (top_p < 1.0) border = find_border<WAVES, true>(row, w, sh, bins_per_unit, border, top_p);
 
-    const double least = min_p * one;
-    auto kept_weight = [&](uint32_t k, int j, bool* kept) -> u64 {
-        if (k == 0 || !border.keeps(k, j)) return 0;
-        const u64 v = w.whole(k);
-        if ((double)v < least) return 0;
-        *kept = true;
-        return v;
-    };
+    const u64 least = (u64)ceil(fmax(min_p, 0.0) * (double)(1ull << bits));
     u64 mass = 0, total, all_kept;
     unsigned kept = 0;
-    __syncthreads();
-    row.each([&](int c, const uint32_t (&k)[4]) {
+    row.each([&](int c, const float (&l)[4]) {
+        u64 v[4];
+        bool keep[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) keep[e] = border.keeps(l[e], row.index(c, e));
+        w.whole4(l, keep, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            bool here = false;
-            mass += kept_weight(k[e], row.index(c, e), &here);
-            kept += here;
+            const bool stays = keep[e] && v[e] >= least;
+            mass += stays ? v[e] : 0ull;
+            kept += __popcll(__ballot(stays));
         }
     });
     const u64 mine = wave_total(mass);
-    // both sums in one exchange: a row has at most 2^20 tokens
-    join<WAVES>(wave_total(kept), sh, &all_kept);
+    join<WAVES>(kept, sh, &all_kept);
     const u64 front = join<WAVES>(mine, sh, &total);
     const double want = fmin(fmax((double)a.u[m], 0.0), 0x1.fffffep-1) * (double)total;
     in_order<WAVES>(
-        row, front, mine, want,
-        [&](uint32_t k, int j) {
-            bool here;
-            return kept_weight(k, j, &here);
+        row, sh, front, mine, want,
+        [&](float v, int j) -> u64 {
+            const u64 x = w.whole(v);
+            return border.keeps(v, j) && x >= least ? x : 0ull;
         },
-        [&](int j, uint32_t k) {
+        [&](int j, u64 v) {
             a.token[m] = j;
-            if (a.prob) a.prob[m] = (float)((double)w.whole(k) / (double)total);
+            if (a.prob) a.prob[m] = (float)((double)v / (double)total);
         });
     if (tid == 0 && a.kept) a.kept[m] = (int)all_kept;
 }
