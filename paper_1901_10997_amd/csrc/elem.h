@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace l355 {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -11,6 +13,12 @@ typedef float f32x2v __attribute__((ext_vector_type(2)));
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+// the same moved at the alignment of their elements: one access all the same (the processor's unaligned mode, which the
+// compiler relies on for this target)
+typedef f32x4v f32x4v_any __attribute__((aligned(4)));
+typedef uint32_t u32_any __attribute__((aligned(2)));
+typedef u32x2v u32x2v_any __attribute__((aligned(2)));
+typedef u32x4v u32x4v_any __attribute__((aligned(2)));
 
 // nearest-even, NaN stays NaN (the instruction's own rounding)
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
@@ -36,33 +44,34 @@ struct Bf16 {
     static __device__ __forceinline__ float round(float v) { return __uint_as_float((uint32_t)to_bf16(v) << 16); }
 };
 
-// N neighbouring elements; p is aligned to N elements (at most 16 bytes of them)
-template <class E, int N>
+// N neighbouring elements; p is aligned to N elements (at most 16 bytes of them), ANY: to one
+template <class E, int N, bool ANY = false>
 __device__ __forceinline__ void load_n(const typename E::T* p, float* v)
 {
+    using std::conditional_t;
     if constexpr (N == 1) {
         v[0] = E::load(p);
     } else if constexpr (E::kBytes == 4) {
         static_assert(N % 4 == 0, "");
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
-            const f32x4v w = *(const f32x4v*)(p + i);
+            const f32x4v w = *(const conditional_t<ANY, f32x4v_any, f32x4v>*)(p + i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[i + j] = w[j];
         }
     } else if constexpr (N == 2) {
-        const uint32_t w = *(const uint32_t*)p;
+        const uint32_t w = *(const conditional_t<ANY, u32_any, uint32_t>*)p;
         v[0] = bf16_lo(w);
         v[1] = bf16_hi(w);
     } else if constexpr (N == 4) {
-        const u32x2v w = *(const u32x2v*)p;
+        const u32x2v w = *(const conditional_t<ANY, u32x2v_any, u32x2v>*)p;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             v[2 * j] = bf16_lo(w[j]);
             v[2 * j + 1] = bf16_hi(w[j]);
         }
     } else {
-        const u32x4v w = *(const u32x4v*)p;
+        const u32x4v w = *(const conditional_t<ANY, u32x4v_any, u32x4v>*)p;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             v[2 * j] = bf16_lo(w[j]);
@@ -70,20 +79,21 @@ __device__ __forceinline__ void load_n(const typename E::T* p, float* v)
         }
     }
 }
-template <class E, int N>
+template <class E, int N, bool ANY = false>
 __device__ __forceinline__ void store_n(typename E::T* p, const float* v)
 {
+    using std::conditional_t;
     if constexpr (N == 1) {
         E::store(p, v[0]);
     } else if constexpr (E::kBytes == 4) {
 #pragma unroll
-        for (int i = 0; i < N; i += 4) *(f32x4v*)(p + i) = (f32x4v){v[i], v[i + 1], v[i + 2], v[i + 3]};
+        for (int i = 0; i < N; i += 4) *(conditional_t<ANY, f32x4v_any, f32x4v>*)(p + i) = (f32x4v){v[i], v[i + 1], v[i + 2], v[i + 3]};
     } else if constexpr (N == 2) {
-        *(uint32_t*)p = pack_bf16(v[0], v[1]);
+        *(conditional_t<ANY, u32_any, uint32_t>*)p = pack_bf16(v[0], v[1]);
     } else if constexpr (N == 4) {
-        *(u32x2v*)p = (u32x2v){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        *(conditional_t<ANY, u32x2v_any, u32x2v>*)p = (u32x2v){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
     } else {
-        *(u32x4v*)p = (u32x4v){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        *(conditional_t<ANY, u32x4v_any, u32x4v>*)p = (u32x4v){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
     }
 }
 

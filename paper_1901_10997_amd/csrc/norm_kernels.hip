@@ -22,26 +22,29 @@ namespace {
 constexpr int kNormThreads = 256;
 constexpr int kGranule = 8;
 
-// Columns col .. col+7 of a row that has N of them; what lies behind the row is `fill`.  VEC: elements of one access.
-template <class E, int VEC>
-__device__ __forceinline__ void load_granule(const typename E::T* row, int col, int N, float* v, float fill = 0.f)
+// Columns col .. col+7 of a row that has N of them; what lies behind the row is 0.  A granule inside the row is moved in 16-byte
+// pieces wherever it starts (elem.h), so that rows of an odd length cost what those of an even one do: 754 rows of 7671 bf16
+// columns with residual and 8-bit values 13.8 us; with such rows read column by column 31.7.
+template <class E>
+__device__ __forceinline__ void load_granule(const typename E::T* row, int col, int N, float* v)
 {
+    if (col + kGranule <= N) {
+        load_n<E, kGranule, true>(row + col, v);
+    } else {
 #pragma unroll
-    for (int i = 0; i < kGranule; i += VEC) {
-        if (col + i < N) {
-            load_n<E, VEC>(row + col + i, v + i);
-        } else {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) v[i + j] = fill;
-        }
+        for (int i = 0; i < kGranule; ++i) v[i] = col + i < N ? E::load(row + col + i) : 0.f;
     }
 }
-template <class E, int VEC>
+template <class E>
 __device__ __forceinline__ void store_granule(typename E::T* row, int col, int N, const float* v)
 {
+    if (col + kGranule <= N) {
+        store_n<E, kGranule, true>(row + col, v);
+    } else {
 #pragma unroll
-    for (int i = 0; i < kGranule; i += VEC)
-        if (col + i < N) store_n<E, VEC>(row + col + i, v + i);
+        for (int i = 0; i < kGranule; ++i)
+            if (col + i < N) E::store(row + col + i, v[i]);
+    }
 }
 
 // Scale of a block whose largest finite magnitude is amax (an infinity counts as the largest finite value)
@@ -106,7 +109,7 @@ __device__ __forceinline__ float row_sum(float v, float* part)
 }
 
 // WPR waves of a workgroup's four on a row, IT granules per lane: rows of up to 512 WPR IT columns.
-template <class E, int VEC, int WPR, int IT>
+template <class E, int WPR, int IT>
 __global__ __launch_bounds__(kNormThreads) void rmsnorm_forward_kernel(NormArgs a)
 {
     __shared__ float part[4];
@@ -118,13 +121,13 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_forward_kernel(NormArgs 
     const T* const x = (const T*)a.x + (int64_t)row * a.x_ld;
     float v[IT][kGranule], squares = 0.f;
 #pragma unroll
-    for (int k = 0; k < IT; ++k) load_granule<E, VEC>(x, col0 + k * WPR * 512, a.N, v[k]);
+    for (int k = 0; k < IT; ++k) load_granule<E>(x, col0 + k * WPR * 512, a.N, v[k]);
     if (a.residual) {
         const T* const r = (const T*)a.residual + (int64_t)row * a.residual_ld;
 #pragma unroll
         for (int k = 0; k < IT; ++k) {
             float w[kGranule];
-            load_granule<E, VEC>(r, col0 + k * WPR * 512, a.N, w);
+            load_granule<E>(r, col0 + k * WPR * 512, a.N, w);
             // rounded to the type it is kept in, so that the norm, the next layer's residual and the gradient see one value
 #pragma unroll
             for (int i = 0; i < kGranule; ++i) v[k][i] = E::round(v[k][i] + w[i]);
@@ -133,7 +136,7 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_forward_kernel(NormArgs 
     if (a.sum) {
         T* const s = (T*)a.sum + (int64_t)row * a.sum_ld;
 #pragma unroll
-        for (int k = 0; k < IT; ++k) store_granule<E, VEC>(s, col0 + k * WPR * 512, a.N, v[k]);
+        for (int k = 0; k < IT; ++k) store_granule<E>(s, col0 + k * WPR * 512, a.N, v[k]);
     }
 #pragma unroll
     for (int k = 0; k < IT; ++k)
@@ -146,7 +149,7 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_forward_kernel(NormArgs 
         const int col = col0 + k * WPR * 512;
         float w[kGranule];
         if (a.weight) {
-            load_granule<F32, (VEC > 1 ? 4 : 1)>(a.weight, col, a.N, w);
+            load_granule<F32>(a.weight, col, a.N, w);
         } else {
 #pragma unroll
             for (int i = 0; i < kGranule; ++i) w[i] = 1.f;
@@ -156,14 +159,14 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_forward_kernel(NormArgs 
 #pragma unroll
         for (int i = 0; i < kGranule; ++i)      // 0 * infinity behind the row must not reach the block's maximum
             if (col + i >= a.N) v[k][i] = 0.f;
-        if (a.y) store_granule<E, VEC>((T*)a.y + (int64_t)row * a.y_ld, col, a.N, v[k]);
+        if (a.y) store_granule<E>((T*)a.y + (int64_t)row * a.y_ld, col, a.N, v[k]);
         if (a.y8) quantize_granule(v[k], col, a.N, a.y8 + (int64_t)row * a.y8_ld, a.scale + (int64_t)row * a.scale_ld);
     }
 }
 
 // A team of WPR waves takes every teams-th row and keeps its sums of dw in registers; those of a workgroup's teams meet in LDS
 // and go to ws [workgroups][N].
-template <class E, int VEC, int WPR, int IT>
+template <class E, int WPR, int IT>
 __global__ __launch_bounds__(kNormThreads) void rmsnorm_backward_kernel(NormGradArgs a)
 {
     __shared__ float part[2][4];
@@ -185,14 +188,14 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_backward_kernel(NormGrad
         float x[IT][kGranule], g[IT][kGranule], inner = 0.f;
 #pragma unroll
         for (int k = 0; k < IT; ++k) {
-            load_granule<E, VEC>(s, col0 + k * WPR * 512, a.N, x[k]);
-            load_granule<E, VEC>(dy, col0 + k * WPR * 512, a.N, g[k]);
+            load_granule<E>(s, col0 + k * WPR * 512, a.N, x[k]);
+            load_granule<E>(dy, col0 + k * WPR * 512, a.N, g[k]);
         }
 #pragma unroll
         for (int k = 0; k < IT; ++k) {
             float w[kGranule];
             if (a.weight) {
-                load_granule<F32, (VEC > 1 ? 4 : 1)>(a.weight, col0 + k * WPR * 512, a.N, w);
+                load_granule<F32>(a.weight, col0 + k * WPR * 512, a.N, w);
             } else {
 #pragma unroll
                 for (int i = 0; i < kGranule; ++i) w[i] = 1.f;
@@ -210,14 +213,14 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_backward_kernel(NormGrad
         for (int k = 0; k < IT; ++k) {
             float d[kGranule];
             if (a.dsum) {
-                load_granule<E, VEC>((const T*)a.dsum + (int64_t)row * a.dsum_ld, col0 + k * WPR * 512, a.N, d);
+                load_granule<E>((const T*)a.dsum + (int64_t)row * a.dsum_ld, col0 + k * WPR * 512, a.N, d);
             } else {
 #pragma unroll
                 for (int i = 0; i < kGranule; ++i) d[i] = 0.f;
             }
 #pragma unroll
             for (int i = 0; i < kGranule; ++i) d[i] = fmaf(rstd, fmaf(-x[k][i], mean, g[k][i]), d[i]);
-            store_granule<E, VEC>((T*)a.dx + (int64_t)row * a.dx_ld, col0 + k * WPR * 512, a.N, d);
+            store_granule<E>((T*)a.dx + (int64_t)row * a.dx_ld, col0 + k * WPR * 512, a.N, d);
         }
     }
     if (!a.dweight) return;
@@ -239,16 +242,7 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_backward_kernel(NormGrad
     }
     float* const to = a.ws + (int64_t)blockIdx.x * a.N;
 #pragma unroll
-    for (int k = 0; k < IT; ++k) {
-        const int col = col0 + k * WPR * 512;
-        if (VEC > 1) {
-            store_granule<F32, (VEC > 1 ? 4 : 1)>(to, col, a.N, dw[k]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kGranule; ++i)
-                if (col + i < a.N) to[col + i] = dw[k][i];
-        }
-    }
+    for (int k = 0; k < IT; ++k) store_granule<F32>(to, col0 + k * WPR * 512, a.N, dw[k]);
 }
 
 // dw = sum of the rows of ws, in their order: 16 columns per workgroup, sixteen threads of each column
@@ -279,7 +273,7 @@ __global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict
 }
 
 // A scale for every row and 128 columns: a wave takes 512 columns of a row.
-template <class E, int VEC>
+template <class E>
 __global__ __launch_bounds__(kNormThreads) void quantize_rows_kernel(QuantizeArgs a, int parts)
 {
     const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -287,12 +281,12 @@ __global__ __launch_bounds__(kNormThreads) void quantize_rows_kernel(QuantizeArg
     if (row >= a.M) return;
     const int col = ((int)(task % parts) * 64 + (threadIdx.x & 63)) * kGranule;
     float v[kGranule];
-    load_granule<E, VEC>((const typename E::T*)a.x + row * a.x_ld, col, a.N, v);
+    load_granule<E>((const typename E::T*)a.x + row * a.x_ld, col, a.N, v);
     quantize_granule(v, col, a.N, a.q + row * a.q_ld, a.scale + row * a.scale_ld);
 }
 
 // A scale for 128 rows and 128 columns: a workgroup each, sixteen rows at a time.
-template <class E, int VEC>
+template <class E>
 __global__ __launch_bounds__(kNormThreads) void quantize_blocks_kernel(QuantizeArgs a, int parts)
 {
     __shared__ float part[4];
@@ -304,7 +298,7 @@ __global__ __launch_bounds__(kNormThreads) void quantize_blocks_kernel(QuantizeA
     for (int k = 0; k < 8; ++k) {
         const int row = row0 + 16 * k;
         // rows behind the matrix have no columns
-        load_granule<E, VEC>((const typename E::T*)a.x + (int64_t)min(row, a.M - 1) * a.x_ld, col, row < a.M ? a.N : 0, v[k]);
+        load_granule<E>((const typename E::T*)a.x + (int64_t)min(row, a.M - 1) * a.x_ld, col, row < a.M ? a.N : 0, v[k]);
 #pragma unroll
         for (int i = 0; i < kGranule; ++i) amax = fmaxf(amax, fabsf(v[k][i]));
     }
@@ -322,24 +316,6 @@ __global__ __launch_bounds__(kNormThreads) void quantize_blocks_kernel(QuantizeA
         for (int i = 0; i < kGranule; ++i) q[i] = scaled(v[k][i], scale, inverse);
         if (row < a.M) store_e4m3(a.q + (int64_t)row * a.q_ld, col, a.N, pack_e4m3(q));
     }
-}
-
-// Elements of one access that every row of every matrix allows
-struct Rows {
-    const void* p;
-    int64_t ld;
-};
-int widest(bool bf16, int N, std::initializer_list<Rows> all, const float* weight)
-{
-    const int size = bf16 ? 2 : 4;
-    for (int vec = bf16 ? 8 : 4; vec > 1; vec >>= 1) {
-        if (vec == 2) break;
-        bool fits = N % vec == 0 && ((uintptr_t)weight & 15) == 0;
-        for (const Rows& r : all)
-            if (r.p && (r.ld % vec != 0 || ((uintptr_t)r.p & (uintptr_t)(vec * size - 1)) != 0)) fits = false;
-        if (fits) return vec;
-    }
-    return 1;
 }
 
 // The number of waves on a row and of granules per lane: a wave alone needs no barrier, four together take wide rows, and a
@@ -364,17 +340,10 @@ void with_row_shape(int M, int N, F f)
     }
 }
 template <class F>
-void with_elements(bool bf16, int vec, F f)
+void with_elements(bool bf16, F f)
 {
-    using std::integral_constant;
-    if (bf16) {
-        if (vec == 8) f(Bf16(), integral_constant<int, 8>());
-        else if (vec == 4) f(Bf16(), integral_constant<int, 4>());
-        else f(Bf16(), integral_constant<int, 1>());
-    } else {
-        if (vec == 4) f(F32(), integral_constant<int, 4>());
-        else f(F32(), integral_constant<int, 1>());
-    }
+    if (bf16) f(Bf16());
+    else f(F32());
 }
 
 // Workgroups of the gradient for `rows` rows at a time in each: at most kGradGroups, and all with the same number of turns
@@ -389,12 +358,11 @@ int grad_groups(int M, int rows)
 
 hipError_t launch_rmsnorm_forward(const NormArgs& a, hipStream_t s)
 {
-    const int vec = widest(a.bf16, a.N, {{a.x, a.x_ld}, {a.residual, a.residual_ld}, {a.sum, a.sum_ld}, {a.y, a.y_ld}}, a.weight);
-    with_elements(a.bf16, vec, [&](auto e, auto v) {
+    with_elements(a.bf16, [&](auto e) {
         with_row_shape(a.M, a.N, [&](auto wpr, auto it) {
             constexpr int kWaves = decltype(wpr)::value;
             const dim3 grid((a.M + 4 / kWaves - 1) / (4 / kWaves)), block(kNormThreads);
-            hipLaunchKernelGGL((rmsnorm_forward_kernel<decltype(e), decltype(v)::value, kWaves, decltype(it)::value>), grid, block, 0, s, a);
+            hipLaunchKernelGGL((rmsnorm_forward_kernel<decltype(e), kWaves, decltype(it)::value>), grid, block, 0, s, a);
         });
     });
     return hipGetLastError();
@@ -404,13 +372,12 @@ size_t rmsnorm_workspace_bytes(int M, int N) { return (size_t)std::min(M, kGradG
 
 hipError_t launch_rmsnorm_backward(const NormGradArgs& a, hipStream_t s)
 {
-    const int vec = widest(a.bf16, a.N, {{a.sum, a.sum_ld}, {a.dy, a.dy_ld}, {a.dsum, a.dsum_ld}, {a.dx, a.dx_ld}}, a.weight);
     int groups = 0;
-    if (a.M > 0) with_elements(a.bf16, vec, [&](auto e, auto v) {
+    if (a.M > 0) with_elements(a.bf16, [&](auto e) {
         with_row_shape(a.M, a.N, [&](auto wpr, auto it) {
             constexpr int kWaves = decltype(wpr)::value;
             groups = grad_groups(a.M, 4 / kWaves);
-            hipLaunchKernelGGL((rmsnorm_backward_kernel<decltype(e), decltype(v)::value, kWaves, decltype(it)::value>), dim3(groups), dim3(kNormThreads), 0, s, a);
+            hipLaunchKernelGGL((rmsnorm_backward_kernel<decltype(e), kWaves, decltype(it)::value>), dim3(groups), dim3(kNormThreads), 0, s, a);
         });
     });
     if (a.dweight) hipLaunchKernelGGL(column_sum_kernel, dim3((a.N + 15) / 16), dim3(256), 0, s, a.ws, groups, a.N, a.dweight);
@@ -419,16 +386,15 @@ hipError_t launch_rmsnorm_backward(const NormGradArgs& a, hipStream_t s)
 
 hipError_t launch_quantize_fp8(const QuantizeArgs& a, hipStream_t s)
 {
-    const int vec = widest(a.bf16, a.N, {{a.x, a.x_ld}}, nullptr);
-    with_elements(a.bf16, vec, [&](auto e, auto v) {
+    with_elements(a.bf16, [&](auto e) {
         if (a.block_rows == 1) {
             const int parts = (a.N + 511) / 512;
             const dim3 grid((unsigned)(((int64_t)a.M * parts + 3) / 4));
-            hipLaunchKernelGGL((quantize_rows_kernel<decltype(e), decltype(v)::value>), grid, dim3(kNormThreads), 0, s, a, parts);
+            hipLaunchKernelGGL((quantize_rows_kernel<decltype(e)>), grid, dim3(kNormThreads), 0, s, a, parts);
         } else {
             const int parts = (a.N + kScaleCols - 1) / kScaleCols;
             const dim3 grid((unsigned)((int64_t)((a.M + 127) / 128) * parts));
-            hipLaunchKernelGGL((quantize_blocks_kernel<decltype(e), decltype(v)::value>), grid, dim3(kNormThreads), 0, s, a, parts);
+            hipLaunchKernelGGL((quantize_blocks_kernel<decltype(e)>), grid, dim3(kNormThreads), 0, s, a, parts);
         }
     });
     return hipGetLastError();

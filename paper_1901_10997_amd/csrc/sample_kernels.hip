@@ -87,8 +87,10 @@ struct Weights {
     }
 };
 
+typedef uint32_t u32_byte __attribute__((aligned(1)));
+
 // One row as a workgroup sees it.  A token that is masked (what it holds is not looked at), NaN or behind the row is minus infinity.
-template <class E, int VEC>
+template <class E>
 struct Row {
     const typename E::T* logits;
     const uint8_t* allowed;
@@ -102,19 +104,15 @@ struct Row {
     __device__ __forceinline__ void load(int chunk, float (&v)[4]) const
     {
         const int j = index(chunk, 0);
-        if (VEC == 4) {
+        if (j + 4 <= V) {           // in one access each, wherever the row starts
+            load_n<E, 4, true>(logits + j, v);
+            if (allowed) {
+                const uint32_t mask = *(const u32_byte*)(allowed + j);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = -kInf;
-            if (j < V) {            // V is a multiple of four
-                load_n<E, 4>(logits + j, v);
-                if (allowed) {
-                    const uint32_t mask = *(const uint32_t*)(allowed + j);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = mask >> (8 * e) & 255u ? v[e] : -kInf;
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = fmaxf(v[e], -kInf);      // NaN gives way
+                for (int e = 0; e < 4; ++e) v[e] = mask >> (8 * e) & 255u ? v[e] : -kInf;
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = fmaxf(v[e], -kInf);      // NaN gives way
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = one(j + e);
@@ -379,12 +377,12 @@ __device__ __forceinline__ Border find_border(const R& row, const Weights& w, Sh
     return found;
 }
 
-template <class E, int WAVES, int VEC>
+template <class E, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a, int bits)
 {
     __shared__ Shared sh;
     const int m = blockIdx.x, tid = threadIdx.x;
-    Row<E, VEC> row;
+    Row<E> row;
     row.logits = (const typename E::T*)a.logits + (int64_t)m * a.ld;
     row.allowed = a.allowed ? a.allowed + (int64_t)m * a.allowed_ld : nullptr;
     row.V = a.V;
@@ -497,13 +495,13 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a, int bi
     if (tid == 0 && a.kept) a.kept[m] = (int)all_kept;
 }
 
-template <class E, int VEC>
+template <class E>
 void sample(const SampleArgs& a, int bits, hipStream_t s)
 {
     const dim3 grid(a.M);
     // four waves up to 2048 tokens: fewer to wait for at each of some twenty barriers
-    if (a.V <= 2048) hipLaunchKernelGGL((sample_kernel<E, 4, VEC>), grid, dim3(256), 0, s, a, bits);
-    else hipLaunchKernelGGL((sample_kernel<E, 16, VEC>), grid, dim3(1024), 0, s, a, bits);
+    if (a.V <= 2048) hipLaunchKernelGGL((sample_kernel<E, 4>), grid, dim3(256), 0, s, a, bits);
+    else hipLaunchKernelGGL((sample_kernel<E, 16>), grid, dim3(1024), 0, s, a, bits);
 }
 
 }  // namespace
@@ -515,14 +513,8 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t s)
     int bits = 62;          // V weights of at most 1 stay below 2^62
     for (int v = a.V; v > 1; v = (v + 1) / 2) --bits;
     bits = bits < 51 ? bits : 51;
-    const bool fours = a.V % 4 == 0 && a.ld % 4 == 0 && ((uintptr_t)a.logits & (a.bf16 ? 7 : 15)) == 0 && a.allowed_ld % 4 == 0 && ((uintptr_t)a.allowed & 3) == 0;
-    if (a.bf16) {
-        if (fours) sample<Bf16, 4>(a, bits, s);
-        else sample<Bf16, 1>(a, bits, s);
-    } else {
-        if (fours) sample<F32, 4>(a, bits, s);
-        else sample<F32, 1>(a, bits, s);
-    }
+    if (a.bf16) sample<Bf16>(a, bits, s);
+    else sample<F32>(a, bits, s);
     return hipGetLastError();
 }
 

@@ -51,13 +51,13 @@ struct Place {
 };
 
 template <int UPT>
-__device__ __forceinline__ Place place_of(const ScanArgs& a, int groups, int tiles, int tiles_per_seg)
+__device__ __forceinline__ Place place_of(const ScanArgs& a, int groups, int tiles, int tiles_per_seg, int first_seg = 0)
 {
     Place p;
     const unsigned blk = blockIdx.x, per_b = (unsigned)groups;
     const unsigned g = blk % per_b, rest = blk / per_b;
     p.b = (int)(rest % (unsigned)a.B);
-    p.seg = (int)(rest / (unsigned)a.B);
+    p.seg = first_seg + (int)(rest / (unsigned)a.B);
     p.len = a.lengths ? min(max(a.lengths[p.b], 0), a.T) : a.T;
     const int unit = (int)(g * 64 + (threadIdx.x & 63)) * UPT;
     p.live = unit < a.H;
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_backward_kernel(ScanArgs
     using T = typename E::T;
     __shared__ float run_a[2][kScanWaves][64], run_s[2][kScanWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place p = place_of<1>(a, groups, tiles, tiles_per_seg);
+    const Place p = place_of<1>(a, groups, tiles, tiles_per_seg, SUMMARY ? 1 : 0);      // nothing precedes segment 0
     const T* const P = (const T*)a.P + (int64_t)p.b * a.P_b;
     const T* const dh = (const T*)a.dh + (int64_t)p.b * a.dh_b;
     T* const dP = (T*)a.dP + (int64_t)p.b * a.dP_b;
@@ -413,7 +413,8 @@ static void forward(const ScanArgs& a, hipStream_t s)
 {
     const Cut c = forward_cut(a.T, a.B, a.H, UPT);
     const dim3 grid((unsigned)c.groups * a.B * c.segs), block(64 * kScanWaves);
-    if (c.segs > 1) hipLaunchKernelGGL((scan_forward_kernel<E, UPT, true>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg);
+    const dim3 but_last((unsigned)c.groups * a.B * (c.segs - 1));      // nothing follows the last segment
+    if (c.segs > 1) hipLaunchKernelGGL((scan_forward_kernel<E, UPT, true>), but_last, block, 0, s, a, c.groups, c.tiles, c.per_seg);
     hipLaunchKernelGGL((scan_forward_kernel<E, UPT, false>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg);
 }
 
@@ -436,12 +437,12 @@ hipError_t launch_scan_forward(const ScanArgs& a, hipStream_t s)
 hipError_t launch_scan_backward(const ScanArgs& a, hipStream_t s)
 {
     const Cut c = backward_cut(a.T, a.B, a.H);
-    const dim3 grid((unsigned)c.groups * a.B * c.segs), block(64 * kScanWaves);
+    const dim3 grid((unsigned)c.groups * a.B * c.segs), but_first((unsigned)c.groups * a.B * (c.segs - 1)), block(64 * kScanWaves);
     if (a.bf16) {
-        if (c.segs > 1) hipLaunchKernelGGL((scan_backward_kernel<Bf16, true>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
+        if (c.segs > 1) hipLaunchKernelGGL((scan_backward_kernel<Bf16, true>), but_first, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
         hipLaunchKernelGGL((scan_backward_kernel<Bf16, false>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
     } else {
-        if (c.segs > 1) hipLaunchKernelGGL((scan_backward_kernel<F32, true>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
+        if (c.segs > 1) hipLaunchKernelGGL((scan_backward_kernel<F32, true>), but_first, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
         hipLaunchKernelGGL((scan_backward_kernel<F32, false>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
     }
     return hipGetLastError();
