@@ -9,8 +9,10 @@
 // One thread takes a run of consecutive steps of one or two neighbouring units with their pre-activations in registers;
 // the waves of a workgroup take consecutive runs of the same units (a tile), pass (A, S) through LDS and go on to the next
 // tile with the state in registers.  Where batch and width alone give too few workgroups, time is also cut into segments: a
-// first launch leaves every segment's (A, S) in the workspace, the second starts each segment from the product of those in
-// front of it.
+// first launch leaves the segments' (A, S) in the workspace, the second starts each segment from the product of those in
+// front of it.  The final state may overwrite the first one, and workgroups of the second launch may start when others have
+// ended: so the first launch puts the first state into its segment's S, and beside them where the segment that starts from it
+// finds it.
 #include "device_math.h"
 #include "elem.h"
 #include "lm_ops.h"
@@ -70,9 +72,12 @@ __device__ __forceinline__ Place place_of(const ScanArgs& a, int groups, int til
 // position in memory of step s < len
 __device__ __forceinline__ int at_step(const ScanArgs& a, int len, int s) { return a.reverse ? len - 1 - s : s; }
 
+// (A, S) of a segment.  ws: [segments][B][H][2]
+__device__ __forceinline__ float* slot(const ScanArgs& a, const Place& p, int seg, int u) { return a.ws + (((int64_t)seg * a.B + p.b) * a.H + p.unit + u) * 2; }
+
 // State in front of a segment, or gradient behind it: the (A, S) of `n` segments (first, first + step, ..) applied to `v`.
 // Each wave joins a part of them, eight requested at a time (one after the other their loads took longer than the segment);
-// the parts meet in LDS.  ws: [segments][B][H][2].  Called by the whole workgroup.
+// the parts meet in LDS.  Called by the whole workgroup.
 template <int UPT>
 __device__ __forceinline__ void through_segments(const ScanArgs& a, const Place& p, int first, int n, int step, float (&part_a)[kScanWaves][64 * UPT],
                                                  float (&part_s)[kScanWaves][64 * UPT], float (&v)[UPT])
@@ -90,7 +95,7 @@ __device__ __forceinline__ void through_segments(const ScanArgs& a, const Place&
         float w[8][2 * UPT];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float* const q = a.ws + (((int64_t)(first + min(k + i, k1 - 1) * step) * a.B + p.b) * a.H + p.unit) * 2;
+            const float* const q = slot(a, p, first + min(k + i, k1 - 1) * step, 0);
 #pragma unroll
             for (int u = 0; u < 2 * UPT; ++u) w[i][u] = q[u];
         }
@@ -120,7 +125,7 @@ __device__ __forceinline__ void through_segments(const ScanArgs& a, const Place&
 // is covered by the runs' joining, the second half of the arithmetic and the stores.
 // SUMMARY: only the segment's (A, S), into the workspace.
 template <class E, int UPT, bool SUMMARY>
-__global__ __launch_bounds__(64 * kScanWaves) void scan_forward_kernel(ScanArgs a, int groups, int tiles, int tiles_per_seg)
+__global__ __launch_bounds__(64 * kScanWaves) void scan_forward_kernel(ScanArgs a, int groups, int tiles, int tiles_per_seg, int segs)
 {
     using T = typename E::T;
     using R = Raw<E, UPT>;
@@ -134,9 +139,12 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_forward_kernel(ScanArgs 
     float carry[UPT], whole[UPT];
 #pragma unroll
     for (int u = 0; u < UPT; ++u) {
-        carry[u] = !SUMMARY && a.c0 ? a.c0[(int64_t)p.b * a.H + p.unit + u] : 0.f;
+        carry[u] = 0.f;
         whole[u] = 1.f;
     }
+    if (!SUMMARY && a.c0 && p.seg == 0)
+#pragma unroll
+        for (int u = 0; u < UPT; ++u) carry[u] = segs > 1 ? slot(a, p, segs - 1, u)[0] : a.c0[(int64_t)p.b * a.H + p.unit + u];
     R pf[kRun], pi[kRun], pg[kRun], po[kRun];
     auto request = [&](int tile) {
         const int s0 = tile * kTile + wave * kRun, on = min(p.len - s0, kRun);
@@ -237,7 +245,13 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_forward_kernel(ScanArgs 
 #pragma unroll
     for (int u = 0; u < UPT; ++u) {
         if (SUMMARY) {
-            float* const w = a.ws + (((int64_t)p.seg * a.B + p.b) * a.H + p.unit + u) * 2;
+            float* const w = slot(a, p, p.seg, u);
+            if (p.seg == 0 && a.c0) {
+                const float c0 = a.c0[(int64_t)p.b * a.H + p.unit + u];
+                slot(a, p, segs - 1, u)[0] = c0;            // whose own is not needed
+                carry[u] = fmaf(whole[u], c0, carry[u]);
+                whole[u] = 0.f;
+            }
             w[0] = whole[u];
             w[1] = carry[u];
         } else if (a.cT && p.tile1 == tiles) {
@@ -260,7 +274,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_backward_kernel(ScanArgs
     const T* const dh = (const T*)a.dh + (int64_t)p.b * a.dh_b;
     T* const dP = (T*)a.dP + (int64_t)p.b * a.dP_b;
     const int64_t H = a.H, P_step = a.reverse ? -a.P_t : a.P_t, dh_step = a.reverse ? -a.dh_t : a.dh_t, dP_step = a.reverse ? -a.dP_t : a.dP_t;
-    float carry[1] = {!SUMMARY && a.dcT ? a.dcT[(int64_t)p.b * a.H + p.unit] : 0.f}, whole = 1.f;
+    const bool last = p.seg == segs - 1 && a.dcT;
+    float carry[1] = {SUMMARY || !last ? 0.f : segs > 1 ? slot(a, p, 0, 0)[0] : a.dcT[(int64_t)p.b * a.H + p.unit]}, whole = 1.f;
     if (!SUMMARY) through_segments<1>(a, p, segs - 1, segs - 1 - p.seg, -1, run_a[1], run_s[1], carry);
     int turn = 0;
     for (int tile = p.tile1 - 1; tile >= p.tile0; --tile, turn ^= 1) {
@@ -346,9 +361,11 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_backward_kernel(ScanArgs
     }
     if (wave != 0 || !p.live) return;
     if (SUMMARY) {
-        float* const w = a.ws + (((int64_t)p.seg * a.B + p.b) * H + p.unit) * 2;
-        w[0] = whole;
-        w[1] = carry[0];
+        float* const w = slot(a, p, p.seg, 0);
+        const float dcT = last ? a.dcT[(int64_t)p.b * a.H + p.unit] : 0.f;
+        w[0] = last ? 0.f : whole;
+        w[1] = fmaf(whole, dcT, carry[0]);
+        if (last) slot(a, p, 0, 0)[0] = dcT;                // whose own is not needed
     } else if (a.dc0 && p.seg == 0) {
         a.dc0[(int64_t)p.b * H + p.unit] = carry[0];
     }
@@ -414,8 +431,8 @@ static void forward(const ScanArgs& a, hipStream_t s)
     const Cut c = forward_cut(a.T, a.B, a.H, UPT);
     const dim3 grid((unsigned)c.groups * a.B * c.segs), block(64 * kScanWaves);
     const dim3 but_last((unsigned)c.groups * a.B * (c.segs - 1));      // nothing follows the last segment
-    if (c.segs > 1) hipLaunchKernelGGL((scan_forward_kernel<E, UPT, true>), but_last, block, 0, s, a, c.groups, c.tiles, c.per_seg);
-    hipLaunchKernelGGL((scan_forward_kernel<E, UPT, false>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg);
+    if (c.segs > 1) hipLaunchKernelGGL((scan_forward_kernel<E, UPT, true>), but_last, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
+    hipLaunchKernelGGL((scan_forward_kernel<E, UPT, false>), grid, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
 }
 
 hipError_t launch_scan_forward(const ScanArgs& a, hipStream_t s)
