@@ -8,14 +8,16 @@
 // Weights are evaluated in 64 bits and summed as 64-bit whole numbers: a sum has the same bits in every order, so atomics and
 // the cut of the work do not change who is drawn.
 //
-// A workgroup per row; each wave has a run of neighbouring tokens, 256 at a time (four to a lane), which every step reads again
-// from the caches (kept in registers, 32 a lane, the unrolled steps spilled).  A border is found by a histogram over 2048 bins
-// of the logit's distance to the largest one - of counts for top_k, of masses for top_p - and the tokens of the bin in which it
-// lies are compared one by one (kList of them; more than that, in rows of equal or of very far logits, by the digits of the
-// logit's bit pattern).  The token is found in two steps: the wave in whose run the sum is passed, then that run cut over
-// all threads.
+// A workgroup per row; each wave has a run of neighbouring tokens, 256 at a time (four to a lane).  Every step reads them again,
+// from LDS where the row fits there (HELD: masks and NaN done), else from the caches (in registers, 32 a lane, the unrolled
+// steps spilled).  A border is found by a histogram over 2048 bins of the logit's distance to the largest one - of counts for
+// top_k, of masses for top_p - and the tokens of the bin in which it lies are compared one by one (kList of them; more than
+// that, in rows of equal or of very far logits, by the digits of the logit's bit pattern).  The token is found in two steps:
+// the wave in whose run the sum is passed, then that run cut over all threads.
 //
-// Bound: the vector units of the row's compute unit, about 25 instructions a weight, and the barriers between the steps.
+// Bound: the vector units of the row's compute unit, about 25 instructions a weight, and the sixteen barriers between the
+// steps (256 rows of 32 000 bf16 with mixed settings and masks: 45 us; one row of 10 000 with top_k and top_p 18, of 1000 10).
+#include "common.h"
 #include "elem.h"
 #include "lm_ops.h"
 
@@ -26,8 +28,15 @@ namespace {
 typedef unsigned long long u64;
 constexpr int kBins = 2048, kList = 512, kTable = 1024;
 constexpr int kChunk = 256;         // tokens of a wave at a time
-constexpr int kAhead = 2;           // ... and of these so many are requested at once
+constexpr int kAhead = 2;           // ... and of these so many are requested at once from memory
 constexpr float kInf = __builtin_inff();
+// A row is held where it fits beside Shared, up to 28 672 fp32 and 57 344 bf16 tokens.  us held and read again from the caches,
+// top_k 50 and top_p 0.95: one row of 10 000 fp32 18.2 and 22.0, 28 000 25.9 and 33.4, 512 rows of 4000 26.7 and 30.9, of 28 000
+// 59 and 82; 2048 rows of 2000 42.0 and 39.7, whose smaller workgroups are fewer on a compute unit then (the mixed settings there
+// 35.3 and 35.7).
+constexpr size_t kHeldBytes = 112 << 10;
+// chunks of each of `waves` runs over a row
+__host__ __device__ constexpr int chunks_of(int V, int waves) { return ((V + kChunk - 1) / kChunk + waves - 1) / waves; }
 
 // Bits of a value in ascending order; both zeros are one value
 __device__ __forceinline__ uint32_t key_of(float v)
@@ -46,7 +55,7 @@ struct Shared {
     u64 list_weight[kList], list_front[kList];
     float list_value[kList];
     int list_index[kList];
-    u64 part[16];
+    u64 part[2][16], kept[16];
     u64 found_before;
     unsigned found_bin, listed;
     float border_value;
@@ -90,17 +99,20 @@ struct Weights {
 typedef uint32_t u32_byte __attribute__((aligned(1)));
 
 // One row as a workgroup sees it.  A token that is masked (what it holds is not looked at), NaN or behind the row is minus infinity.
-template <class E>
+template <class E, bool HELD>
 struct Row {
     const typename E::T* logits;
     const uint8_t* allowed;
+    typename E::T* held;
     int V, first, chunks, lane;     // first: of the wave's tokens
 
     __device__ __forceinline__ int index(int chunk, int e) const { return first + chunk * kChunk + lane * 4 + e; }
     __device__ __forceinline__ float one(int j) const
     {
-        return j < V && (!allowed || allowed[j]) ? fmaxf(E::load(logits + j), -kInf) : -kInf;
+        if (HELD) return E::load(held + j);
+        return j < V ? from_memory(j) : -kInf;
     }
+    __device__ __forceinline__ float from_memory(int j) const { return !allowed || allowed[j] ? fmaxf(E::load(logits + j), -kInf) : -kInf; }
     __device__ __forceinline__ void load(int chunk, float (&v)[4]) const
     {
         const int j = index(chunk, 0);
@@ -115,19 +127,33 @@ struct Row {
             for (int e = 0; e < 4; ++e) v[e] = fmaxf(v[e], -kInf);      // NaN gives way
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = one(j + e);
+            for (int e = 0; e < 4; ++e) v[e] = j + e < V ? from_memory(j + e) : -kInf;
         }
     }
-    // f(chunk, values) for the wave's tokens in their order
     template <class F>
-    __device__ __forceinline__ void each(F f) const
+    __device__ __forceinline__ void each_from_memory(F f) const
     {
         for (int c0 = 0; c0 < chunks; c0 += kAhead) {
             float v[kAhead][4];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) load(c0 + i < chunks ? c0 + i : 1 << 21, v[i]);    // (behind every row: nothing is read)
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) f(c0 + i, v[i]);
+            for (int i = 0; i < kAhead; ++i)
+                if (c0 + i < chunks) f(c0 + i, v[i]);
+        }
+    }
+    // f(chunk, values) for the wave's tokens in their order
+    template <class F>
+    __device__ __forceinline__ void each(F f) const
+    {
+        if constexpr (HELD) {
+            for (int c = 0; c < chunks; ++c) {
+                float v[4];
+                load_n<E, 4>(held + index(c, 0), v);
+                f(c, v);
+            }
+        } else {
+            each_from_memory(f);
         }
     }
 };
@@ -161,18 +187,20 @@ __device__ __forceinline__ u64 wave_total(u64 v)
     wave_scan(v, &total);
     return total;
 }
-// Sum over the waves in front of this one and over all of them, of a value that every lane of a wave has
+// Sum over the waves in front of this one and over all of them, of a value that every lane of a wave has.  Its barrier is the only
+// one: what the next join writes is the other half of `part`, and this half again only behind the next one's barrier.
 template <int WAVES>
-__device__ __forceinline__ u64 join(u64 v, Shared& sh, u64* total)
+__device__ __forceinline__ u64 join(u64 v, Shared& sh, int& turn, u64* total)
 {
     const int wave = threadIdx.x >> 6;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.part[wave] = v;
+    u64* const part = sh.part[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) part[wave] = v;
     __syncthreads();
     u64 front = 0, all = 0;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
-        const u64 p = sh.part[i];
+        const u64 p = part[i];
         if (i < wave) front += p;
         all += p;
     }
@@ -181,9 +209,10 @@ __device__ __forceinline__ u64 join(u64 v, Shared& sh, u64* total)
 }
 
 // The first bin from 0 up (DOWN: from the last down) at which base + the sum so far reaches `want`, and the sum in front of it.
-// Behind a barrier; all threads.
-template <int WAVES, bool MASS, bool DOWN>
-__device__ __forceinline__ void crossing(Shared& sh, u64 base, double want, unsigned* bin, u64* before)
+// SHARE: `want` comes as a share of the bins' sum and becomes that part of it, at least 1 (the likeliest token always stays).
+// Behind a barrier; all threads.  Nobody reads the bins after it.
+template <int WAVES, bool MASS, bool DOWN, bool SHARE>
+__device__ __forceinline__ void crossing(Shared& sh, int& turn, u64 base, double& want, unsigned* bin, u64* before)
 {
     constexpr int kEach = kBins / (64 * WAVES);
     u64 v[kEach], sum = 0;
@@ -195,7 +224,8 @@ __device__ __forceinline__ void crossing(Shared& sh, u64 base, double want, unsi
     }
     u64 mine, total;
     const u64 inside = wave_scan(sum, &mine) - sum;
-    u64 front = base + join<WAVES>(mine, sh, &total) + inside;
+    u64 front = base + join<WAVES>(mine, sh, turn, &total) + inside;
+    if (SHARE) want = fmax(want * (double)total, 1.0);
     if ((double)front < want && (double)(front + sum) >= want) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
@@ -215,7 +245,7 @@ __device__ __forceinline__ void crossing(Shared& sh, u64 base, double want, unsi
 // The first token in index order at which the running sum of weight(value, index) exceeds `past`, given each wave's sum over its
 // run: found(index, weight) is called by the thread that has it.  All threads.
 template <int WAVES, class R, class W, class F>
-__device__ __forceinline__ void in_order(const R& row, Shared& sh, u64 front, u64 mine, double past, W weight, F found)
+__device__ __forceinline__ void in_order(const R& row, Shared& sh, int& turn, u64 front, u64 mine, double past, W weight, F found)
 {
     if ((double)front <= past && (double)(front + mine) > past && row.lane == 0) {
         sh.border_index = row.first;
@@ -223,11 +253,12 @@ __device__ __forceinline__ void in_order(const R& row, Shared& sh, u64 front, u6
         sh.found_before = front;
     }
     __syncthreads();
-    const int each = sh.found_bin / (64 * WAVES), j0 = sh.border_index + threadIdx.x * each;     // (a run is whole chunks: no rest)
+    const int n = sh.found_bin, share = (n + 64 * WAVES - 1) / (64 * WAVES), j0 = sh.border_index + min(threadIdx.x * share, n);
+    const int each = min(share, sh.border_index + n - j0);
     u64 run = sh.found_before, sum = 0, wave_sum, total;
     for (int i = 0; i < each; ++i) sum += weight(row.one(j0 + i), j0 + i);
     const u64 upto = wave_scan(sum, &wave_sum);
-    run += join<WAVES>(wave_sum, sh, &total) + upto - sum;
+    run += join<WAVES>(wave_sum, sh, turn, &total) + upto - sum;
     if ((double)run <= past && (double)(run + sum) > past)
         for (int i = 0; i < each; ++i) {
             const u64 w = weight(row.one(j0 + i), j0 + i);
@@ -246,26 +277,23 @@ struct Border {
     __device__ __forceinline__ bool keeps(float v, int j) const { return v > value || (v == value && j <= index); }
 };
 
+template <int WAVES>
+__device__ __forceinline__ void clear_bins(Shared& sh)
+{
+    for (int i = threadIdx.x; i < kBins; i += 64 * WAVES) sh.mass[i] = 0;
+}
+
 // The border among the tokens that `old` keeps: the first token at which the sum of their counts or masses reaches `want`
-// (MASS: share * the sum of all, at least 1).
+// (MASS: share * the sum of all, at least 1).  Bins and `listed` are zero, a barrier behind, and are left so for the next
+// barrier.
 template <int WAVES, bool MASS, class R>
-__device__ __forceinline__ Border find_border(const R& row, const Weights& w, Shared& sh, float bins_per_unit, const Border& old, double want)
+__device__ __forceinline__ Border find_border(const R& row, const Weights& w, Shared& sh, int& turn, float bins_per_unit, const Border& old, double want)
 {
     constexpr int kThreads = 64 * WAVES;
     const int tid = threadIdx.x;
     auto weight = [&](float v) -> u64 { return MASS ? w.whole(v) : 1ull; };
     // a larger distance never has a smaller bin: difference, product and conversion are monotone (infinity less itself has bin 0)
     auto bin_of = [&](float v) -> unsigned { return (unsigned)fminf(fmaxf((w.top - v) * bins_per_unit, 0.f), (float)(kBins - 1)); };
-    auto clear = [&]() {
-        for (int i = tid; i < kBins; i += kThreads) {
-            if (MASS) sh.mass[i] = 0;
-            else sh.count[i] = 0;
-        }
-        if (tid == 0) sh.listed = 0;
-    };
-    __syncthreads();
-    clear();
-    __syncthreads();
     row.each([&](int c, const float (&l)[4]) {
         bool mine[4];
 #pragma unroll
@@ -280,15 +308,10 @@ __device__ __forceinline__ Border find_border(const R& row, const Weights& w, Sh
             }
     });
     __syncthreads();
-    if (MASS) {
-        u64 sum = 0, total;
-        for (int i = tid; i < kBins; i += kThreads) sum += sh.mass[i];
-        join<WAVES>(wave_total(sum), sh, &total);
-        want = fmax(want * (double)total, 1.0);     // the likeliest token always stays
-    }
     unsigned bin;
     u64 before;
-    crossing<WAVES, MASS, false>(sh, 0, want, &bin, &before);
+    crossing<WAVES, MASS, false, MASS>(sh, turn, 0, want, &bin, &before);
+    clear_bins<WAVES>(sh);
     // the tokens of that bin
     row.each([&](int c, const float (&l)[4]) {
 #pragma unroll
@@ -333,16 +356,13 @@ __device__ __forceinline__ Border find_border(const R& row, const Weights& w, Sh
                 sh.border_index = sh.list_index[k];
             }
         }
+        if (tid == 0) sh.listed = 0;            // everybody has read it
         __syncthreads();
-        const Border found = {sh.border_value, sh.border_index};
-        __syncthreads();
-        return found;
+        return {sh.border_value, sh.border_index};
     }
     // many: digit by digit of the bit pattern, then by index among equal ones
     uint32_t prefix = 0;
     for (int d = 0; d < 3; ++d) {
-        __syncthreads();
-        clear();
         __syncthreads();
         row.each([&](int c, const float (&l)[4]) {
 #pragma unroll
@@ -357,7 +377,8 @@ __device__ __forceinline__ Border find_border(const R& row, const Weights& w, Sh
         });
         __syncthreads();
         unsigned digit;
-        crossing<WAVES, MASS, true>(sh, before, want, &digit, &before);
+        crossing<WAVES, MASS, true, false>(sh, turn, before, want, &digit, &before);
+        clear_bins<WAVES>(sh);
         prefix |= digit << kDigitShift[d];
     }
     const float value = value_of(prefix);
@@ -368,41 +389,43 @@ __device__ __forceinline__ Border find_border(const R& row, const Weights& w, Sh
 #pragma unroll
         for (int e = 0; e < 4; ++e) count += equal(l[e], row.index(c, e));
     });
-    const u64 mine = wave_total(count), front = join<WAVES>(mine, sh, &total);
+    const u64 mine = wave_total(count), front = join<WAVES>(mine, sh, turn, &total);
+    if (tid == 0) sh.listed = 0;
     int* const at = (int*)sh.list_index;
-    in_order<WAVES>(row, sh, front, mine, fmin(nth, (double)total) - 1.0, equal, [&](int j, u64) { at[0] = j; });
+    in_order<WAVES>(row, sh, turn, front, mine, fmin(nth, (double)total) - 1.0, equal, [&](int j, u64) { at[0] = j; });
     __syncthreads();
-    const Border found = {value, at[0]};
-    __syncthreads();
-    return found;
+    return {value, at[0]};
 }
 
-template <class E, int WAVES>
+template <class E, int WAVES, bool HELD>
 __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a, int bits)
 {
     __shared__ Shared sh;
+    extern __shared__ __attribute__((aligned(16))) uint8_t held_row[];
     const int m = blockIdx.x, tid = threadIdx.x;
-    Row<E> row;
+    int turn = 1;                   // part[0] is used here
+    Row<E, HELD> row;
+    row.held = (typename E::T*)held_row;
     row.logits = (const typename E::T*)a.logits + (int64_t)m * a.ld;
     row.allowed = a.allowed ? a.allowed + (int64_t)m * a.allowed_ld : nullptr;
     row.V = a.V;
     row.lane = tid & 63;
-    // runs of as many chunks for every wave, of at least four, so that in_order cuts a run without a rest
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), all_chunks = (a.V + kChunk - 1) / kChunk;
-    constexpr int kLeast = 64 * WAVES > kChunk ? 64 * WAVES / kChunk : 1;
-    const int each = ((all_chunks + WAVES - 1) / WAVES + kLeast - 1) / kLeast * kLeast;
-    row.first = wave * each * kChunk;
-    row.chunks = each;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    row.chunks = chunks_of(a.V, WAVES);
+    row.first = wave * row.chunks * kChunk;
     const float heat = a.temperature ? a.temperature[m] : 1.f;
     const bool greedy = !(heat > 0.f);
     const int top_k = a.top_k ? a.top_k[m] : 0;
     const double top_p = a.top_p ? (double)a.top_p[m] : 1.0, min_p = a.min_p ? fmin((double)a.min_p[m], 1.0) : 0.0;
     for (int i = tid; i < kTable; i += 64 * WAVES) sh.table[i] = exp2((double)i / kTable);
+    clear_bins<WAVES>(sh);
+    if (tid == 0) sh.listed = 0;
 
     // the largest logit, and how many tokens there are
     float best = -kInf;
     int there = 0;
-    row.each([&](int, const float (&l)[4]) {
+    row.each_from_memory([&](int c, const float (&l)[4]) {
+        if (HELD) store_n<E, 4>(row.held + row.index(c, 0), l);     // a value of the type, or minus infinity
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             best = fmaxf(best, l[e]);
@@ -411,12 +434,12 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a, int bi
     });
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
-    if (row.lane == 0) sh.part[wave] = (u64)__float_as_uint(best) << 32 | (unsigned)there;
+    if (row.lane == 0) sh.part[0][wave] = (u64)__float_as_uint(best) << 32 | (unsigned)there;
     __syncthreads();
     int tokens = 0;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
-        const u64 p = sh.part[i];
+        const u64 p = sh.part[0][i];
         best = fmaxf(best, __uint_as_float((uint32_t)(p >> 32)));
         tokens += (int)(unsigned)p;
     }
@@ -437,7 +460,6 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a, int bi
         });
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) first = min(first, __shfl_xor(first, off, 64));
-        __syncthreads();
         if (row.lane == 0) sh.list_index[wave] = first;
         __syncthreads();
         if (tid == 0) {
@@ -455,15 +477,17 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a, int bi
     w.scale = 1024.0 * 1.4426950408889634 / (double)heat;
     w.shift = best == kInf ? -0x1p1000 : -(double)best * w.scale;      // plus infinity: everything else is far below
     w.bits = bits;
-    // 64 bins to a factor of e, over 32 of them; a weight behind that is below 2^-46
-    const float bins_per_unit = fminf(64.f / heat, 0x1p100f);
+    // Masses: 64 bins to a factor of e, over 32 of them; a weight behind that is below 2^-46.  Counts: 64 to a unit of the logit
+    // whatever the temperature (by the weights a cold row's last bin held hundreds: 256 rows of 1000 with mixed settings took 31 us).
+    constexpr float kCountBins = 64.f;
+    const float mass_bins = fminf(64.f / heat, 0x1p100f);
 
     Border border = {-kInf, -1};    // all
-    if (top_k > 0 && top_k < tokens) border = find_border<WAVES, false>(row, w, sh, bins_per_unit, border, (double)top_k);
-    if (top_p < 1.0) border = find_border<WAVES, true>(row, w, sh, bins_per_unit, border, top_p);
+    if (top_k > 0 && top_k < tokens) border = find_border<WAVES, false>(row, w, sh, turn, kCountBins, border, (double)top_k);
+    if (top_p < 1.0) border = find_border<WAVES, true>(row, w, sh, turn, mass_bins, border, top_p);
 
     const u64 least = (u64)ceil(fmax(min_p, 0.0) * (double)(1ull << bits));
-    u64 mass = 0, total, all_kept;
+    u64 mass = 0, total;
     unsigned kept = 0;
     row.each([&](int c, const float (&l)[4]) {
         u64 v[4];
@@ -479,11 +503,15 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a, int bi
         }
     });
     const u64 mine = wave_total(mass);
-    join<WAVES>(kept, sh, &all_kept);
-    const u64 front = join<WAVES>(mine, sh, &total);
+    if (row.lane == 0) sh.kept[wave] = kept;
+    const u64 front = join<WAVES>(mine, sh, turn, &total);
+    if (tid == 0 && a.kept) {
+        for (int i = 1; i < WAVES; ++i) kept += (unsigned)sh.kept[i];
+        a.kept[m] = (int)kept;
+    }
     const double want = fmin(fmax((double)a.u[m], 0.0), 0x1.fffffep-1) * (double)total;
     in_order<WAVES>(
-        row, sh, front, mine, want,
+        row, sh, turn, front, mine, want,
         [&](float v, int j) -> u64 {
             const u64 x = w.whole(v);
             return border.keeps(v, j) && x >= least ? x : 0ull;
@@ -492,16 +520,20 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a, int bi
             a.token[m] = j;
             if (a.prob) a.prob[m] = (float)((double)v / (double)total);
         });
-    if (tid == 0 && a.kept) a.kept[m] = (int)all_kept;
 }
 
-template <class E>
-void sample(const SampleArgs& a, int bits, hipStream_t s)
+template <class E, int WAVES>
+hipError_t sample(const SampleArgs& a, int bits, hipStream_t s)
 {
-    const dim3 grid(a.M);
-    // four waves up to 2048 tokens: fewer to wait for at each of some twenty barriers
-    if (a.V <= 2048) hipLaunchKernelGGL((sample_kernel<E, 4>), grid, dim3(256), 0, s, a, bits);
-    else hipLaunchKernelGGL((sample_kernel<E, 16>), grid, dim3(1024), 0, s, a, bits);
+    const size_t held = (size_t)WAVES * chunks_of(a.V, WAVES) * kChunk * E::kBytes;
+    if (held > kHeldBytes) {
+        hipLaunchKernelGGL((sample_kernel<E, WAVES, false>), dim3(a.M), dim3(64 * WAVES), 0, s, a, bits);
+        return hipGetLastError();
+    }
+    const hipError_t e = allow_dynamic_lds((const void*)sample_kernel<E, WAVES, true>, held);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((sample_kernel<E, WAVES, true>), dim3(a.M), dim3(64 * WAVES), held, s, a, bits);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -513,9 +545,9 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t s)
     int bits = 62;          // V weights of at most 1 stay below 2^62
     for (int v = a.V; v > 1; v = (v + 1) / 2) --bits;
     bits = bits < 51 ? bits : 51;
-    if (a.bf16) sample<Bf16>(a, bits, s);
-    else sample<F32>(a, bits, s);
-    return hipGetLastError();
+    // four waves up to 2048 tokens: fewer to wait for at each barrier
+    if (a.V <= 2048) return a.bf16 ? sample<Bf16, 4>(a, bits, s) : sample<F32, 4>(a, bits, s);
+    return a.bf16 ? sample<Bf16, 16>(a, bits, s) : sample<F32, 16>(a, bits, s);
 }
 
 }  // namespace l355
