@@ -26,7 +26,6 @@ namespace {
 
 constexpr int kScanWaves = 4;                       // waves of a workgroup
 constexpr int kRun = 8;                             // steps of a thread in the forward pass; the gradient's are kScanSteps
-constexpr int kScanWhole = 512;                     // so many workgroups without cutting time are enough
 constexpr int kScanTarget = 1024;                   // workgroups aimed at where time is cut: four on each compute unit
 
 // one or two neighbouring elements as loaded
@@ -393,42 +392,51 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a)
 struct Cut {
     int groups, tiles, per_seg, segs;
 };
-// How a layer of `H` units with `upt` of them per thread, and tiles of `steps` steps, is cut.  Time is cut only where that leaves
-// compute units idle otherwise: the summary reads three quarters of the pre-activations once more.
-Cut cut_of(int T, int B, int H, int upt, int steps)
+// How a layer of `H` units with `upt` of them per thread, and tiles of `steps` steps, is cut: not from `whole` workgroups on, nor
+// for fewer than `least` tiles.
+Cut cut_of(int T, int B, int H, int upt, int steps, int whole, int least)
 {
     Cut c;
     c.groups = (H + 64 * upt - 1) / (64 * upt);
     c.tiles = (T + steps - 1) / steps;
     const int64_t wgs = std::max<int64_t>(1, (int64_t)c.groups * B);
-    const int segs = wgs >= kScanWhole ? 1 : (int)std::min<int64_t>(std::max<int64_t>(1, kScanTarget / wgs), std::max(1, c.tiles));
+    const int segs = wgs >= whole || c.tiles < least ? 1 : (int)std::min<int64_t>(std::max<int64_t>(1, kScanTarget / wgs), std::max(1, c.tiles));
     c.per_seg = std::max(1, (c.tiles + segs - 1) / segs);
     c.segs = std::max(1, (c.tiles + c.per_seg - 1) / c.per_seg);
     return c;
 }
-Cut forward_cut(int T, int B, int H, int upt) { return cut_of(T, B, H, upt, kRun * kScanWaves); }
-Cut backward_cut(int T, int B, int H) { return cut_of(T, B, H, 1, kScanSteps * kScanWaves); }
+// The summaries read three quarters of the pre-activations once more in the forward pass, and everything in the gradient's, so
+// cutting pays while a tile is a chain of waits: up to three workgroups for four compute units forward, one for two back; some
+// more where sequences have lengths of their own and the longest alone would hold its workgroups.  us without and with the cut at
+// 1500 units, fp32, batch 6, 8 and 12 (144, 192, 288 workgroups): forward of 300 steps 27 and 26, 29 and 31, 36 and 45; gradient
+// of 1500 steps at batch 4 (96) 165 and 118 to bf16, 121 and 118 to fp32, at batch 6 136 and 177; with lengths, forward of 300
+// steps at batch 8 28 and 25, at batch 12 32 and 34, gradient at batch 8 37 and 41.  Of few tiles the second launch costs more
+// than it gives (64 steps, batch 1: 5.3 and 6.9).
+Cut forward_cut(int T, int B, int H, int upt, bool lengths) { return cut_of(T, B, H, upt, kRun * kScanWaves, lengths ? 256 : 176, 4); }
+Cut backward_cut(int T, int B, int H, bool lengths) { return cut_of(T, B, H, 1, kScanSteps * kScanWaves, lengths ? 176 : 128, 3); }
 
 }  // namespace
 
-// the largest of the cuts: one or two units per thread, forward or back
+// the largest of the cuts: one or two units per thread, forward or back, with lengths or without
 size_t scan_workspace_bytes(int T, int B, int H)
 {
-    const int segs = std::max(std::max(forward_cut(T, B, H, 1).segs, forward_cut(T, B, H, 2).segs), backward_cut(T, B, H).segs);
+    int segs = 1;
+    for (const bool lengths : {false, true})
+        segs = std::max({segs, forward_cut(T, B, H, 1, lengths).segs, forward_cut(T, B, H, 2, lengths).segs, backward_cut(T, B, H, lengths).segs});
     return segs < 2 ? 256 : (size_t)segs * B * H * 2 * sizeof(float);
 }
 
 // a grid's threads have to stay under 2^32
 bool scan_fits(int T, int B, int H)
 {
-    const Cut c = forward_cut(T, B, H, 1);
+    const Cut c = forward_cut(T, B, H, 1, true);
     return (int64_t)c.groups * B * c.segs < (1 << 24);
 }
 
 template <class E, int UPT>
 static void forward(const ScanArgs& a, hipStream_t s)
 {
-    const Cut c = forward_cut(a.T, a.B, a.H, UPT);
+    const Cut c = forward_cut(a.T, a.B, a.H, UPT, a.lengths != nullptr);
     const dim3 grid((unsigned)c.groups * a.B * c.segs), block(64 * kScanWaves);
     const dim3 but_last((unsigned)c.groups * a.B * (c.segs - 1));      // nothing follows the last segment
     if (c.segs > 1) hipLaunchKernelGGL((scan_forward_kernel<E, UPT, true>), but_last, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
@@ -453,7 +461,7 @@ hipError_t launch_scan_forward(const ScanArgs& a, hipStream_t s)
 
 hipError_t launch_scan_backward(const ScanArgs& a, hipStream_t s)
 {
-    const Cut c = backward_cut(a.T, a.B, a.H);
+    const Cut c = backward_cut(a.T, a.B, a.H, a.lengths != nullptr);
     const dim3 grid((unsigned)c.groups * a.B * c.segs), but_first((unsigned)c.groups * a.B * (c.segs - 1)), block(64 * kScanWaves);
     if (a.bf16) {
         if (c.segs > 1) hipLaunchKernelGGL((scan_backward_kernel<Bf16, true>), but_first, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
