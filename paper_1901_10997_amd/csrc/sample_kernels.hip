@@ -16,7 +16,7 @@
 // the wave in whose run the sum is passed, then that run cut over all threads.
 //
 // Bound: the vector units of the row's compute unit, about 25 instructions a weight, and the sixteen barriers between the
-// steps (256 rows of 32 000 bf16 with mixed settings and masks: 45 us; one row of 10 000 with top_k and top_p 18, of 1000 10).
+// steps (256 rows of 32 000 bf16 with mixed settings and masks: 35 us; one row of 10 000 with top_k and top_p 16.6).
 #include "common.h"
 #include "elem.h"
 #include "lm_ops.h"
@@ -30,8 +30,8 @@ constexpr int kBins = 2048, kList = 512, kTable = 1024;
 constexpr int kChunk = 256;         // tokens of a wave at a time
 constexpr int kAhead = 2;           // ... and of these so many are requested at once from memory
 constexpr float kInf = __builtin_inff();
-// A row is held where it fits beside Shared, up to 28 672 fp32 and 57 344 bf16 tokens.  us held and read again from the caches,
-// top_k 50 and top_p 0.95: one row of 10 000 fp32 18.2 and 22.0, 28 000 25.9 and 33.4, 512 rows of 4000 26.7 and 30.9, of 28 000
+// A row is held where it fits beside Shared, up to 28 672 fp32 and 57 344 bf16 tokens.  us held and read again from the caches
+// (both before each_kept), top_k 50 and top_p 0.95: one row of 10 000 fp32 18.2 and 22.0, 28 000 25.9 and 33.4, 512 rows of 4000 26.7 and 30.9, of 28 000
 // 59 and 82; 2048 rows of 2000 42.0 and 39.7, whose smaller workgroups are fewer on a compute unit then (the mixed settings there
 // 35.3 and 35.7).
 constexpr size_t kHeldBytes = 112 << 10;
@@ -56,6 +56,7 @@ struct Shared {
     float list_value[kList];
     int list_index[kList];
     u64 part[2][16], kept[16];
+    float gathered[16][128];        // of each wave: what each_kept waits with
     u64 found_before;
     unsigned found_bin, listed;
     float border_value;
@@ -277,6 +278,39 @@ struct Border {
     __device__ __forceinline__ bool keeps(float v, int j) const { return v > value || (v == value && j <= index); }
 };
 
+// f(value, there) for the wave's tokens that the border keeps, in any order, 64 of them at a time: a border mostly leaves a few
+// tokens in every 256, whose weights would cost as much as those of all (one row of 10 000 words 18.1 us so, 256 rows of 32 000
+// bf16 with mixed settings 40.9; gathered 16.6 and 34.8).  All lanes call f; `there` says whether a lane has one.
+template <class R, class F>
+__device__ __forceinline__ void each_kept(const R& row, const Border& border, float* gathered, F f)
+{
+    int n = 0;
+    auto in_order_of_this_wave = []() {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    row.each([&](int c, const float (&l)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool mine = border.keeps(l[e], row.index(c, e));
+            const u64 all = __ballot(mine);
+            if (all == 0) continue;
+            if (mine) gathered[n + __popcll(all & ((1ull << row.lane) - 1))] = l[e];
+            n += __popcll(all);
+            if (n < 64) continue;
+            in_order_of_this_wave();
+            n -= 64;
+            const float v = gathered[n + row.lane];
+            in_order_of_this_wave();
+            f(v, true);
+        }
+    });
+    if (n == 0) return;
+    in_order_of_this_wave();
+    const bool there = row.lane < n;
+    f(gathered[there ? row.lane : 0], there);
+}
+
 template <int WAVES>
 __device__ __forceinline__ void clear_bins(Shared& sh)
 {
@@ -294,19 +328,26 @@ __device__ __forceinline__ Border find_border(const R& row, const Weights& w, Sh
     auto weight = [&](float v) -> u64 { return MASS ? w.whole(v) : 1ull; };
     // a larger distance never has a smaller bin: difference, product and conversion are monotone (infinity less itself has bin 0)
     auto bin_of = [&](float v) -> unsigned { return (unsigned)fminf(fmaxf((w.top - v) * bins_per_unit, 0.f), (float)(kBins - 1)); };
-    row.each([&](int c, const float (&l)[4]) {
-        bool mine[4];
+    if (MASS && old.value > -kInf) {
+        each_kept(row, old, sh.gathered[tid >> 6], [&](float v, bool there) {
+            const u64 x = weight(v);
+            if (there) atomicAdd(&sh.mass[bin_of(v)], x);
+        });
+    } else {
+        row.each([&](int c, const float (&l)[4]) {
+            bool mine[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mine[e] = old.keeps(l[e], row.index(c, e));
-        u64 v[4];
-        if (MASS) w.whole4(l, mine, v);
+            for (int e = 0; e < 4; ++e) mine[e] = old.keeps(l[e], row.index(c, e));
+            u64 v[4];
+            if (MASS) w.whole4(l, mine, v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (mine[e]) {
-                if (MASS) atomicAdd(&sh.mass[bin_of(l[e])], v[e]);
-                else atomicAdd(&sh.count[bin_of(l[e])], 1u);
-            }
-    });
+            for (int e = 0; e < 4; ++e)
+                if (mine[e]) {
+                    if (MASS) atomicAdd(&sh.mass[bin_of(l[e])], v[e]);
+                    else atomicAdd(&sh.count[bin_of(l[e])], 1u);
+                }
+        });
+    }
     __syncthreads();
     unsigned bin;
     u64 before;
@@ -489,19 +530,28 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a, int bi
     const u64 least = (u64)ceil(fmax(min_p, 0.0) * (double)(1ull << bits));
     u64 mass = 0, total;
     unsigned kept = 0;
-    row.each([&](int c, const float (&l)[4]) {
-        u64 v[4];
-        bool keep[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) keep[e] = border.keeps(l[e], row.index(c, e));
-        w.whole4(l, keep, v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const bool stays = keep[e] && v[e] >= least;
-            mass += stays ? v[e] : 0ull;
+    if (border.value > -kInf) {
+        each_kept(row, border, sh.gathered[wave], [&](float v, bool there) {
+            const u64 x = w.whole(v);
+            const bool stays = there && x >= least;
+            mass += stays ? x : 0ull;
             kept += __popcll(__ballot(stays));
-        }
-    });
+        });
+    } else {
+        row.each([&](int c, const float (&l)[4]) {
+            u64 v[4];
+            bool keep[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) keep[e] = border.keeps(l[e], row.index(c, e));
+            w.whole4(l, keep, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool stays = keep[e] && v[e] >= least;
+                mass += stays ? v[e] : 0ull;
+                kept += __popcll(__ballot(stays));
+            }
+        });
+    }
     const u64 mine = wave_total(mass);
     if (row.lane == 0) sh.kept[wave] = kept;
     const u64 front = join<WAVES>(mine, sh, turn, &total);
