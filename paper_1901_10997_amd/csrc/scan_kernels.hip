@@ -411,8 +411,13 @@ Cut cut_of(int T, int B, int H, int upt, int steps, int whole, int least)
 // 1500 units, fp32, batch 6, 8 and 12 (144, 192, 288 workgroups): forward of 300 steps 27 and 26, 29 and 31, 36 and 45; gradient
 // of 1500 steps at batch 4 (96) 165 and 118 to bf16, 121 and 118 to fp32, at batch 6 136 and 177; with lengths, forward of 300
 // steps at batch 8 28 and 25, at batch 12 32 and 34, gradient at batch 8 37 and 41.  Of few tiles the second launch costs more
-// than it gives (64 steps, batch 1: 5.3 and 6.9).
-Cut forward_cut(int T, int B, int H, int upt, bool lengths) { return cut_of(T, B, H, upt, kRun * kScanWaves, lengths ? 256 : 176, 4); }
+// than it gives (64 steps, batch 1: 5.3 and 6.9), of many the chain grows longer (bf16, 201 units at batch 47, 188 workgroups:
+// 100 steps 10.1 and 10.7, 300 22 and 21, 1500 101 and 77, 6000 396 and 288; at batch 80, 320 workgroups, 1500 steps 112 and 126).
+Cut forward_cut(int T, int B, int H, int upt, bool lengths)
+{
+    constexpr int kTile = kRun * kScanWaves, kManyTiles = 16;
+    return cut_of(T, B, H, upt, kTile, lengths || T > (kManyTiles - 1) * kTile ? 256 : 176, 4);
+}
 Cut backward_cut(int T, int B, int H, bool lengths) { return cut_of(T, B, H, 1, kScanSteps * kScanWaves, lengths ? 176 : 128, 3); }
 
 }  // namespace
