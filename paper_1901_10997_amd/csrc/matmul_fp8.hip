@@ -134,67 +134,52 @@ __global__ __launch_bounds__(64 * kRowsWaves) void matmul_fp8_rows_kernel(Matmul
 // Sixteen-byte chunk c of row r stands at chunk c ^ key(r), and lanes (r, g) read chunks g and g + 4, so that the lanes that
 // are served together meet different banks (chunks 2 g and 2 g + 1 cost twice the reads).
 //
-// Bound: the path from L2 to LDS.  16384 x 8192 x 2048 to bf16 takes 343 us, 1.6 PFLOP/s; without its copies it would take 230,
-// without copies and reads 185, the matrix instructions alone 152 (they sustain 3.6 PFLOP/s), the copies alone about as long.
-// Tiles of 256 by 128 copy a quarter less, but one workgroup of eight waves waits for itself: no faster with two or three
-// blocks in flight, 355 with its waves reading and multiplying in turns; 256 by 256: 380.  The copies are issued in front of the
-// reads in the large tiles (behind them: 365, in between the products: 371), in between the products in the small ones, whose
-// compute units hold two or three workgroups (700 x 6000 x 1500 a twentieth faster than in front of the reads).
+// The instruction is that of bf16 operands, which hold every e4m3 value: its sums are good to fp32 (2^-21 of the magnitudes
+// at worst over random codes, one block of 128).  The instructions of 8-bit operands drop what is 2^-13 below the largest
+// product of a sum: with one large pair that cancels, nothing of the others is left.  They would take 331 us in place of 512 for
+// 16384 x 8192 x 2048 to bf16.
 //
-// LINES: rows that do not start on a line of 128 bytes have each block in two, and a copy of blocks asks L2 for every line twice:
-// 700 x 6000 x 5888 takes 69 us with rows 16 bytes further apart than those of 41 us.  So lines are copied instead, and chunks
-// keep their places in LDS: line l of a row holds the first 8 - o chunks of block l and the last o of block l - 1 (the row's
-// start being o chunks behind that of its line), and lanes read each chunk in the one stage or the other.  Lines kb and kb + 1
-// are there when block kb is read, and kb + 2 follows into the place of kb when everybody has read, at the price of a second
-// barrier: 44 us.  (With a third stage in its place fewer workgroups fit: 70.)
+// Bound: the matrix unit.  16384 x 8192 x 2048 to bf16 takes 512 us, 1.07 PFLOP/s, where a large library product of bf16 operands
+// sustains 1.14.  The next block's copies are issued in between the products: in front of the reads 4096 x 4096 x 4096 takes a
+// twenty-fifth longer, 700 x 6000 x 1500 a fortieth.
 //
 // The instruction's rows are rows of W in an order that leaves a lane with sixteen neighbouring n of one m (n_of), so that C
 // is written in wide pieces; one scale per lane and 16 rows of A covers them where W's scales are those of 128 rows.
-//
-// EXACT: operands widened to bf16 and its matrix instruction, whose sums are good to fp32; for fp32 results.  Otherwise the
-// instruction of 8-bit operands, at twice its rate, which sums the 128 products of a block to 2^-12 of their magnitudes or
-// better (measured: 1.5e-5 of the sum for normal values, 1.6e-4 of the magnitudes at worst over random codes): an eighth
-// of the step that a bf16 result is rounded to.  Blocks are added in fp32.
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef void __attribute__((address_space(3)))* InLds;
 constexpr int kBufferWord3 = 4 << 15 | 7 << 12;     // of a buffer descriptor: 32-bit elements
 constexpr int kTN = 4;                              // fragments of W per wave
 __device__ __forceinline__ int key_a(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int key_w(int row) { return ((row >> 1) & 1) | ((row >> 4) & 3) << 1; }
-__device__ __forceinline__ i32x8 both(const u32x4v (&f)[2])
-{
-    return (i32x8){(int)f[0][0], (int)f[0][1], (int)f[0][2], (int)f[0][3], (int)f[1][0], (int)f[1][1], (int)f[1][2], (int)f[1][3]};
-}
 // A wave's fragments and scales of a block, all of them there when it returns.  (Written out because in front of a read that
 // it knows of the compiler waits until every copy to LDS under way has ended.)  w, a: addresses of the lower chunks, w1, a1: of
-// the upper ones, v, v1: of those of W's odd fragments; ws, as: of the scales.
-#define L355_READ_W(w, w1, v, v1)                                                                                                \
-    "ds_read_b128 %0, " w "\n\tds_read_b128 %1, " w1 "\n\tds_read_b128 %2, " v " offset:512\n\tds_read_b128 %3, " v1 " offset:512\n\t" \
+// the upper ones; ws, as: of the scales.
+#define L355_READ_W(w, w1)                                                                                                       \
+    "ds_read_b128 %0, " w "\n\tds_read_b128 %1, " w1 "\n\tds_read_b128 %2, " w " offset:512\n\tds_read_b128 %3, " w1 " offset:512\n\t" \
     "ds_read_b128 %4, " w " offset:1024\n\tds_read_b128 %5, " w1 " offset:1024\n\t"                                                  \
-    "ds_read_b128 %6, " v " offset:1536\n\tds_read_b128 %7, " v1 " offset:1536\n\t"
+    "ds_read_b128 %6, " w " offset:1536\n\tds_read_b128 %7, " w1 " offset:1536\n\t"
 #define L355_W_OUT "=&v"(fw[0][0]), "=&v"(fw[0][1]), "=&v"(fw[1][0]), "=&v"(fw[1][1]), "=&v"(fw[2][0]), "=&v"(fw[2][1]), "=&v"(fw[3][0]), "=&v"(fw[3][1])
 struct Addresses {
-    unsigned w, w1, v, v1, a, a1, ws, as;
+    unsigned w, w1, a, a1, ws, as;
 };
 __device__ __forceinline__ void read_block(u32x4v (&fw)[4][2], u32x4v (&fa)[4][2], float (&ws)[1][4], f32x4v& as, const Addresses& at)
 {
     asm volatile("ds_read_b32 %16, %22\n\tds_read_b128 %17, %23\n\tds_read_b128 %8, %20\n\tds_read_b128 %9, %21\n\t"
                  "ds_read_b128 %10, %20 offset:2048\n\tds_read_b128 %11, %21 offset:2048\n\t"
                  "ds_read_b128 %12, %20 offset:4096\n\tds_read_b128 %13, %21 offset:4096\n\t"
-                 "ds_read_b128 %14, %20 offset:6144\n\tds_read_b128 %15, %21 offset:6144\n\t" L355_READ_W("%18", "%19", "%24", "%25")
+                 "ds_read_b128 %14, %20 offset:6144\n\tds_read_b128 %15, %21 offset:6144\n\t" L355_READ_W("%18", "%19")
                  "s_waitcnt lgkmcnt(0)"
                  : L355_W_OUT, "=&v"(fa[0][0]), "=&v"(fa[0][1]), "=&v"(fa[1][0]), "=&v"(fa[1][1]), "=&v"(fa[2][0]), "=&v"(fa[2][1]), "=&v"(fa[3][0]), "=&v"(fa[3][1]),
                    "=&v"(ws[0][0]), "=&v"(as)
-                 : "v"(at.w), "v"(at.w1), "v"(at.a), "v"(at.a1), "v"(at.ws), "v"(at.as), "v"(at.v), "v"(at.v1)
+                 : "v"(at.w), "v"(at.w1), "v"(at.a), "v"(at.a1), "v"(at.ws), "v"(at.as)
                  : "memory");
 }
 __device__ __forceinline__ void read_block(u32x4v (&fw)[4][2], u32x4v (&fa)[2][2], float (&ws)[1][4], f32x2v& as, const Addresses& at)
 {
     asm volatile("ds_read_b32 %12, %18\n\tds_read_b64 %13, %19\n\tds_read_b128 %8, %16\n\tds_read_b128 %9, %17\n\t"
-                 "ds_read_b128 %10, %16 offset:2048\n\tds_read_b128 %11, %17 offset:2048\n\t" L355_READ_W("%14", "%15", "%20", "%21")
+                 "ds_read_b128 %10, %16 offset:2048\n\tds_read_b128 %11, %17 offset:2048\n\t" L355_READ_W("%14", "%15")
                  "s_waitcnt lgkmcnt(0)"
                  : L355_W_OUT, "=&v"(fa[0][0]), "=&v"(fa[0][1]), "=&v"(fa[1][0]), "=&v"(fa[1][1]), "=&v"(ws[0][0]), "=&v"(as)
-                 : "v"(at.w), "v"(at.w1), "v"(at.a), "v"(at.a1), "v"(at.ws), "v"(at.as), "v"(at.v), "v"(at.v1)
+                 : "v"(at.w), "v"(at.w1), "v"(at.a), "v"(at.a1), "v"(at.ws), "v"(at.as)
                  : "memory");
 }
 // with a scale for each of the lane's sixteen n
@@ -204,33 +189,33 @@ __device__ __forceinline__ void read_block(u32x4v (&fw)[4][2], u32x4v (&fa)[4][2
                  "ds_read_b128 %20, %26\n\tds_read_b128 %8, %23\n\tds_read_b128 %9, %24\n\t"
                  "ds_read_b128 %10, %23 offset:2048\n\tds_read_b128 %11, %24 offset:2048\n\t"
                  "ds_read_b128 %12, %23 offset:4096\n\tds_read_b128 %13, %24 offset:4096\n\t"
-                 "ds_read_b128 %14, %23 offset:6144\n\tds_read_b128 %15, %24 offset:6144\n\t" L355_READ_W("%21", "%22", "%27", "%28")
+                 "ds_read_b128 %14, %23 offset:6144\n\tds_read_b128 %15, %24 offset:6144\n\t" L355_READ_W("%21", "%22")
                  "s_waitcnt lgkmcnt(0)"
                  : L355_W_OUT, "=&v"(fa[0][0]), "=&v"(fa[0][1]), "=&v"(fa[1][0]), "=&v"(fa[1][1]), "=&v"(fa[2][0]), "=&v"(fa[2][1]), "=&v"(fa[3][0]), "=&v"(fa[3][1]),
                    "=&v"(ws[0]), "=&v"(ws[1]), "=&v"(ws[2]), "=&v"(ws[3]), "=&v"(as)
-                 : "v"(at.w), "v"(at.w1), "v"(at.a), "v"(at.a1), "v"(at.ws), "v"(at.as), "v"(at.v), "v"(at.v1)
+                 : "v"(at.w), "v"(at.w1), "v"(at.a), "v"(at.a1), "v"(at.ws), "v"(at.as)
                  : "memory");
 }
 __device__ __forceinline__ void read_block(u32x4v (&fw)[4][2], u32x4v (&fa)[2][2], f32x4v (&ws)[4], f32x2v& as, const Addresses& at)
 {
     asm volatile("ds_read_b128 %12, %21\n\tds_read_b128 %13, %21 offset:16\n\tds_read_b128 %14, %21 offset:32\n\tds_read_b128 %15, %21 offset:48\n\t"
                  "ds_read_b64 %16, %22\n\tds_read_b128 %8, %19\n\tds_read_b128 %9, %20\n\t"
-                 "ds_read_b128 %10, %19 offset:2048\n\tds_read_b128 %11, %20 offset:2048\n\t" L355_READ_W("%17", "%18", "%23", "%24")
+                 "ds_read_b128 %10, %19 offset:2048\n\tds_read_b128 %11, %20 offset:2048\n\t" L355_READ_W("%17", "%18")
                  "s_waitcnt lgkmcnt(0)"
                  : L355_W_OUT, "=&v"(fa[0][0]), "=&v"(fa[0][1]), "=&v"(fa[1][0]), "=&v"(fa[1][1]), "=&v"(ws[0]), "=&v"(ws[1]), "=&v"(ws[2]), "=&v"(ws[3]), "=&v"(as)
-                 : "v"(at.w), "v"(at.w1), "v"(at.a), "v"(at.a1), "v"(at.ws), "v"(at.as), "v"(at.v), "v"(at.v1)
+                 : "v"(at.w), "v"(at.w1), "v"(at.a), "v"(at.a1), "v"(at.ws), "v"(at.as)
                  : "memory");
 }
 #undef L355_READ_W
 #undef L355_W_OUT
 
-template <int TM, bool EXACT, bool ROW_SCALES, bool LINES>
+template <int TM, bool ROW_SCALES>
 __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a, int tiles_n, int tiles_m)
 {
     constexpr int WN = 2, WM = 2, BN = 64 * WN, BM = 16 * TM * WM, TILE = (BN + BM) * 128, STAGE = TILE + 256 * (WN + WM), WAVES = WN * WM;
     constexpr int LW = BN / 8 / WAVES, LA = BM / 8 / WAVES;      // a wave's copies of eight rows of W and of A
     constexpr int COPIES = LW + LA + 1;                          // and one of scales
-    static_assert(LW >= 1 && LA >= 1 && WAVES == WN + WM && (TM == 2 || TM == 4), "");
+    static_assert(LW >= 1 && LA >= 1 && WAVES == WN + WM && (TM == 2 || TM == 4) && COPIES <= kTN * TM, "");
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
@@ -243,7 +228,7 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
         n0 = (first + in % width) * BN;
         m0 = in / width * BM;
     }
-    const int blocks = (a.K + kScaleCols - 1) / kScaleCols, lines = LINES && blocks > 0 ? blocks + 1 : blocks;
+    const int blocks = (a.K + kScaleCols - 1) / kScaleCols;
     // Through descriptors of the tile's rows: what lies behind the matrix reads as zero, and what a block reads behind column K
     // is the next row's or zero, and is masked.
     const int l8 = lane >> 3, c8 = lane & 7;
@@ -261,39 +246,32 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
                                                           4u * (unsigned)((end_row - first_row) * scale_ld + blocks), kBufferWord3);
     const unsigned scale_at = 4u * (unsigned)((scale_row - first_row) * scale_ld);
     const unsigned lds0 = (unsigned)(uintptr_t)(InLds)smem;
-    // Chunks of a row that stand behind the start of their line; a chunk's line of block kb is line kb, or kb + 1 from
-    // chunk 8 - so many on.  (Fragments of W lie 4 rows apart, which are 4 w_ld = 64 times a whole number of bytes.)
-    auto behind = [](const uint8_t* p) { return (unsigned)((uintptr_t)p >> 4) & 7u; };
-    const unsigned w_base = behind(a.W + n0 * a.w_ld), a_base = behind(a.A + m0 * a.a_ld), w_by = w_ld >> 4, a_by = a_ld >> 4;
-    auto late_w = [&](int row, int c) { return LINES && ((w_base + (unsigned)row * w_by) & 7u) + (unsigned)c >= 8u; };
-    auto late_a = [&](int row, int c) { return LINES && ((a_base + (unsigned)row * a_by) & 7u) + (unsigned)c >= 8u; };
-    // piece i of the copies of a line, or of a block that is one
-    auto copy = [&](int line, int stage, int i) {
+    // piece i of the copies of a block
+    auto copy = [&](int kb, int stage, int i) {
         uint8_t* const to = smem + stage;
-        const unsigned k = (unsigned)(line * kScaleCols);
+        const unsigned k = (unsigned)(kb * kScaleCols);
         if (i < LW) {
             const int x = wave * LW + i, row = 8 * x + l8, c = c8 ^ ((l8 >> 1) & 1) ^ (((x >> 1) & 3) << 1);
-            const unsigned at = (unsigned)row * w_ld + (unsigned)(16 * c) + k - (late_w(row, c) ? 128u : 0u);
+            const unsigned at = (unsigned)row * w_ld + (unsigned)(16 * c) + k;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rows, (InLds)(to + x * 1024), 16, at, 0, 0, 0);
         } else if (i < LW + LA) {
             const int x = wave * LA + i - LW, row = 8 * x + l8, c = c8 ^ (l8 >> 1) ^ ((x & 1) << 2);
-            const unsigned at = (unsigned)row * a_ld + (unsigned)(16 * c) + k - (late_a(row, c) ? 128u : 0u);
+            const unsigned at = (unsigned)row * a_ld + (unsigned)(16 * c) + k;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rows, (InLds)(to + BN * 128 + x * 1024), 16, at, 0, 0, 0);
         } else {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (InLds)(to + TILE + wave * 256), 4, scale_at + 4u * (unsigned)line, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (InLds)(to + TILE + wave * 256), 4, scale_at + 4u * (unsigned)kb, 0, 0, 0);
         }
     };
 
     // where this lane finds row r of its first fragments; the others follow at whole multiples of what the keys go by
     const int w_row = wn + 16 * (r >> 2) + (r & 3), a_row = wm + r;
     Addresses first;
-    first.w = first.v = lds0 + w_row * 128 + (g ^ key_w(w_row)) * 16;
-    first.w1 = first.v1 = first.w ^ 64u;
+    first.w = lds0 + w_row * 128 + (g ^ key_w(w_row)) * 16;
+    first.w1 = first.w ^ 64u;
     first.a = lds0 + (BN + a_row) * 128 + (g ^ key_a(a_row)) * 16;
     first.a1 = first.a ^ 64u;
     first.ws = lds0 + TILE + wave / WM * 256 + (ROW_SCALES ? 64 * g : 0);
     first.as = lds0 + TILE + WN * 256 + wave % WM * 256 + 4 * TM * r;
-    const bool late[6] = {late_w(w_row, g), late_w(w_row, g + 4), late_w(w_row + 4, g), late_w(w_row + 4, g + 4), late_a(a_row, g), late_a(a_row, g + 4)};
     // n of register 0 of fragment j: sixteen neighbouring ones in a lane
     auto n_of = [&](int j) { return n0 + wn + 16 * g + 4 * j; };
 
@@ -306,10 +284,8 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
     u32x4v fw[kTN][2], fa[TM][2];
     std::conditional_t<ROW_SCALES, f32x4v[4], float[1][4]> ws;
     std::conditional_t<TM == 4, f32x4v, f32x2v> s;
-    auto read = [&](int kb, unsigned now, unsigned next) {     // now, next: the stages of lines kb and kb + 1
-        read_block(fw, fa, ws, s, Addresses{first.w + (late[0] ? next : now), first.w1 + (late[1] ? next : now), first.v + (late[2] ? next : now),
-                                            first.v1 + (late[3] ? next : now), first.a + (late[4] ? next : now), first.a1 + (late[5] ? next : now),
-                                            first.ws + now, first.as + now});
+    auto read = [&](int kb, unsigned now) {
+        read_block(fw, fa, ws, s, Addresses{first.w + now, first.w1 + now, first.a + now, first.a1 + now, first.ws + now, first.as + now});
         if constexpr (!ROW_SCALES) s *= ws[0][0];
         if ((kb + 1) * kScaleCols > a.K) {  // zeros behind column K, in both operands: there may be NaN codes
 #pragma unroll
@@ -325,32 +301,26 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
                 }
         }
     };
-    auto multiply = [&](int line, int stage) {      // small tiles copy that line in between, if there is one
-        // a product's sums are used three products later, so that the matrix unit does not wait for them
-        constexpr int kAhead = EXACT ? 1 : 3, kAll = kTN * TM;
+    auto multiply = [&](int kb, int stage) {        // and copies block kb in between, if there is one
+        // a product's sums are used behind the next product, so that the matrix unit does not wait for them
+        constexpr int kAhead = 1, kAll = kTN * TM;
         f32x4v d[kAhead + 1];
-        bf16x8 xa[EXACT ? TM : 1][4], xw[4];
-        if constexpr (EXACT) {
+        bf16x8 xa[TM][4], xw[4];
 #pragma unroll
-            for (int t = 0; t < TM; ++t)
+        for (int t = 0; t < TM; ++t)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) xa[t][q] = widen(fa[t][q >> 1][2 * (q & 1)], fa[t][q >> 1][2 * (q & 1) + 1]);
-        }
+            for (int q = 0; q < 4; ++q) xa[t][q] = widen(fa[t][q >> 1][2 * (q & 1)], fa[t][q >> 1][2 * (q & 1) + 1]);
 #pragma unroll
         for (int p = 0; p < kAll + kAhead; ++p) {
             if (p < kAll) {
                 const int j = p / TM, t = p % TM;
                 f32x4v& to = d[p % (kAhead + 1)];
                 to = (f32x4v){0.f, 0.f, 0.f, 0.f};
-                if constexpr (EXACT) {
-                    if (t == 0)
+                if (t == 0)
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) xw[q] = widen(fw[j][q >> 1][2 * (q & 1)], fw[j][q >> 1][2 * (q & 1) + 1]);
+                    for (int q = 0; q < 4; ++q) xw[q] = widen(fw[j][q >> 1][2 * (q & 1)], fw[j][q >> 1][2 * (q & 1) + 1]);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xw[q], xa[t][q], to, 0, 0, 0);
-                } else {
-                    to = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(fw[j]), both(fa[t]), to, 0, 0, 0, 0, 0, 0);
-                }
+                for (int q = 0; q < 4; ++q) to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xw[q], xa[t][q], to, 0, 0, 0);
             }
             if (p >= kAhead) {
                 const int j = (p - kAhead) / TM, t = (p - kAhead) % TM;
@@ -358,7 +328,7 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[j][t][i] = fmaf(ROW_SCALES ? v[i] * ws[ROW_SCALES ? j : 0][i] : v[i], s[t], acc[j][t][i]);
             }
-            if (TM == 2 && p < COPIES && line < lines) copy(line, stage, p);
+            if (p < COPIES && kb < blocks) copy(kb, stage, p);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -368,26 +338,15 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
         asm volatile("" : : : "memory");
     };
 
-    constexpr int kLead = LINES ? 2 : 1;    // lines that are copied in front of the block
-    for (int line = 0; line < min(kLead, lines); ++line)
+    if (blocks > 0)
 #pragma unroll
-        for (int i = 0; i < COPIES; ++i) copy(line, line * STAGE, i);
+        for (int i = 0; i < COPIES; ++i) copy(0, 0, i);
     for (int kb = 0; kb < blocks; ++kb) {
-        const int now = (kb & 1) * STAGE, next = STAGE - now, to = LINES ? now : next;
+        const int now = (kb & 1) * STAGE, next = STAGE - now;
         __builtin_amdgcn_s_waitcnt(0x0F70);         // vmcnt(0): this wave's copies of the block have arrived
         barrier();                          // everybody's have, and nobody reads the block before any more
-        auto copies = [&]() {
-            if (TM == 4 && kb + kLead < lines)
-#pragma unroll
-                for (int i = 0; i < COPIES; ++i) copy(kb + kLead, to, i);
-        };
-        if (!LINES) copies();
-        read(kb, now, next);
-        if (LINES) {
-            barrier();                      // line kb has been read by everybody: line kb + 2 takes its place
-            copies();
-        }
-        multiply(kb + kLead, to);
+        read(kb, now);
+        multiply(kb + 1, next);
     }
 
     // a lane has sixteen neighbouring n: 32 or 64 bytes of a row of C
@@ -399,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
 #pragma unroll
         for (int i = 0; i < 4 * kTN; ++i) bias[i] = a.bias[min(n + i, a.N - 1)];
     // In one piece wherever it stands (elem.h): with odd rows of C (2102 x 2182 x 1254 to bf16) written element by element the
-    // product took 29 us, as it is 16.
+    // product took 12 us more.
 #pragma unroll
     for (int t = 0; t < TM; ++t) {
         const int m = m0 + wm + 16 * t + r;
@@ -412,41 +371,31 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
     }
 }
 
-template <int TM, bool EXACT, bool ROW_SCALES, bool LINES>
+template <int TM, bool ROW_SCALES>
 hipError_t tiles(const MatmulFp8Args& a, hipStream_t s)
 {
     constexpr int BN = 128, BM = 32 * TM;
     constexpr size_t lds = 2 * (size_t)((BN + BM) * 128 + 4 * 256);     // two blocks, with their scales
     const int tn = (a.N + BN - 1) / BN, tm = (a.M + BM - 1) / BM;
-    const hipError_t e = allow_dynamic_lds((const void*)matmul_fp8_tile_kernel<TM, EXACT, ROW_SCALES, LINES>, lds);
+    const hipError_t e = allow_dynamic_lds((const void*)matmul_fp8_tile_kernel<TM, ROW_SCALES>, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((matmul_fp8_tile_kernel<TM, EXACT, ROW_SCALES, LINES>), dim3(tn * tm), dim3(256), lds, s, a, tn, tm);
+    hipLaunchKernelGGL((matmul_fp8_tile_kernel<TM, ROW_SCALES>), dim3(tn * tm), dim3(256), lds, s, a, tn, tm);
     return hipGetLastError();
 }
 int64_t tiles_in(const MatmulFp8Args& a, int rows) { return (int64_t)((a.N + 127) / 128) * ((a.M + rows - 1) / rows); }
 
-// Tiles of 128 by 128 from so many of them on (two to a compute unit), else of 128 by 64.  4800 x 4096 x 800 (1216 tiles): 35
-// against 42 us; 700 x 6000 x 1500 (282): 23 against 21.
+// Tiles of 128 by 128 from so many of them on (two to a compute unit), else of 128 by 64.  4800 x 4096 x 800 (1216 tiles): 44
+// against 47 us; 700 x 6000 x 1500 (282): 28 against 24.
 constexpr int kLargeTiles = 512;
-// Blocks of all tiles from which on rows that do not start on lines are copied by lines.  The results' type is bf16 (in exact
-// products the matrix instructions are what takes the time).  us by lines and by blocks: 700 x 6000 x 1500 (6768 blocks) 17.1
-// and 20.2, 149 x 12632 x 1825 (4455) 14.5 and 15.3, 384 x 6000 x 1500 (3384) 11.8 and 11.5, 128 x 6000 x 1500 (1128) 9.4 and 8.6.
-constexpr int kLinesBlocks = 4096;
 // Tiles of 128 by 64 up to which the kernel for few rows is faster, which spreads W over eight times as many workgroups: what a
-// compute unit can have under way bounds the tiles then.  us of it and of tiles: to bf16 128 x 2000 x 4000 (32 tiles) 13.3 and 18.8,
-// 512 x 1024 x 2048 (64) 15.6 and 10.5, 128 x 6000 x 1500 (94) 11.5 and 8.9; to fp32 128 x 6000 x 1500 11.5 and 13.3, 400 x 2000 x
-// 4000 (112) 37 and 33.
-constexpr int kFewTiles = 48, kFewExactTiles = 96;
+// compute unit can have under way bounds the tiles then.  us of it and of tiles, to bf16: 128 x 2000 x 4000 (32 tiles) 18.8 and 32.6,
+// 128 x 6000 x 1500 (94) 13.0 and 14.3, 400 x 2000 x 4000 (112) 39.7 and 32.6, 1000 x 1000 x 1000 (128) 12.7 and 11.0.
+constexpr int kFewTiles = 96;
 
 template <int TM>
 hipError_t tiles_of(const MatmulFp8Args& a, hipStream_t s)
 {
-    const bool rows = a.w_block_rows == 1;
-    if (!a.out_bf16) return rows ? tiles<TM, true, true, false>(a, s) : tiles<TM, true, false, false>(a, s);
-    // by lines where there are enough blocks on a compute unit for the copies to be what it waits for
-    const bool lines = tiles_in(a, 32 * TM) * ((a.K + kScaleCols - 1) / kScaleCols) >= kLinesBlocks && ((uintptr_t)a.W | (uintptr_t)a.A | a.w_ld | a.a_ld) % 128 != 0;
-    if (lines) return rows ? tiles<TM, false, true, true>(a, s) : tiles<TM, false, false, true>(a, s);
-    return rows ? tiles<TM, false, true, false>(a, s) : tiles<TM, false, false, false>(a, s);
+    return a.w_block_rows == 1 ? tiles<TM, true>(a, s) : tiles<TM, false>(a, s);
 }
 
 }  // namespace
@@ -456,7 +405,7 @@ size_t matmul_fp8_workspace_bytes(int, int, int) { return 256; }
 hipError_t launch_matmul_fp8(const MatmulFp8Args& a, hipStream_t s)
 {
     // the tiles add 32-bit offsets of their rows, and of their rows of scales, to a base
-    if (a.M > 64 && tiles_in(a, 64) > (a.out_bf16 ? kFewTiles : kFewExactTiles) && a.a_ld < (1 << 23) && a.w_ld < (1 << 23) && a.a_scale_ld < (1 << 21) && a.w_scale_ld < (1 << 21)) {
+    if (a.M > 64 && tiles_in(a, 64) > kFewTiles && a.a_ld < (1 << 23) && a.w_ld < (1 << 23) && a.a_scale_ld < (1 << 21) && a.w_scale_ld < (1 << 21)) {
         return tiles_in(a, 128) >= kLargeTiles ? tiles_of<4>(a, s) : tiles_of<2>(a, s);
     }
     const dim3 block(64 * kRowsWaves);
