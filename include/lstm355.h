@@ -529,10 +529,12 @@ int lstm_quantize_fp8(int M, int N, int dtype, int block_rows, const void* x, in
  *
  *   A [M, K], W [N, K] uint8 (e4m3): 16-byte aligned, a_ld and w_ld multiples of 16 and at least K.  A row is read up to the
  *     next multiple of 16 columns; what stands behind column K does not enter.
- *   a_scale [M, ceil(K / 128)], w_scale [ceil(N / w_block_rows), ceil(K / 128)] fp32; w_block_rows 1 or 128.
+ *   a_scale [M, ceil(K / 128)], w_scale [ceil(N / w_block_rows), ceil(K / 128)] fp32; w_block_rows 1 or 128.  Scales as
+ *     lstm_quantize_fp8 leaves them, at most 2^119: whatever their product, a result that fp32 holds is not lost to them.
  *   bias [N] fp32 or NULL.  C [M, N] of out_dtype.  workspace: at least lstm_matmul_fp8_workspace_bytes(M, N, K).
  * Both gradients are the same call: dA = dC . W with dC quantized along N and W transposed; dW = dC^T . A with both
- * transposed and quantized along M (w_block_rows = 1).  K = 0 gives the bias.  The same call gives the same bits.
+ * transposed and quantized along M (w_block_rows = 1).  K = 0 gives the bias.  Sums are those of fp32 for either type of result
+ * and any number of rows.  The same call gives the same bits.
  */
 size_t lstm_matmul_fp8_workspace_bytes(int M, int N, int K);
 int lstm_matmul_fp8(int M, int N, int K, const uint8_t* A, int64_t a_ld, const float* a_scale, int64_t a_scale_ld,

@@ -6,6 +6,7 @@
 #include "lm_ops.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 namespace l355 {
@@ -30,15 +31,31 @@ __device__ __forceinline__ u32x4v load16(const uint8_t* row, int k, int K)
     }
     return v;
 }
-// eight e4m3 values as bf16, which holds them all
-__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi)
+// eight e4m3 values times a power of two (up to 2^60 either way) as bf16, which holds them all
+__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi, float power = 1.f)
 {
-    const u32x4v w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true))};
+    const u32x4v w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, true)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true))};
     return __builtin_bit_cast(bf16x8, w);
 }
+
+// A block's sum is multiplied by two scales, each of which may be anything from 2^-126 to 2^119: their product may leave the
+// range of fp32, and so may the sum times either, where the result does not.  So the power of two of a row's scale of A, up to 2^60
+// of it, comes first - in the tiles with its values, as they are widened - and the sum is multiplied by W's scale and what is left
+// after that: nothing on the way is out of range then unless the result is.  (16384 x 8192 x 2048 511 us with one product of
+// the scales instead, 527 so; 128 x 2000 x 4000 18.8 and 19.4.)
+struct RowScale {
+    float power, rest;
+};
+__device__ __forceinline__ RowScale split_scale(float scale)
+{
+    const int e = max(-60, min(60, __builtin_amdgcn_frexp_expf(scale) - 1));
+    return {__builtin_amdgcn_ldexpf(1.f, e), __builtin_amdgcn_ldexpf(scale, -e)};
+}
+// infinities as the largest finite values, NaN as it is
+__device__ __forceinline__ float within(float v) { return fabsf(v) == __builtin_inff() ? copysignf(FLT_MAX, v) : v; }
 
 // COUNT neighbouring results of a row, those of them that it has
 template <class E, int COUNT>
@@ -102,9 +119,9 @@ __global__ __launch_bounds__(64 * kRowsWaves) void matmul_fp8_rows_kernel(Matmul
             d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[1], widen(x0[2], x0[3]), d, 0, 0, 0);
             d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[2], widen(x1[0], x1[1]), d, 0, 0, 0);
             d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[3], widen(x1[2], x1[3]), d, 0, 0, 0);
-            const float as = a_scale[t][kb];
+            const RowScale as = split_scale(a_scale[t][kb]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(d[i] * ws[i], as, acc[t][i]);
+            for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(d[i] * as.power * ws[i], as.rest, acc[t][i]);
         }
     }
 #pragma unroll
@@ -136,10 +153,10 @@ __global__ __launch_bounds__(64 * kRowsWaves) void matmul_fp8_rows_kernel(Matmul
 //
 // The instruction is that of bf16 operands, which hold every e4m3 value: its sums are good to fp32 (2^-21 of the magnitudes
 // at worst over random codes, one block of 128).  The instructions of 8-bit operands drop what is 2^-13 below the largest
-// product of a sum: with one large pair that cancels, nothing of the others is left.  They would take 331 us in place of 512 for
+// product of a sum: with one large pair that cancels, nothing of the others is left.  They would take 331 us in place of 527 for
 // 16384 x 8192 x 2048 to bf16.
 //
-// Bound: the matrix unit.  16384 x 8192 x 2048 to bf16 takes 512 us, 1.07 PFLOP/s, where a large library product of bf16 operands
+// Bound: the matrix unit.  16384 x 8192 x 2048 to bf16 takes 527 us, 1.04 PFLOP/s, where a large library product of bf16 operands
 // sustains 1.14.  The next block's copies are issued in between the products: in front of the reads 4096 x 4096 x 4096 takes a
 // twenty-fifth longer, 700 x 6000 x 1500 a fortieth.
 //
@@ -284,9 +301,16 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
     u32x4v fw[kTN][2], fa[TM][2];
     std::conditional_t<ROW_SCALES, f32x4v[4], float[1][4]> ws;
     std::conditional_t<TM == 4, f32x4v, f32x2v> s;
+    float power[TM];
     auto read = [&](int kb, unsigned now) {
         read_block(fw, fa, ws, s, Addresses{first.w + now, first.w1 + now, first.a + now, first.a1 + now, first.ws + now, first.as + now});
-        if constexpr (!ROW_SCALES) s *= ws[0][0];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+            const RowScale as = split_scale(s[t]);
+            power[t] = as.power;
+            // one scale of W: the product of the two is beyond fp32 only where the result is, or where the sum is zero
+            s[t] = ROW_SCALES ? as.rest : within(as.rest * ws[0][0]);
+        }
         if ((kb + 1) * kScaleCols > a.K) {  // zeros behind column K, in both operands: there may be NaN codes
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -309,7 +333,7 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
 #pragma unroll
         for (int t = 0; t < TM; ++t)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) xa[t][q] = widen(fa[t][q >> 1][2 * (q & 1)], fa[t][q >> 1][2 * (q & 1) + 1]);
+            for (int q = 0; q < 4; ++q) xa[t][q] = widen(fa[t][q >> 1][2 * (q & 1)], fa[t][q >> 1][2 * (q & 1) + 1], power[t]);
 #pragma unroll
         for (int p = 0; p < kAll + kAhead; ++p) {
             if (p < kAll) {

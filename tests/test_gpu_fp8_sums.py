@@ -68,3 +68,50 @@ def test_codes_of_every_size(M, N, out):
     a_scale, w_scale = (np.exp(rng.uniform(-3, 3, s)).astype(np.float32) for s in ((M, 6), (-(-N // 128), 6)))
     want, size = oracle.matmul(A, a_scale, W, w_scale, 128)
     close(_product(A, a_scale, W, w_scale, 128, out), want, _tolerance(K, out, size, want))
+
+
+SCALES = {
+    # what log2 of A's and of W's scales lies around in each block of 128 columns
+    "opposite": ([100, -100, 60, -60, 118, -125], [-100, 100, -70, 70, -120, 119]),
+    "both small": ([-68] * 6, [-68] * 6),               # the product of two scales is below the normal numbers
+    "one far larger": ([-100, -90, -110, -61, -62, -80], [119, 110, 119, 80, 80, 100]),       # .. a sum times W's above the largest
+    "one far smaller": ([119, 110, 100, 61, 62, 80], [-126, -120, -126, -90, -80, -100]),
+}
+
+
+@pytest.mark.parametrize("M,N", SIZES)
+@pytest.mark.parametrize("out,w_rows", [("f32", 1), ("f32", 128), ("bf16", 1), ("bf16", 128)])
+@pytest.mark.parametrize("scales", list(SCALES))
+def test_scales_far_from_one(M, N, out, w_rows, scales):
+    """Scales of any size that results of ordinary size have."""
+    K = 700
+    rng = np.random.default_rng(M * N + len(scales))
+    A, W = (rng.integers(30, 80, (R, K)).astype(np.uint8) for R in (M, N))
+    if scales != "both small":          # whose results would be subnormal where the signs are mixed
+        A |= (rng.integers(0, 2, (M, K)) << 7).astype(np.uint8)
+    ea, ew = SCALES[scales]
+    near = lambda e, R: np.ldexp(rng.uniform(1, 1.6, (R, 6)), e).astype(np.float32)  # noqa: E731
+    a_scale, w_scale = near(ea, M), near(ew, -(-N // w_rows))
+    want, size = oracle.matmul(A, a_scale, W, w_scale, w_rows)
+    assert 2.0 ** -126 < size.min() and size.max() < 2.0 ** 126
+    close(_product(A, a_scale, W, w_scale, w_rows, out), want, _tolerance(K, out, size, want))
+
+
+@pytest.mark.parametrize("M,N", SIZES)
+@pytest.mark.parametrize("out,w_rows", [("f32", 1), ("f32", 128), ("bf16", 1), ("bf16", 128)])
+def test_large_scales_of_small_values_and_of_zeros(M, N, out, w_rows):
+    """Scales whose product is beyond the largest number, of blocks in which the smallest codes meet once or not at all; a NaN among
+    the scales reaches its row and its columns alone."""
+    K = 200
+    A, W = np.zeros((M, K), np.uint8), np.zeros((N, K), np.uint8)
+    A[:, 5], A[::3, 150], W[::2, 5], W[1::2, 150] = 1, 1, 1, 129
+    a_scale, w_scale = np.full((M, 2), 2.0 ** 70, np.float32), np.full((-(-N // w_rows), 2), 2.0 ** 70, np.float32)
+    want, size = oracle.matmul(A, a_scale, W, w_scale, w_rows)
+    assert set(np.unique(want)) == {-2.0 ** 122, 0.0, 2.0 ** 122}
+    close(_product(A, a_scale, W, w_scale, w_rows, out), want, 0)
+    a_scale[M // 2, 1] = w_scale[-1, 0] = np.nan
+    got = _product(A, a_scale, W, w_scale, w_rows, out)
+    nan = np.zeros((M, N), bool)
+    nan[M // 2], nan[:, (w_scale.shape[0] - 1) * w_rows:] = True, True
+    assert np.array_equal(np.isnan(got), nan)
+    assert np.array_equal(got[~nan], want[~nan])
