@@ -17,12 +17,21 @@ int bad(const char* entry, const char* what)
     std::snprintf(msg, sizeof msg, "%s: %s", entry, what);
     return op_error(LSTM_ERR_ARG, msg);
 }
-int launched(const char* entry, hipError_t e)
+// Every call that reaches the device goes through here: the runtime allocates on the host, and so does the table of kernels
+// with their LDS sizes, and no exception may leave a C entry.
+template <class A>
+int launched(const char* entry, hipError_t (*launch)(const A&, hipStream_t), const A& a, void* stream) noexcept
 {
-    if (e == hipSuccess) return LSTM_OK;
     char msg[256];
-    std::snprintf(msg, sizeof msg, "%s: %s", entry, hipGetErrorString(e));
-    return op_error(e == hipErrorOutOfMemory ? LSTM_ERR_NOMEM : LSTM_ERR_LAUNCH, msg);
+    try {
+        const hipError_t e = launch(a, (hipStream_t)stream);
+        if (e == hipSuccess) return LSTM_OK;
+        std::snprintf(msg, sizeof msg, "%s: %s", entry, hipGetErrorString(e));
+        return op_error(e == hipErrorOutOfMemory ? LSTM_ERR_NOMEM : LSTM_ERR_LAUNCH, msg);
+    } catch (...) {
+        std::snprintf(msg, sizeof msg, "%s: host allocation failed", entry);
+        return op_error(LSTM_ERR_NOMEM, msg);
+    }
 }
 int small(const char* entry, size_t got, size_t need)
 {
@@ -97,7 +106,7 @@ int lstm_scan_forward(int T, int B, int H, int dtype, int reverse, const void* P
     a.T = T; a.B = B; a.H = H; a.bf16 = dtype == LSTM_BF16; a.reverse = reverse;
     a.P = P; a.P_t = P_t; a.P_b = P_b; a.lengths = lengths; a.c0 = c0;
     a.h = h; a.h_t = h_t; a.h_b = h_b; a.cT = cT; a.states = states; a.ws = (float*)workspace;
-    return launched(entry, launch_scan_forward(a, (hipStream_t)stream));
+    return launched(entry, launch_scan_forward, a, stream);
 }
 
 int lstm_scan_backward(int T, int B, int H, int dtype, int reverse, const void* P, int64_t P_t, int64_t P_b,
@@ -117,7 +126,7 @@ int lstm_scan_backward(int T, int B, int H, int dtype, int reverse, const void* 
     a.P = P; a.P_t = P_t; a.P_b = P_b; a.lengths = lengths; a.states = const_cast<float*>(states);
     a.dh = dh; a.dh_t = dh_t; a.dh_b = dh_b; a.dcT = dcT;
     a.dP = dP; a.dP_t = dP_t; a.dP_b = dP_b; a.dc0 = dc0; a.ws = (float*)workspace;
-    return launched(entry, launch_scan_backward(a, (hipStream_t)stream));
+    return launched(entry, launch_scan_backward, a, stream);
 }
 
 int lstm_rmsnorm_forward(int M, int N, int dtype, const void* x, int64_t x_ld, const void* residual, int64_t residual_ld,
@@ -137,7 +146,7 @@ int lstm_rmsnorm_forward(int M, int N, int dtype, const void* x, int64_t x_ld, c
     if (y8 && !eight_bits_ok(y8, y8_ld, N)) return bad(entry, "y8 must be 16-byte aligned, with y8_ld a multiple of 16 and at least N");
     if (y8 && !stride_ok(y8_scale_ld, blocks_of(N))) return bad(entry, "rows of y8_scale overlap");
     const NormArgs a = {M, N, dtype == LSTM_BF16, x, x_ld, residual, residual_ld, weight, eps, sum, sum_ld, y, y_ld, y8, y8_ld, y8_scale, y8_scale_ld, rstd};
-    return launched(entry, launch_rmsnorm_forward(a, (hipStream_t)stream));
+    return launched(entry, launch_rmsnorm_forward, a, stream);
 }
 
 size_t lstm_rmsnorm_workspace_bytes(int M, int N)
@@ -163,7 +172,7 @@ int lstm_rmsnorm_backward(int M, int N, int dtype, const void* sum, int64_t sum_
     if (!aligned(workspace, 16)) return bad(entry, "the workspace is not 16-byte aligned");
     if (M == 0 && !dweight) return LSTM_OK;
     const NormGradArgs a = {M, N, dtype == LSTM_BF16, sum, sum_ld, weight, rstd, dy, dy_ld, dsum, dsum_ld, dx, dx_ld, dweight, (float*)workspace};
-    return launched(entry, launch_rmsnorm_backward(a, (hipStream_t)stream));
+    return launched(entry, launch_rmsnorm_backward, a, stream);
 }
 
 int lstm_quantize_fp8(int M, int N, int dtype, int block_rows, const void* x, int64_t x_ld, uint8_t* q, int64_t q_ld,
@@ -180,7 +189,7 @@ int lstm_quantize_fp8(int M, int N, int dtype, int block_rows, const void* x, in
     if (!eight_bits_ok(q, q_ld, N)) return bad(entry, "q must be 16-byte aligned, with q_ld a multiple of 16 and at least N");
     if (!stride_ok(scale_ld, blocks_of(N))) return bad(entry, "rows of scale overlap");
     const QuantizeArgs a = {M, N, dtype == LSTM_BF16, block_rows, x, x_ld, q, q_ld, scale, scale_ld};
-    return launched(entry, launch_quantize_fp8(a, (hipStream_t)stream));
+    return launched(entry, launch_quantize_fp8, a, stream);
 }
 
 static bool product_fits(int M, int N, int K)
@@ -216,11 +225,7 @@ int lstm_matmul_fp8(int M, int N, int K, const uint8_t* A, int64_t a_ld, const f
     if (!workspace) return bad(entry, kNull);
     if (!aligned(workspace, 16)) return bad(entry, "the workspace is not 16-byte aligned");
     const MatmulFp8Args a = {M, N, K, w_block_rows, out_dtype == LSTM_BF16, A, a_ld, a_scale, a_scale_ld, W, w_ld, w_scale, w_scale_ld, bias, C, c_ld, (float*)workspace};
-    try {
-        return launched(entry, launch_matmul_fp8(a, (hipStream_t)stream));
-    } catch (...) {     // the table of kernels with their LDS sizes allocates
-        return op_error(LSTM_ERR_NOMEM, "lstm_matmul_fp8: host allocation failed");
-    }
+    return launched(entry, launch_matmul_fp8, a, stream);
 }
 
 static bool sample_fits(int M, int V) { return M >= 0 && M < (1 << 22) && V >= 1 && V <= kSampleMaxVocabulary; }
@@ -244,7 +249,7 @@ int lstm_sample(int M, int V, int dtype, const void* logits, int64_t ld, const u
     if (!workspace) return bad(entry, kNull);
     if (!aligned(workspace, 16)) return bad(entry, "the workspace is not 16-byte aligned");
     const SampleArgs a = {M, V, dtype == LSTM_BF16, logits, ld, allowed, allowed_ld, temperature, top_k, top_p, min_p, u, token, prob, kept, workspace};
-    return launched(entry, launch_sample(a, (hipStream_t)stream));
+    return launched(entry, launch_sample, a, stream);
 }
 
 }  // extern "C"
