@@ -456,7 +456,7 @@ int lstm_bench_group_exchange(int slots, int members, int groups, int placed, in
  *   lengths [B] int32 or NULL (all T): steps of each sequence, counted from t = 0 and taken into [0, T].  What P holds behind
  *     a sequence's end is not read into any result; h is 0 there, and the state is that of the last step (c0 for length 0).
  *   c0 [B, H] fp32 or NULL = zeros; cT [B, H] fp32 or NULL, the final state; it may be c0 itself.
- *   h [T, B, H] of dtype, strides h_t and h_b (at least H where there is more than one row).
+ *   h [T, B, H] of dtype, strides h_t and h_b: rows of H values in any order of which no two share one.
  *   states: NULL, or fp32 [ceil(T / LSTM_SCAN_STEPS), B, H], what lstm_scan_backward needs: the state in front of every
  *     LSTM_SCAN_STEPS-th step.
  *   workspace: at least lstm_scan_workspace_bytes(T, B, H) bytes.
@@ -472,7 +472,7 @@ int lstm_scan_forward(int T, int B, int H, int dtype, int reverse, const void* P
  * Its gradient.  T, B, H, dtype, reverse, P, lengths as in the forward that left `states`.
  *   dh [T, B, H] of dtype, strides dh_t, dh_b (>= 0): gradient of h; what it holds behind a sequence's end is not read.
  *   dcT [B, H] fp32 or NULL = zeros: gradient of the final state.
- *   dP [T, B, 4H] of dtype, strides dP_t, dP_b (at least 4H where there is more than one row): gradient of P, 0 behind the
+ *   dP [T, B, 4H] of dtype, strides dP_t, dP_b (rows that share no value, as those of h): gradient of P, 0 behind the
  *     end of a sequence.  dc0 [B, H] fp32 or NULL: gradient of c0; it may be dcT itself.
  */
 int lstm_scan_backward(int T, int B, int H, int dtype, int reverse, const void* P, int64_t P_t, int64_t P_b,

@@ -70,10 +70,29 @@ int check_scan(const char* entry, int T, int B, int H, int dtype, int reverse, c
     if (!aligned(ws, 16)) return bad(entry, "the workspace is not 16-byte aligned");
     return LSTM_OK;
 }
-// rows of `width` elements that must not share any
+// T x B rows of `width` elements, t and b apart, that must not share any
 bool apart(int T, int B, int64_t t, int64_t b, int64_t width)
 {
-    return T == 0 || (stride_ok(t, T > 1 ? width : 0) && stride_ok(b, B > 1 ? width : 0));
+    if (T == 0) return true;
+    if (!stride_ok(t, T > 1 ? width : 0) || !stride_ok(b, B > 1 ? width : 0)) return false;
+    if (T == 1 || B == 1) return true;
+    // i rows along the fewer ones are as far as j along the others and `rest` elements: rows meet where that is within a row of
+    // j or of j + 1 of them.  Where one dimension lies within a step of the other this ends at its first i.
+    const bool steps_fewer = T < B;
+    const int64_t few = steps_fewer ? T : B, many = steps_fewer ? B : T, s_few = steps_fewer ? t : b, s_many = steps_fewer ? b : t;
+    if (s_many >= (few - 1) * (__int128)s_few + width) return true;
+    int64_t j = 0, rest = 0;
+    for (int64_t i = 1; i < few; ++i) {
+        j += s_few / s_many;
+        rest += s_few % s_many;
+        if (rest >= s_many) {
+            rest -= s_many;
+            ++j;
+        }
+        if (j >= many) break;
+        if (rest < width || (j + 1 < many && s_many - rest < width)) return false;
+    }
+    return true;
 }
 // a matrix of `cols` columns: NULL is fine
 bool matrix_ok(const void* p, int64_t ld, int rows, int cols, int dtype)
