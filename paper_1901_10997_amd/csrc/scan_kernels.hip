@@ -74,6 +74,25 @@ __device__ __forceinline__ int at_step(const ScanArgs& a, int len, int s) { retu
 // (A, S) of a segment.  ws: [segments][B][H][2]
 __device__ __forceinline__ float* slot(const ScanArgs& a, const Place& p, int seg, int u) { return a.ws + (((int64_t)seg * a.B + p.b) * a.H + p.unit + u) * 2; }
 
+// A product of forget gates is zero only if one of them is: where it would underflow it stays the smallest number, so that an
+// infinite state in front of it (or gradient behind it) stays infinite, as it does step by step, and does not become 0 * infinity.
+// What a finite one adds through such a product is below 2^-21.
+constexpr float kLeast = 0x1p-149f;
+__device__ __forceinline__ float product_of(float a, float b)
+{
+    const float p = a * b;
+    return p == 0.f && a != 0.f && b != 0.f ? kLeast : p;
+}
+// that of a run, once it has come out as zero
+template <int N, class F>
+__device__ __forceinline__ float product_of_run(int on, F gate)
+{
+    bool zero = false;
+#pragma unroll
+    for (int j = 0; j < N; ++j) zero |= j < on && gate(j) == 0.f;
+    return zero ? 0.f : kLeast;
+}
+
 // State in front of a segment, or gradient behind it: the (A, S) of `n` segments (first, first + step, ..) applied to `v`.
 // Each wave joins a part of them, eight requested at a time (one after the other their loads took longer than the segment);
 // the parts meet in LDS.  Called by the whole workgroup.
@@ -104,7 +123,7 @@ __device__ __forceinline__ void through_segments(const ScanArgs& a, const Place&
 #pragma unroll
             for (int u = 0; u < UPT; ++u) {
                 S[u] = fmaf(w[i][2 * u], S[u], w[i][2 * u + 1]);
-                A[u] *= w[i][2 * u];
+                A[u] = product_of(A[u], w[i][2 * u]);
             }
         }
     }
@@ -192,6 +211,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_forward_kernel(ScanArgs 
         };
         if (on == kRun) gates(std::true_type());
         else gates(std::false_type());
+#pragma unroll
+        for (int u = 0; u < UPT; ++u)
+            if (A[u] == 0.f) A[u] = product_of_run<kRun>(on, [&](int j) { return f[j][u]; });
         request(tile + 1);
 #pragma unroll
         for (int u = 0; u < UPT; ++u) {
@@ -210,7 +232,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_forward_kernel(ScanArgs 
             for (int u = 0; u < UPT; ++u) {
                 if (w == wave) in[u] = carry[u];
                 carry[u] = fmaf(run_a[turn][w][u * 64 + lane], carry[u], run_s[turn][w][u * 64 + lane]);
-                if (SUMMARY) whole[u] *= run_a[turn][w][u * 64 + lane];
+                if (SUMMARY) whole[u] = product_of(whole[u], run_a[turn][w][u * 64 + lane]);
             }
         if (SUMMARY) continue;
         if (a.states && s0 % kScanSteps == 0 && s0 < a.T && p.live)
@@ -324,6 +346,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_backward_kernel(ScanArgs
         };
         if (on == kScanSteps) load_run(std::true_type());
         else if (on > 0) load_run(std::false_type());
+        if (A == 0.f) A = product_of_run<kScanSteps>(on, [&](int j) { return f[j]; });
         run_a[turn][wave][lane] = A;
         run_s[turn][wave][lane] = U;
         __syncthreads();        // one is enough: the other buffer is written next, and everybody has read it in front of this one
@@ -332,7 +355,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_backward_kernel(ScanArgs
         for (int w = kScanWaves - 1; w >= 0; --w) {
             if (w == wave) e = carry[0];
             carry[0] = fmaf(run_a[turn][w][lane], carry[0], run_s[turn][w][lane]);
-            if (SUMMARY) whole *= run_a[turn][w][lane];
+            if (SUMMARY) whole = product_of(whole, run_a[turn][w][lane]);
         }
         if (SUMMARY) continue;
         auto store_run = [&](auto full) {
