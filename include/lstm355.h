@@ -492,7 +492,8 @@ int lstm_scan_backward(int T, int B, int H, int dtype, int reverse, const void* 
  *   y8 uint8 (e4m3, no infinities, largest value 448) and y8_scale fp32 [M, ceil(N / 128)]: both or neither.  y8 is 16-byte
  *     aligned and y8_ld a multiple of 16, as lstm_matmul_fp8 takes it; columns behind N are left as they are.
  *   eps >= 0.
- * A NaN or an infinity in a row makes that row's results NaN or 0 as the formula does; rows do not see each other.
+ * A NaN or an infinity in a row makes that row's results NaN or 0 as the formula does; rows do not see each other.  Finite
+ * rows of any size are normed, also those whose sum of squares is outside fp32 (rstd alone may be, of rows below 2^-127).
  */
 int lstm_rmsnorm_forward(int M, int N, int dtype, const void* x, int64_t x_ld, const void* residual, int64_t residual_ld,
                          const float* weight, float eps, void* sum, int64_t sum_ld, void* y, int64_t y_ld, uint8_t* y8,

@@ -108,6 +108,25 @@ __device__ __forceinline__ float row_sum(float v, float* part)
     return v;
 }
 
+// The largest of the WPR waves of a row, in all of their threads; NaN gives way
+template <int WPR>
+__device__ __forceinline__ float row_max(float v, float* part)
+{
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    if constexpr (WPR > 1) {
+        __syncthreads();            // everybody has read what is there
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < WPR; ++i) v = fmaxf(v, part[i]);
+    }
+    return v;
+}
+
+// Mean squares (with eps) outside these: the sum of squares is beyond fp32, or some of them are below its normal numbers.
+constexpr float kSmallMean = 0x1p-100f, kLargeMean = 0x1p110f;
+
 // WPR waves of a workgroup's four on a row, IT granules per lane: rows of up to 512 WPR IT columns.
 template <class E, int WPR, int IT>
 __global__ __launch_bounds__(kNormThreads) void rmsnorm_forward_kernel(NormArgs a)
@@ -142,8 +161,33 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_forward_kernel(NormArgs 
     for (int k = 0; k < IT; ++k)
 #pragma unroll
         for (int i = 0; i < kGranule; ++i) squares = fmaf(v[k][i], v[k][i], squares);
-    const float rstd = 1.f / sqrtf(row_sum<WPR>(squares, part) / (float)a.N + a.eps);
-    if (a.rstd && col0 == 0) a.rstd[row] = rstd;
+    const float mean = row_sum<WPR>(squares, part) / (float)a.N + a.eps;
+    float rstd = 1.f / sqrtf(mean), power = 1.f;
+    if (!(mean >= kSmallMean && mean <= kLargeMean)) {      // all of the row's threads or none
+        float largest = 0.f;
+#pragma unroll
+        for (int k = 0; k < IT; ++k)
+#pragma unroll
+            for (int i = 0; i < kGranule; ++i) largest = fmaxf(largest, fabsf(v[k][i]));
+        largest = fmaxf(row_max<WPR>(largest, part), sqrtf(a.eps));
+        if (largest > 0.f && largest <= FLT_MAX) {          // else a row of zeros without eps, or with an infinity: as it came out
+            // by the power of two that brings the larger of the row and sqrt(eps) to about one
+            const int e = max(-126, min(126, 1 - __builtin_amdgcn_frexp_expf(largest)));
+            power = __builtin_amdgcn_ldexpf(1.f, e);
+            const float root = sqrtf(a.eps) * power;
+            squares = 0.f;
+#pragma unroll
+            for (int k = 0; k < IT; ++k)
+#pragma unroll
+                for (int i = 0; i < kGranule; ++i) {
+                    v[k][i] *= power;
+                    squares = fmaf(v[k][i], v[k][i], squares);
+                }
+            if constexpr (WPR > 1) __syncthreads();
+            rstd = 1.f / sqrtf(row_sum<WPR>(squares, part) / (float)a.N + root * root);
+        }
+    }
+    if (a.rstd && col0 == 0) a.rstd[row] = rstd * power;
 #pragma unroll
     for (int k = 0; k < IT; ++k) {
         const int col = col0 + k * WPR * 512;
