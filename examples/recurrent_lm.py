@@ -66,9 +66,9 @@ def quantize(x, block_rows=1, out=None):
     return q
 
 
-def product(a, w, out, bias=None):
+def product(a, w, out, bias=None, ws=None):
     """out [a.rows, w.rows] = a w^T + bias"""
-    ws = _workspace(B.lstm_matmul_fp8_workspace_bytes(a.rows, w.rows, a.cols))
+    ws = _workspace(B.lstm_matmul_fp8_workspace_bytes(a.rows, w.rows, a.cols)) if ws is None else ws
     B.lstm_matmul_fp8(a.rows, w.rows, a.cols, a.codes.data_ptr(), a.codes.stride(0), a.scale.data_ptr(), a.scale.stride(0),
                       w.codes.data_ptr(), w.codes.stride(0), w.scale.data_ptr(), w.scale.stride(0), w.block_rows, _ptr(bias), TYPE[out.dtype],
                       out.data_ptr(), out.stride(0), ws.data_ptr(), ws.numel(), _stream())
@@ -79,6 +79,8 @@ _held = {}      # one workspace for each stream, as large as any call on it has 
 
 
 def _workspace(nbytes):
+    """For calls that run now.  What is recorded needs one of its own: this one may be given back for a larger one, and a
+    graph may be replayed on another stream."""
     ws = _held.get(_stream())
     if ws is None or ws.numel() < nbytes:
         ws = _held[_stream()] = torch.empty(max(nbytes, 1 << 20), dtype=torch.uint8, device="cuda")
@@ -100,9 +102,9 @@ def norm_gradient(sums, weight, rstd, dy, dsum):
     return dx, dw
 
 
-def scan(P, lengths, c0, h, cT, states=None):
+def scan(P, lengths, c0, h, cT, states=None, ws=None):
     T, batch, H = h.shape
-    ws = _workspace(B.lstm_scan_workspace_bytes(T, batch, H))
+    ws = _workspace(B.lstm_scan_workspace_bytes(T, batch, H)) if ws is None else ws
     B.lstm_scan_forward(T, batch, H, TYPE[P.dtype], False, P.data_ptr(), P.stride(0), P.stride(1), _ptr(lengths), _ptr(c0), h.data_ptr(),
                         h.stride(0), h.stride(1), _ptr(cT), _ptr(states), ws.data_ptr(), ws.numel(), _stream())
 
@@ -216,6 +218,9 @@ class Writer:
         self.y8, self.h8 = Eight(batch, H), Eight(batch, H)
         self.logits = torch.empty((batch, model.words), device="cuda")
         self.prob, self.kept = torch.empty(batch, device="cuda"), torch.empty(batch, dtype=torch.int32, device="cuda")
+        need = [B.lstm_scan_workspace_bytes(1, batch, H), B.lstm_sample_workspace_bytes(batch, model.words)]
+        need += [B.lstm_matmul_fp8_workspace_bytes(batch, n, H) for n in (4 * H, H, model.words)]
+        self.ws = torch.empty(max(need), dtype=torch.uint8, device="cuda")      # as long as the graph that holds its address
         self.graph = None
 
     def step(self):
@@ -225,15 +230,15 @@ class Writer:
         for k in range(m.blocks):
             sums = self.sums[k % 2]
             norm(x, residual, p[f"norm{k}"], self.y8, sums)
-            product(self.y8, m.eight[f"in{k}"], self.P.view(batch, 4 * H), p[f"bias{k}"])
-            scan(self.P, None, self.state[k], self.h, self.state[k])       # one step may write its state in place
+            product(self.y8, m.eight[f"in{k}"], self.P.view(batch, 4 * H), p[f"bias{k}"], ws=self.ws)
+            scan(self.P, None, self.state[k], self.h, self.state[k], ws=self.ws)        # one step may write its state in place
             quantize(self.h.view(batch, H), out=self.h8)
-            x, residual = sums, product(self.h8, m.eight[f"out{k}"], self.r)
+            x, residual = sums, product(self.h8, m.eight[f"out{k}"], self.r, ws=self.ws)
         norm(x, residual, p["norm"], self.y8)
-        product(self.y8, m.eight["vocabulary"], self.logits)
-        ws = _workspace(B.lstm_sample_workspace_bytes(batch, m.words))
+        product(self.y8, m.eight["vocabulary"], self.logits, ws=self.ws)
         B.lstm_sample(batch, m.words, B.LSTM_F32, self.logits.data_ptr(), m.words, None, 0, *(s.data_ptr() for s in self.settings),
-                      self.u.data_ptr(), self.token.data_ptr(), self.prob.data_ptr(), self.kept.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+                      self.u.data_ptr(), self.token.data_ptr(), self.prob.data_ptr(), self.kept.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
+                      _stream())
 
     def record(self):
         """Records a step.  Two are run in front of it, on the stream that records and on copies of what they change."""
