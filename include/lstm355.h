@@ -557,8 +557,9 @@ int lstm_matmul_fp8(int M, int N, int K, const uint8_t* A, int64_t a_ld, const f
  *     times their sum.
  *   token [M] int32, -1 for a row without tokens; prob [M] fp32 or NULL: w of the token over the sum, 0 for such a row;
  *   kept [M] int32 or NULL: how many tokens stayed.  workspace: at least lstm_sample_workspace_bytes(M, V).
- * Weights are evaluated in fp64 and summed as whole multiples of 2^-S, S = 62 - ceil(log2 V): what is drawn does not depend
- * on how the work is cut.
+ * Weights are evaluated in fp64 and summed as whole multiples of 2^-S, S = min(51, 62 - ceil(log2 V)): what is drawn does not
+ * depend on how the work is cut.  A weight below 2^-(S + 1) is 0: any min_p above 0 drops such a token, and `kept` counts it
+ * where min_p is 0.  A NaN in top_p keeps all, in min_p those of weight 1, in u is 0.
  */
 size_t lstm_sample_workspace_bytes(int M, int V);
 int lstm_sample(int M, int V, int dtype, const void* logits, int64_t ld, const uint8_t* allowed, int64_t allowed_ld,
