@@ -440,7 +440,8 @@ int lstm_bench_group_exchange(int slots, int members, int groups, int placed, in
  * handle.  All data pointers are DEVICE and the caller's, `dtype` and `out_dtype` are LSTM_F32 or LSTM_BF16 (raw 16-bit
  * patterns), lengths `*_ld` and strides are in elements.  Every call is asynchronous on `stream`, allocates nothing, keeps
  * nothing and may be recorded into a graph; two calls may run at the same time if their outputs and workspaces are different
- * ones.  A workspace is 16-byte aligned and need not be initialised.  Errors: LSTM_ERR_ARG (NULL where required, a size, type,
+ * ones.  A workspace is 16-byte aligned and need not be initialised; every call that has the argument checks it, also
+ * lstm_matmul_fp8 and lstm_sample, which ask for 256 bytes and touch none of them.  Errors: LSTM_ERR_ARG (NULL where required, a size, type,
  * stride or alignment outside what is named), LSTM_ERR_NOMEM (workspace too small), LSTM_ERR_LAUNCH; the text is what
  * lstm_last_error(NULL) returns.  Nothing is launched by a call that returns an error of an argument.
  */

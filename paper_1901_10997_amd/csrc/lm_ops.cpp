@@ -52,6 +52,9 @@ bool floats(std::initializer_list<const void*> all)
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
 bool stride_ok(int64_t s, int64_t least) { return s >= least && s <= kMaxStride; }
 
+// The least that a workspace has to hold.  The product and the draw ask for no more, and touch none of it.
+constexpr size_t kLeastWorkspace = 256;
+
 const char kType[] = "unknown dtype", kSize[] = "a size is negative or too large", kNull[] = "a required pointer is NULL";
 const char kAlign[] = "a pointer is not aligned to its element type";
 
@@ -170,7 +173,7 @@ int lstm_rmsnorm_forward(int M, int N, int dtype, const void* x, int64_t x_ld, c
 
 size_t lstm_rmsnorm_workspace_bytes(int M, int N)
 {
-    return M < 0 || M >= (1 << 24) || N < 1 || N > kNormMaxCols ? 0 : std::max<size_t>(256, rmsnorm_workspace_bytes(M, N));
+    return M < 0 || M >= (1 << 24) || N < 1 || N > kNormMaxCols ? 0 : std::max(kLeastWorkspace, rmsnorm_workspace_bytes(M, N));
 }
 
 int lstm_rmsnorm_backward(int M, int N, int dtype, const void* sum, int64_t sum_ld, const float* weight, const float* rstd,
@@ -220,7 +223,7 @@ static bool product_fits(int M, int N, int K)
 
 size_t lstm_matmul_fp8_workspace_bytes(int M, int N, int K)
 {
-    return product_fits(M, N, K) ? std::max<size_t>(256, matmul_fp8_workspace_bytes(M, N, K)) : 0;
+    return product_fits(M, N, K) ? kLeastWorkspace : 0;
 }
 
 int lstm_matmul_fp8(int M, int N, int K, const uint8_t* A, int64_t a_ld, const float* a_scale, int64_t a_scale_ld,
@@ -243,13 +246,13 @@ int lstm_matmul_fp8(int M, int N, int K, const uint8_t* A, int64_t a_ld, const f
     if (workspace_bytes < need) return small(entry, workspace_bytes, need);
     if (!workspace) return bad(entry, kNull);
     if (!aligned(workspace, 16)) return bad(entry, "the workspace is not 16-byte aligned");
-    const MatmulFp8Args a = {M, N, K, w_block_rows, out_dtype == LSTM_BF16, A, a_ld, a_scale, a_scale_ld, W, w_ld, w_scale, w_scale_ld, bias, C, c_ld, (float*)workspace};
+    const MatmulFp8Args a = {M, N, K, w_block_rows, out_dtype == LSTM_BF16, A, a_ld, a_scale, a_scale_ld, W, w_ld, w_scale, w_scale_ld, bias, C, c_ld};
     return launched(entry, launch_matmul_fp8, a, stream);
 }
 
 static bool sample_fits(int M, int V) { return M >= 0 && M < (1 << 22) && V >= 1 && V <= kSampleMaxVocabulary; }
 
-size_t lstm_sample_workspace_bytes(int M, int V) { return sample_fits(M, V) ? std::max<size_t>(256, sample_workspace_bytes(M, V)) : 0; }
+size_t lstm_sample_workspace_bytes(int M, int V) { return sample_fits(M, V) ? kLeastWorkspace : 0; }
 
 int lstm_sample(int M, int V, int dtype, const void* logits, int64_t ld, const uint8_t* allowed, int64_t allowed_ld,
                 const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
@@ -267,7 +270,7 @@ int lstm_sample(int M, int V, int dtype, const void* logits, int64_t ld, const u
     if (workspace_bytes < need) return small(entry, workspace_bytes, need);
     if (!workspace) return bad(entry, kNull);
     if (!aligned(workspace, 16)) return bad(entry, "the workspace is not 16-byte aligned");
-    const SampleArgs a = {M, V, dtype == LSTM_BF16, logits, ld, allowed, allowed_ld, temperature, top_k, top_p, min_p, u, token, prob, kept, workspace};
+    const SampleArgs a = {M, V, dtype == LSTM_BF16, logits, ld, allowed, allowed_ld, temperature, top_k, top_p, min_p, u, token, prob, kept};
     return launched(entry, launch_sample, a, stream);
 }
 

@@ -102,9 +102,7 @@ struct MatmulFp8Args {
     const float* bias;
     void* C;
     int64_t c_ld;
-    float* ws;
 };
-size_t matmul_fp8_workspace_bytes(int M, int N, int K);
 hipError_t launch_matmul_fp8(const MatmulFp8Args& a, hipStream_t s);
 
 // ---- sampling (sample_kernels.hip)
@@ -123,9 +121,7 @@ struct SampleArgs {
     int* token;
     float* prob;
     int* kept;
-    void* ws;
 };
-size_t sample_workspace_bytes(int M, int V);
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
 
 }  // namespace l355

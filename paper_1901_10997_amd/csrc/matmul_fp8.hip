@@ -424,8 +424,6 @@ hipError_t tiles_of(const MatmulFp8Args& a, hipStream_t s)
 
 }  // namespace
 
-size_t matmul_fp8_workspace_bytes(int, int, int) { return 256; }
-
 hipError_t launch_matmul_fp8(const MatmulFp8Args& a, hipStream_t s)
 {
     // the tiles add 32-bit offsets of their rows, and of their rows of scales, to a base

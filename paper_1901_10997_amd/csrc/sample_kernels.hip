@@ -588,8 +588,6 @@ hipError_t sample(const SampleArgs& a, int bits, hipStream_t s)
 
 }  // namespace
 
-size_t sample_workspace_bytes(int, int) { return 256; }
-
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s)
 {
     int bits = 62;          // V weights of at most 1 stay below 2^62
