@@ -434,37 +434,44 @@ Cut cut_of(int T, int B, int H, int upt, int steps, int whole, int least)
 // 1500 units, fp32, batch 6, 8 and 12 (144, 192, 288 workgroups): forward of 300 steps 27 and 26, 29 and 31, 36 and 45; gradient
 // of 1500 steps at batch 4 (96) 165 and 118 to bf16, 121 and 118 to fp32, at batch 6 136 and 177; with lengths, forward of 300
 // steps at batch 8 28 and 25, at batch 12 32 and 34, gradient at batch 8 37 and 41.  Of few tiles the second launch costs more
-// than it gives (64 steps, batch 1: 5.3 and 6.9), of many the chain grows longer (bf16, 201 units at batch 47, 188 workgroups:
-// 100 steps 10.1 and 10.7, 300 22 and 21, 1500 101 and 77, 6000 396 and 288; at batch 80, 320 workgroups, 1500 steps 112 and 126).
-Cut forward_cut(int T, int B, int H, int upt, bool lengths)
+// than it gives (64 steps, batch 1: 5.3 and 6.9).  Of many the chain grows longer, and that of a bf16 sequence has half as
+// much to read: us without and with the cut at 188 to 192 workgroups (201 units at batch 47, 1500 at 16) 300 steps 22.5 and 21.6,
+// 36.5 and 36.7, 1500 steps 103 and 79, 155 and 131, 4000 steps 266 and 196, 386 and 347; at 208 (1024 at 26) 55.7 and 59.6 for 520
+// steps, 144 and 143, 375 and 383; at 240 (1500 at 20) 61 and 66, 156 and 159, 394 and 425.  fp32 at 188 to 192 (201 at 47, 1500 at 8)
+// 1500 steps 119 and 110, 123 and 118, 4000 steps 292 and 286, 300 and 326; at 208 (1024 at 13) 113 and 122, 278 and 344; at 240 (1500
+// at 10) 128 and 143, 313 and 405.  With lengths, at 240 workgroups (256 at 60, fp32) 300 steps 26.2 and 25.4, 1500 111 and 108.
+Cut forward_cut(int T, int B, int H, int upt, bool lengths, bool bf16)
 {
     constexpr int kTile = kRun * kScanWaves, kManyTiles = 16;
-    return cut_of(T, B, H, upt, kTile, lengths || T > (kManyTiles - 1) * kTile ? 256 : 176, 4);
+    return cut_of(T, B, H, upt, kTile, lengths ? 256 : T <= (kManyTiles - 1) * kTile ? 176 : bf16 ? 208 : 192, 4);
 }
 Cut backward_cut(int T, int B, int H, bool lengths) { return cut_of(T, B, H, 1, kScanSteps * kScanWaves, lengths ? 176 : 128, 3); }
 
 }  // namespace
 
-// the largest of the cuts: one or two units per thread, forward or back, with lengths or without
+// the largest of the cuts: one or two units per thread, forward or back, with lengths or without, of either type
 size_t scan_workspace_bytes(int T, int B, int H)
 {
     int segs = 1;
-    for (const bool lengths : {false, true})
-        segs = std::max({segs, forward_cut(T, B, H, 1, lengths).segs, forward_cut(T, B, H, 2, lengths).segs, backward_cut(T, B, H, lengths).segs});
+    for (const bool lengths : {false, true}) {
+        segs = std::max(segs, backward_cut(T, B, H, lengths).segs);
+        for (const bool bf16 : {false, true})
+            for (const int upt : {1, 2}) segs = std::max(segs, forward_cut(T, B, H, upt, lengths, bf16).segs);
+    }
     return segs < 2 ? 256 : (size_t)segs * B * H * 2 * sizeof(float);
 }
 
 // a grid's threads have to stay under 2^32
 bool scan_fits(int T, int B, int H)
 {
-    const Cut c = forward_cut(T, B, H, 1, true);
+    const Cut c = forward_cut(T, B, H, 1, true, true);
     return (int64_t)c.groups * B * c.segs < (1 << 24);
 }
 
 template <class E, int UPT>
 static void forward(const ScanArgs& a, hipStream_t s)
 {
-    const Cut c = forward_cut(a.T, a.B, a.H, UPT, a.lengths != nullptr);
+    const Cut c = forward_cut(a.T, a.B, a.H, UPT, a.lengths != nullptr, a.bf16);
     const dim3 grid((unsigned)c.groups * a.B * c.segs), block(64 * kScanWaves);
     const dim3 but_last((unsigned)c.groups * a.B * (c.segs - 1));      // nothing follows the last segment
     if (c.segs > 1) hipLaunchKernelGGL((scan_forward_kernel<E, UPT, true>), but_last, block, 0, s, a, c.groups, c.tiles, c.per_seg, c.segs);
