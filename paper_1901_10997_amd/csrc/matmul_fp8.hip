@@ -156,9 +156,11 @@ __global__ __launch_bounds__(64 * kRowsWaves) void matmul_fp8_rows_kernel(Matmul
 // product of a sum: with one large pair that cancels, nothing of the others is left.  They would take 331 us in place of 527 for
 // 16384 x 8192 x 2048 to bf16.
 //
-// Bound: the matrix unit.  16384 x 8192 x 2048 to bf16 takes 527 us, 1.04 PFLOP/s, where a large library product of bf16 operands
-// sustains 1.14.  The next block's copies are issued in between the products: in front of the reads 4096 x 4096 x 4096 takes a
-// twenty-fifth longer, 700 x 6000 x 1500 a fortieth.
+// Bound: what a wave has to issue, and the clock.  16384 x 8192 x 2048 to bf16 takes 527 us, 1.04 PFLOP/s, where a large library
+// product of bf16 operands sustains 1.14 (up to 700 where the card has lowered its clock under launches in a row).  For 64
+// matrix instructions of a block a wave of the large tiles issues 128 conversions and 64 multiplications by scales: the matrix unit is
+// busy for half of the cycles.  The next block's copies are issued in between the products: in front of the reads
+// 4096 x 4096 x 4096 takes a twenty-fifth longer, 700 x 6000 x 1500 a fortieth.
 //
 // The instruction's rows are rows of W in an order that leaves a lane with sixteen neighbouring n of one m (n_of), so that C
 // is written in wide pieces; one scale per lane and 16 rows of A covers them where W's scales are those of 128 rows.

@@ -15,8 +15,9 @@
 // that, in rows of equal or of very far logits, by the digits of the logit's bit pattern).  The token is found in two steps:
 // the wave in whose run the sum is passed, then that run cut over all threads.
 //
-// Bound: the vector units of the row's compute unit, about 25 instructions a weight, and the sixteen barriers between the
-// steps (256 rows of 32 000 bf16 with mixed settings and masks: 35 us; one row of 10 000 with top_k and top_p 16.6).
+// Bound: the row's one compute unit, in steps that wait for each other at sixteen barriers; a batch takes what its slowest rows
+// take.  256 rows of 32 000 bf16: 9.8 us greedy, 19.6 without a filter, 21.7 with top_k 50, 33 with top_p 0.95, 29 with both, 36 to
+// 38 with mixed settings and masks (vector instructions fill 55 % of the busy cycles there); one row of 10 000 with both 17.0.
 #include "common.h"
 #include "elem.h"
 #include "lm_ops.h"
@@ -30,10 +31,9 @@ constexpr int kBins = 2048, kList = 512, kTable = 1024;
 constexpr int kChunk = 256;         // tokens of a wave at a time
 constexpr int kAhead = 2;           // ... and of these so many are requested at once from memory
 constexpr float kInf = __builtin_inff();
-// A row is held where it fits beside Shared, up to 28 672 fp32 and 57 344 bf16 tokens.  us held and read again from the caches
-// (both before each_kept), top_k 50 and top_p 0.95: one row of 10 000 fp32 18.2 and 22.0, 28 000 25.9 and 33.4, 512 rows of 4000 26.7 and 30.9, of 28 000
-// 59 and 82; 2048 rows of 2000 42.0 and 39.7, whose smaller workgroups are fewer on a compute unit then (the mixed settings there
-// 35.3 and 35.7).
+// A row is held where it fits beside Shared, up to 28 672 fp32 and 57 344 bf16 tokens.  us held and read again from the caches,
+// top_k 50 and top_p 0.95: one row of 10 000 fp32 17.0 and 20.8, 28 000 24.2 and 31.5, of 57 344 bf16 37.7 and 51.0, 512 rows of 4000
+// 27.1 and 31.0, of 28 000 55 and 79, 2048 rows of 2000 42.8 and 48.1; with mixed settings 36.0 and 40.3 there.
 constexpr size_t kHeldBytes = 112 << 10;
 // chunks of each of `waves` runs over a row
 __host__ __device__ constexpr int chunks_of(int V, int waves) { return ((V + kChunk - 1) / kChunk + waves - 1) / waves; }
