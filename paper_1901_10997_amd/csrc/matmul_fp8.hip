@@ -45,7 +45,7 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi, float power = 
 // range of fp32, and so may the sum times either, where the result does not.  So the power of two of a row's scale of A, up to 2^60
 // of it, comes first - in the tiles with its values, as they are widened - and the sum is multiplied by W's scale and what is left
 // after that: nothing on the way is out of range then unless the result is.  (16384 x 8192 x 2048 511 us with one product of
-// the scales instead, 527 so; 128 x 2000 x 4000 18.8 and 19.4.)
+// the scales instead, 535 so; 128 x 2000 x 4000 18.8 and 19.4.)
 struct RowScale {
     float power, rest;
 };
@@ -54,8 +54,12 @@ __device__ __forceinline__ RowScale split_scale(float scale)
     const int e = max(-60, min(60, __builtin_amdgcn_frexp_expf(scale) - 1));
     return {__builtin_amdgcn_ldexpf(1.f, e), __builtin_amdgcn_ldexpf(scale, -e)};
 }
-// infinities as the largest finite values, NaN as it is
-__device__ __forceinline__ float within(float v) { return fabsf(v) == __builtin_inff() ? copysignf(FLT_MAX, v) : v; }
+// a b; where two finite numbers give an infinity the largest finite value, so that zero times it is zero
+__device__ __forceinline__ float within(float a, float b)
+{
+    const float p = a * b;
+    return fabsf(p) == __builtin_inff() && fabsf(a) <= FLT_MAX && fabsf(b) <= FLT_MAX ? copysignf(FLT_MAX, p) : p;
+}
 
 // COUNT neighbouring results of a row, those of them that it has
 template <class E, int COUNT>
@@ -153,10 +157,10 @@ __global__ __launch_bounds__(64 * kRowsWaves) void matmul_fp8_rows_kernel(Matmul
 //
 // The instruction is that of bf16 operands, which hold every e4m3 value: its sums are good to fp32 (2^-21 of the magnitudes
 // at worst over random codes, one block of 128).  The instructions of 8-bit operands drop what is 2^-13 below the largest
-// product of a sum: with one large pair that cancels, nothing of the others is left.  They would take 331 us in place of 527 for
+// product of a sum: with one large pair that cancels, nothing of the others is left.  They would take 331 us in place of 535 for
 // 16384 x 8192 x 2048 to bf16.
 //
-// Bound: what a wave has to issue, and the clock.  16384 x 8192 x 2048 to bf16 takes 527 us, 1.04 PFLOP/s, where a large library
+// Bound: what a wave has to issue, and the clock.  16384 x 8192 x 2048 to bf16 takes 535 us, 1.03 PFLOP/s, where a large library
 // product of bf16 operands sustains 1.14 (up to 700 where the card has lowered its clock under launches in a row).  For 64
 // matrix instructions of a block a wave of the large tiles issues 128 conversions and 64 multiplications by scales: the matrix unit is
 // busy for half of the cycles.  The next block's copies are issued in between the products: in front of the reads
@@ -311,7 +315,7 @@ __global__ __launch_bounds__(256, 2) void matmul_fp8_tile_kernel(MatmulFp8Args a
             const RowScale as = split_scale(s[t]);
             power[t] = as.power;
             // one scale of W: the product of the two is beyond fp32 only where the result is, or where the sum is zero
-            s[t] = ROW_SCALES ? as.rest : within(as.rest * ws[0][0]);
+            s[t] = ROW_SCALES ? as.rest : within(as.rest, ws[0][0]);
         }
         if ((kb + 1) * kScaleCols > a.K) {  // zeros behind column K, in both operands: there may be NaN codes
 #pragma unroll

@@ -115,3 +115,23 @@ def test_large_scales_of_small_values_and_of_zeros(M, N, out, w_rows):
     nan[M // 2], nan[:, (w_scale.shape[0] - 1) * w_rows:] = True, True
     assert np.array_equal(np.isnan(got), nan)
     assert np.array_equal(got[~nan], want[~nan])
+
+
+@pytest.mark.parametrize("M,N", SIZES)
+@pytest.mark.parametrize("out,w_rows", [("f32", 1), ("f32", 128), ("bf16", 1), ("bf16", 128)])
+def test_infinite_scales(M, N, out, w_rows):
+    """They make every sum infinite, and a sum of zeros NaN, however small the sum is."""
+    K = 200
+    A, W = np.zeros((M, K), np.uint8), np.ones((N, K), np.uint8)
+    A[:, 5], A[1::2, 5] = 1, 129                            # one product of 2^-18, of either sign, in the first block
+    A[0] = 0
+    a_scale, w_scale = np.full((M, 2), 2.0 ** -20, np.float32), np.full((-(-N // w_rows), 2), 2.0 ** -20, np.float32)
+    a_scale[M // 2, 0] = a_scale[0, 0] = w_scale[-1, 0] = np.inf
+    got = _product(A, a_scale, W, w_scale, w_rows, out)
+    with np.errstate(invalid="ignore"):
+        first = oracle.e4m3_decode(A[:, :128]) @ oracle.e4m3_decode(W[:, :128]).T
+        want = first * a_scale[:, :1].astype(np.float64) * np.repeat(w_scale[:, 0], w_rows)[:N].astype(np.float64)
+    assert np.isinf(want[M // 2]).all() and np.isnan(want[0, -1]) and np.isnan(want).sum() >= N
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    rest = ~np.isnan(want)
+    assert np.array_equal(got[rest], want[rest])
