@@ -161,7 +161,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void matmul_fp8_rows_kernel(Matmul
 // 16384 x 8192 x 2048 to bf16.
 //
 // Bound: what a wave has to issue, and the clock.  16384 x 8192 x 2048 to bf16 takes 535 us, 1.03 PFLOP/s, where a large library
-// product of bf16 operands sustains 1.14 (up to 700 where the card has lowered its clock under launches in a row).  For 64
+// product of bf16 operands sustains 1.14 (up to 690 where the card has lowered its clock under launches in a row).  For 64
 // matrix instructions of a block a wave of the large tiles issues 128 conversions and 64 multiplications by scales: the matrix unit is
 // busy for half of the cycles.  The next block's copies are issued in between the products: in front of the reads
 // 4096 x 4096 x 4096 takes a twenty-fifth longer, 700 x 6000 x 1500 a fortieth.
