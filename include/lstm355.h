@@ -567,6 +567,108 @@ int lstm_sample(int M, int V, int dtype, const void* logits, int64_t ld, const u
                 const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
                 int32_t* token, float* prob, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Gated delta rule: a recurrence whose state is a matrix S [key_dim, value_dim] for each head, in which a key finds a value and
+ * corrects it,
+ *
+ *     S_t = a_t (I - beta_t k_t k_t') S_{t-1} + beta_t k_t v_t'     a_t = exp(log_decay_t)     o_t = scale S_t' q_t
+ *
+ *   q, k [T, B, key_heads * key_dim], v and o [T, B, heads * value_dim] of dtype: row (t, b) at + t*_t + b*_b, the heads of a row side by
+ *     side; input strides are >= 0, rows of o lie apart.  heads is a multiple of key_heads: heads h key_heads / heads .. share a key and a
+ *     query.  key_dim <= 256, value_dim <= 65536.  Keys are used as they are; they are meant to have length 1 (lstm_rmsnorm_forward over rows
+ *     of key_dim columns with weight key_dim^-1/2).
+ *   log_decay fp32 [T, B, heads] or NULL = 0 (the delta rule without gates), meant to be <= 0; what is below -10000, minus infinity too,
+ *     forgets all.  beta fp32 [T, B, heads].
+ *   lengths [B] int32 or NULL (all T): steps of each sequence, taken into [0, T].  What the inputs hold behind a sequence's end is not
+ *     read; o is 0 there, and the state is that of the last step (S0 for length 0).
+ *   S0 [B, heads, key_dim, value_dim] fp32 or NULL = zeros; ST the same, or NULL: the final state; it may be S0 itself.
+ *   states: NULL, or fp32 [ceil(T / LSTM_DELTA_STEPS), B, heads, key_dim, value_dim], what lstm_delta_backward needs: the state in front of
+ *     every LSTM_DELTA_STEPS-th step that a sequence has (the others are left as they are).
+ *   workspace: at least lstm_delta_workspace_bytes(..., backward = 0) bytes.
+ * T = 0 moves S0 to ST; B = 0 does nothing.  State and gates are fp32, o alone is rounded to dtype.  T = 1 is the form for serving: one
+ * launch, S0 = ST in place.  A NaN or an infinity in a step makes what its sequence and head give from the first step of its
+ * LSTM_DELTA_STEPS on not finite, in the columns of v that it reaches; other heads and sequences do not see it.
+ */
+enum { LSTM_DELTA_STEPS = 64 };
+size_t lstm_delta_workspace_bytes(int T, int B, int heads, int key_heads, int key_dim, int value_dim, int backward);
+int lstm_delta_forward(int T, int B, int heads, int key_heads, int key_dim, int value_dim, int dtype, const void* q, int64_t q_t,
+                       int64_t q_b, const void* k, int64_t k_t, int64_t k_b, const void* v, int64_t v_t, int64_t v_b,
+                       const float* log_decay, int64_t log_decay_t, int64_t log_decay_b, const float* beta, int64_t beta_t,
+                       int64_t beta_b, const int32_t* lengths, float scale, const float* S0, void* o, int64_t o_t, int64_t o_b,
+                       float* ST, float* states, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Its gradient.  Everything up to scale as in the forward that left `states`.
+ *   dO: gradient of o, strides >= 0; what it holds behind a sequence's end is not read.  dST or NULL = zeros: gradient of the final state.
+ *   dq, dk, dv, dlog_decay (NULL: not wanted) and dbeta: gradients in the shapes and types of what they belong to, rows apart, 0 behind
+ *     the end of a sequence; those of shared keys and queries are summed over their heads in fp32.  dS0 or NULL; it may be dST itself.
+ *   workspace: at least lstm_delta_workspace_bytes(..., backward = 1) bytes.
+ * Sums are fp32 in one order: the same call gives the same bits.
+ */
+int lstm_delta_backward(int T, int B, int heads, int key_heads, int key_dim, int value_dim, int dtype, const void* q, int64_t q_t,
+                        int64_t q_b, const void* k, int64_t k_t, int64_t k_b, const void* v, int64_t v_t, int64_t v_b,
+                        const float* log_decay, int64_t log_decay_t, int64_t log_decay_b, const float* beta, int64_t beta_t,
+                        int64_t beta_b, const int32_t* lengths, float scale, const float* states, const void* dO, int64_t do_t,
+                        int64_t do_b, const float* dST, void* dq, int64_t dq_t, int64_t dq_b, void* dk, int64_t dk_t, int64_t dk_b,
+                        void* dv, int64_t dv_t, int64_t dv_b, float* dlog_decay, int64_t dlog_decay_t, int64_t dlog_decay_b,
+                        float* dbeta, int64_t dbeta_t, int64_t dbeta_b, float* dS0, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/*
+ * Scores of M rows of logits [M, V] (dtype; V <= 2^20): with log p_j = l_j - log sum_i exp(l_i) over the tokens that exist,
+ *   allowed uint8 [M, V] (allowed_ld = 0: one row for all) or NULL, NaN and minus infinity: as in lstm_sample, tokens that do not exist.
+ *     Tokens whose logit is plus infinity share all mass equally.
+ *   token [M] int32: the given token of each row; outside 0 .. V - 1 (padding) the row has none: logprob 0, rank -1.
+ *   logprob [M] or NULL: log p of the given token, minus infinity where it does not exist.
+ *   rank [M] int32 or NULL: how many tokens stand in front of it, ordered by logit, the largest first, equal ones by index; of one that
+ *     does not exist how many do.
+ *   entropy [M] or NULL: -sum_j p_j log p_j; 0 of a row without tokens.
+ *   top_n (0 .. 64), top_token [M, top_n] int32, top_logprob [M, top_n]: the first tokens of that order and their log p; -1 and minus infinity
+ *     where there are fewer.
+ *   stats fp32 [M, 4] or NULL: what lstm_logprobs_backward needs (largest logit, log of the sum over exp(l - largest), entropy, 1 over the sum).
+ *   workspace: at least lstm_logprobs_workspace_bytes(M, V, top_n) bytes.
+ */
+size_t lstm_logprobs_workspace_bytes(int M, int V, int top_n);
+int lstm_logprobs_forward(int M, int V, int dtype, const void* logits, int64_t ld, const uint8_t* allowed, int64_t allowed_ld,
+                          const int32_t* token, float* logprob, int32_t* rank, float* entropy, float* stats, int top_n,
+                          int32_t* top_token, float* top_logprob, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Its gradient by the logits, rounded to dtype:  dl_j = dlogprob (1 where j is the given token - p_j) - dentropy p_j (log p_j + entropy),
+ * 0 for tokens that do not exist.  Everything up to token as in the forward that left `stats`; dlogprob, dentropy [M] fp32 or NULL = zeros;
+ * token may be NULL where dlogprob is.  A row without a given token takes dentropy alone.  dlogits may be logits itself.  With dlogprob = -1 / M
+ * this is the gradient of the mean cross-entropy.
+ */
+int lstm_logprobs_backward(int M, int V, int dtype, const void* logits, int64_t ld, const uint8_t* allowed, int64_t allowed_ld,
+                           const int32_t* token, const float* stats, const float* dlogprob, const float* dentropy, void* dlogits,
+                           int64_t dlogits_ld, void* stream);
+
+/*
+ * Distillation: how far a student's logits [M, V] (dtype) are from a teacher of whom each row names K words with their logits,
+ *
+ *     s = softmax(l / temperature)     t_j = exp(z_j / temperature - teacher_lse)     t_r = max(0, 1 - sum_j t_j)     s_r = 1 - sum_j s_j
+ *     loss = temperature^2 ( sum over the list of t_j (log t_j - log s_j) + t_r (log t_r - log s_r) )
+ *
+ *   top_token [M, K] int32, top_logit [M, K] fp32 (z): the teacher's words, in any order, K 1 .. 256; row lengths >= 0 (0: one list for
+ *     all).  A word outside 0 .. V - 1 (padding) or one that stands in the list before does not count.  Minus infinity is a share of 0.
+ *   teacher_lse [M] fp32: the log of the teacher's sum of exp(z / temperature) over its whole vocabulary (0 where top_logit are log
+ *     probabilities and temperature is 1); what the list leaves of 1 is one share t_r for all other words together.  NULL: the list is all
+ *     there is, t is softmax(z / temperature) over it and t_r = 0; a row whose list has no words then has loss 0 and no gradient.
+ *   temperature 2^-20 .. 2^20.  loss [M] or NULL.  stats fp32 [M, 4] or NULL: what lstm_distill_backward needs.
+ *   workspace: at least lstm_distill_workspace_bytes(M, V, K) bytes.
+ * A student's logit may be minus infinity (its s_j is 0; the loss is infinite where t_j is not).  A NaN in a row makes its results NaN.
+ */
+size_t lstm_distill_workspace_bytes(int M, int V, int K);
+int lstm_distill_forward(int M, int V, int K, int dtype, const void* logits, int64_t ld, const int32_t* top_token, int64_t top_token_ld,
+                         const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, float temperature, float* loss,
+                         float* stats, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Its gradient by the student's logits, rounded to dtype:  dl_j = dloss temperature (s_j - t_j) in the list, dloss temperature
+ * s_j (1 - t_r / s_r) outside it.  Everything up to temperature as in the forward that left `stats`; dloss [M] fp32.  dlogits may be logits
+ * itself.
+ */
+int lstm_distill_backward(int M, int V, int K, int dtype, const void* logits, int64_t ld, const int32_t* top_token, int64_t top_token_ld,
+                          const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, float temperature,
+                          const float* stats, const float* dloss, void* dlogits, int64_t dlogits_ld, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

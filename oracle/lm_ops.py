@@ -1,5 +1,6 @@
 """The operators around the cells in numpy and 64 bits, from their formulas: gated linear recurrence and its gradient, RMS
-norm and its gradient, e4m3 quantization, the product with block scales, and the draw of a token.  Test infrastructure."""
+norm and its gradient, e4m3 quantization, the product with block scales, the draw of a token, the gated delta rule and its
+gradient, scores of tokens and the distillation loss with their gradients.  Test infrastructure."""
 from __future__ import annotations
 
 import math
@@ -169,3 +170,170 @@ def sample(logits, u, allowed=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0
         if run > want:
             return int(j), float(v / math.fsum(w)), len(order)
     return int(order[-1]), float(w[-1] / math.fsum(w)), len(order)
+
+
+# ---- gated delta rule: S_t = a_t (I - b_t k_t k_t') S_{t-1} + b_t k_t v_t', o_t = scale S_t' q_t
+
+def _delta_rows(x, T, B, heads):
+    return np.asarray(x, np.float64).reshape(T, B, heads, -1)
+
+
+def _delta_inside(T, B, lengths):
+    n = np.full(B, T) if lengths is None else np.clip(np.asarray(lengths), 0, T)
+    return np.arange(T)[:, None] < n[None]
+
+
+def delta_forward(q, k, v, g, beta, heads, key_heads, scale, lengths=None, S0=None):
+    """q, k [T, B, key_heads * Dk], v [T, B, heads * Dv], g (log decay) or None, beta [T, B, heads].  Returns o, the final state and
+    the state in front of every step [T, B, heads, Dk, Dv].  What stands behind a sequence's end is not looked at."""
+    T, B = beta.shape[:2]
+    q, k, v = _delta_rows(q, T, B, key_heads), _delta_rows(k, T, B, key_heads), _delta_rows(v, T, B, heads)
+    q, k = (np.repeat(x, heads // key_heads, axis=2) for x in (q, k))
+    inside = _delta_inside(T, B, lengths)
+    S = np.zeros((B, heads, q.shape[3], v.shape[3])) if S0 is None else np.array(S0, np.float64)
+    o, front = np.zeros((T, B, heads, v.shape[3])), np.zeros((T,) + S.shape)
+    for t in range(T):
+        front[t] = S
+        for b in np.flatnonzero(inside[t]):
+            a = np.ones(heads) if g is None else np.exp(np.asarray(g[t, b], np.float64))
+            S[b] *= a[:, None, None]
+            u = np.asarray(beta[t, b], np.float64)[:, None] * (v[t, b] - np.einsum("hd,hdv->hv", k[t, b], S[b]))
+            S[b] += np.einsum("hd,hv->hdv", k[t, b], u)
+            o[t, b] = scale * np.einsum("hd,hdv->hv", q[t, b], S[b])
+    return o.reshape(T, B, -1), S, front
+
+
+def delta_backward(q, k, v, g, beta, heads, key_heads, scale, front, dO, lengths=None, dST=None, sizes=None):
+    """Gradients dq, dk, dv, dg, dbeta, dS0 from the states delta_forward returned; 0 behind a sequence's end.  sizes: a dict that
+    receives for dg and dbeta, which are inner products, the product of the lengths or the sum of the magnitudes."""
+    T, B = beta.shape[:2]
+    q, k, v, dO = _delta_rows(q, T, B, key_heads), _delta_rows(k, T, B, key_heads), _delta_rows(v, T, B, heads), _delta_rows(dO, T, B, heads)
+    group = heads // key_heads
+    inside = _delta_inside(T, B, lengths)
+    dq, dk, dv, dg, db = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape), np.zeros((T, B, heads)), np.zeros((T, B, heads))
+    D = np.zeros(front.shape[1:]) if dST is None else np.array(dST, np.float64)
+    if sizes is not None:
+        sizes.update(dg=np.zeros(dg.shape), dbeta=np.zeros(db.shape))
+    for t in range(T - 1, -1, -1):
+        for b in np.flatnonzero(inside[t]):
+            K, Q = np.repeat(k[t, b], group, axis=0), np.repeat(q[t, b], group, axis=0)
+            a = np.ones(heads) if g is None else np.exp(np.asarray(g[t, b], np.float64))
+            bt = np.asarray(beta[t, b], np.float64)
+            decayed = a[:, None, None] * front[t, b]
+            miss = v[t, b] - np.einsum("hd,hdv->hv", K, decayed)
+            after = decayed + np.einsum("hd,h,hv->hdv", K, bt, miss)
+            d = D[b] + scale * np.einsum("hd,hv->hdv", Q, dO[t, b])
+            dq[t, b] = (scale * np.einsum("hdv,hv->hd", after, dO[t, b])).reshape(key_heads, group, -1).sum(1)
+            du = np.einsum("hd,hdv->hv", K, d)
+            dk[t, b] = (np.einsum("hdv,h,hv->hd", d, bt, miss) - np.einsum("h,hdv,hv->hd", bt, decayed, du)).reshape(key_heads, group, -1).sum(1)
+            db[t, b] = (du * miss).sum(1)
+            dv[t, b] = bt[:, None] * du
+            ddecayed = d - np.einsum("h,hd,hv->hdv", bt, K, du)
+            dg[t, b] = (ddecayed * decayed).sum((1, 2))
+            if sizes is not None:
+                sizes["dg"][t, b] = abs(ddecayed * decayed).sum((1, 2))
+                sizes["dbeta"][t, b] = np.linalg.norm(du, axis=1) * np.linalg.norm(miss, axis=1)
+            D[b] = a[:, None, None] * ddecayed
+    return dq.reshape(T, B, -1), dk.reshape(T, B, -1), dv.reshape(T, B, -1), dg, db, D
+
+
+# ---- scores of given tokens
+
+def _existing(logits, allowed):
+    l = np.array(logits, np.float64)
+    if allowed is not None:
+        l = np.where(np.broadcast_to(allowed, l.shape) != 0, l, -np.inf)
+    return np.where(np.isnan(l), -np.inf, l)
+
+
+def _log_shares(l):
+    """log p of a row of which some tokens do not exist (minus infinity); infinite ones share all."""
+    top = l.max()
+    if top == -np.inf:
+        return np.full(l.shape, -np.inf)
+    with np.errstate(invalid="ignore"):
+        d = np.where(l == top, 0.0, l - top)
+    return d - np.log(np.exp(d).sum())
+
+
+def logprobs_forward(logits, token=None, allowed=None, top_n=0):
+    """Returns logprob, rank, entropy, top_token [M, top_n], top_logprob [M, top_n]."""
+    l = _existing(logits, allowed)
+    M, V = l.shape
+    logprob, rank, entropy = np.zeros(M), np.full(M, -1), np.zeros(M)
+    top_token, top_logprob = np.full((M, top_n), -1), np.full((M, top_n), -np.inf)
+    for m in range(M):
+        lp = _log_shares(l[m])
+        p = np.exp(lp)
+        entropy[m] = -(p[p > 0] * lp[p > 0]).sum()
+        there = l[m] > -np.inf
+        order = np.argsort(-l[m], kind="stable")[:there.sum()]
+        n = min(top_n, len(order))
+        top_token[m, :n], top_logprob[m, :n] = order[:n], lp[order[:n]]
+        if token is not None and 0 <= token[m] < V:
+            logprob[m] = lp[token[m]]
+            mine, at = l[m, token[m]], np.arange(V)
+            rank[m] = (there & ((l[m] > mine) | ((l[m] == mine) & (at < token[m])))).sum()
+    return logprob, rank, entropy, top_token, top_logprob
+
+
+def logprobs_backward(logits, token=None, allowed=None, dlogprob=None, dentropy=None):
+    l = _existing(logits, allowed)
+    M, V = l.shape
+    out = np.zeros((M, V))
+    for m in range(M):
+        lp = _log_shares(l[m])
+        p = np.exp(lp)
+        if dlogprob is not None and 0 <= token[m] < V:
+            out[m] -= float(dlogprob[m]) * p
+            out[m, token[m]] += float(dlogprob[m])
+        if dentropy is not None:
+            plog = np.where(p > 0, p * np.where(p > 0, lp, 0.0), 0.0)
+            out[m] -= float(dentropy[m]) * (plog - p * plog.sum())
+        out[m, l[m] == -np.inf] = 0.0
+    return out
+
+
+# ---- distillation from a teacher's words
+
+def distill(logits, top_token, top_logit, temperature, teacher_lse=None, dloss=None):
+    """loss [M] and, for dloss, the gradient by the logits."""
+    l = np.array(logits, np.float64)
+    M, V = l.shape
+    heat = float(temperature)
+    loss, grad = np.zeros(M), np.zeros((M, V))
+    for m in range(M):
+        words, z = [], []
+        for j, w in enumerate(top_token[m]):
+            if 0 <= w < V and w not in words:
+                words.append(int(w))
+                z.append(float(top_logit[m, j]) / heat)
+        words, z = np.array(words, int), np.array(z, np.float64)
+        if teacher_lse is None:
+            if not len(words):
+                continue
+            t = np.exp(z - z.max())
+            t, t_rest = t / t.sum(), 0.0
+        else:
+            t = np.exp(z - float(teacher_lse[m]))
+            t_rest = max(0.0, 1.0 - t.sum())
+        log_s = _log_shares(l[m] / heat)
+        outside = np.ones(V, bool)
+        outside[words] = False
+        with np.errstate(divide="ignore", invalid="ignore"):
+            used = t > 0
+            total = (t[used] * (np.log(t[used]) - log_s[words[used]])).sum()
+            inner = _log_shares(log_s[outside]) if outside.any() else np.zeros(0)
+            if t_rest > 0:
+                best = log_s[outside].max() if outside.any() else -np.inf
+                log_s_rest = best + np.log(np.exp(log_s[outside] - best).sum()) if best > -np.inf else -np.inf
+                total += t_rest * (np.log(t_rest) - log_s_rest)
+        loss[m] = heat * heat * total
+        if dloss is not None:
+            want = np.zeros(V)
+            want[words] = t
+            want[outside] = t_rest * np.exp(inner)
+            grad[m] = float(dloss[m]) * heat * (np.exp(log_s) - want)
+            if teacher_lse is None:
+                grad[m, outside] = float(dloss[m]) * heat * np.exp(log_s[outside])
+    return (loss, grad) if dloss is not None else loss

@@ -19,6 +19,7 @@ LSTM_ERR_ARG, LSTM_ERR_SHAPE, LSTM_ERR_STATE, LSTM_ERR_NOMEM, LSTM_ERR_LAUNCH, L
 LSTM_FMT_AUTO, LSTM_FMT_DENSE_MASKED, LSTM_FMT_ROW_COMPRESSED = 0, 1, 2
 LSTM_PLAN_AUTO, LSTM_PLAN_STEPWISE, LSTM_PLAN_PERSISTENT = 0, 1, 2
 LSTM_SCAN_STEPS = 16
+LSTM_DELTA_STEPS = 64
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liblstm355.so")
 
@@ -32,6 +33,8 @@ EXPORTS = [
     "lstm_scan_workspace_bytes", "lstm_scan_forward", "lstm_scan_backward", "lstm_rmsnorm_workspace_bytes", "lstm_rmsnorm_forward",
     "lstm_rmsnorm_backward", "lstm_quantize_fp8", "lstm_matmul_fp8_workspace_bytes", "lstm_matmul_fp8",
     "lstm_sample_workspace_bytes", "lstm_sample",
+    "lstm_delta_workspace_bytes", "lstm_delta_forward", "lstm_delta_backward", "lstm_logprobs_workspace_bytes", "lstm_logprobs_forward",
+    "lstm_logprobs_backward", "lstm_distill_workspace_bytes", "lstm_distill_forward", "lstm_distill_backward",
     "lstm_bench_copy", "lstm_bench_matmul", "lstm_bench_mfma", "lstm_bench_barrier", "lstm_bench_exchange", "lstm_bench_group_exchange",
 ]
 
@@ -122,7 +125,8 @@ def load(build_if_missing: bool = True):
     lib.lstm_bench_group_exchange.argtypes = [ci, ci, ci, ci, ci, ci, ci, ci, c.POINTER(c.c_double), c.POINTER(ci), vp]
     i64, sz = c.c_int64, c.c_size_t
     for name, types in (
-            ("lstm_scan", [ci] * 3), ("lstm_rmsnorm", [ci] * 2), ("lstm_matmul_fp8", [ci] * 3), ("lstm_sample", [ci] * 2)):
+            ("lstm_scan", [ci] * 3), ("lstm_rmsnorm", [ci] * 2), ("lstm_matmul_fp8", [ci] * 3), ("lstm_sample", [ci] * 2),
+            ("lstm_delta", [ci] * 7), ("lstm_logprobs", [ci] * 3), ("lstm_distill", [ci] * 3)):
         fn = getattr(lib, name + "_workspace_bytes")
         fn.restype, fn.argtypes = sz, types
     for name, types in (
@@ -132,7 +136,13 @@ def load(build_if_missing: bool = True):
             ("lstm_rmsnorm_backward", [ci] * 3 + [vp, i64, vp, vp] + [vp, i64] * 3 + [vp, vp, sz, vp]),
             ("lstm_quantize_fp8", [ci] * 4 + [vp, i64] * 3 + [vp]),
             ("lstm_matmul_fp8", [ci] * 3 + [vp, i64] * 4 + [ci, vp, ci, vp, i64, vp, sz, vp]),
-            ("lstm_sample", [ci] * 3 + [vp, i64, vp, i64] + [vp] * 9 + [sz, vp])):
+            ("lstm_sample", [ci] * 3 + [vp, i64, vp, i64] + [vp] * 9 + [sz, vp]),
+            ("lstm_delta_forward", [ci] * 7 + [vp, i64, i64] * 5 + [vp, c.c_float, vp, vp, i64, i64] + [vp] * 3 + [sz, vp]),
+            ("lstm_delta_backward", [ci] * 7 + [vp, i64, i64] * 5 + [vp, c.c_float, vp, vp, i64, i64, vp] + [vp, i64, i64] * 5 + [vp, vp, sz, vp]),
+            ("lstm_logprobs_forward", [ci] * 3 + [vp, i64, vp, i64] + [vp] * 5 + [ci] + [vp] * 3 + [sz, vp]),
+            ("lstm_logprobs_backward", [ci] * 3 + [vp, i64, vp, i64] + [vp] * 5 + [i64, vp]),
+            ("lstm_distill_forward", [ci] * 4 + [vp, i64] * 3 + [vp, c.c_float] + [vp] * 3 + [sz, vp]),
+            ("lstm_distill_backward", [ci] * 4 + [vp, i64] * 3 + [vp, c.c_float] + [vp] * 3 + [i64, vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = ci, types
     _lib = lib
@@ -468,6 +478,61 @@ def lstm_sample(M, V, dtype, logits_ptr, ld, allowed_ptr, allowed_ld, temperatur
                 token_ptr, prob_ptr, kept_ptr, ws_ptr, ws_bytes, stream=None) -> None:
     _check(load().lstm_sample(M, V, dtype, logits_ptr, ld, allowed_ptr, allowed_ld, temperature_ptr, top_k_ptr, top_p_ptr, min_p_ptr,
                               u_ptr, token_ptr, prob_ptr, kept_ptr, ws_ptr, ws_bytes, stream))
+
+
+def lstm_delta_workspace_bytes(T: int, B: int, heads: int, key_heads: int, key_dim: int, value_dim: int, backward: bool = False) -> int:
+    return load().lstm_delta_workspace_bytes(T, B, heads, key_heads, key_dim, value_dim, int(bool(backward)))
+
+
+def lstm_delta_forward(T, B, heads, key_heads, key_dim, value_dim, dtype, q_ptr, q_t, q_b, k_ptr, k_t, k_b, v_ptr, v_t, v_b, log_decay_ptr,
+                       log_decay_t, log_decay_b, beta_ptr, beta_t, beta_b, lengths_ptr, scale, S0_ptr, o_ptr, o_t, o_b, ST_ptr, states_ptr,
+                       ws_ptr, ws_bytes, stream=None) -> None:
+    _check(load().lstm_delta_forward(T, B, heads, key_heads, key_dim, value_dim, dtype, q_ptr, q_t, q_b, k_ptr, k_t, k_b, v_ptr, v_t, v_b,
+                                     log_decay_ptr, log_decay_t, log_decay_b, beta_ptr, beta_t, beta_b, lengths_ptr, scale, S0_ptr, o_ptr,
+                                     o_t, o_b, ST_ptr, states_ptr, ws_ptr, ws_bytes, stream))
+
+
+def lstm_delta_backward(T, B, heads, key_heads, key_dim, value_dim, dtype, q_ptr, q_t, q_b, k_ptr, k_t, k_b, v_ptr, v_t, v_b, log_decay_ptr,
+                        log_decay_t, log_decay_b, beta_ptr, beta_t, beta_b, lengths_ptr, scale, states_ptr, dO_ptr, do_t, do_b, dST_ptr,
+                        dq_ptr, dq_t, dq_b, dk_ptr, dk_t, dk_b, dv_ptr, dv_t, dv_b, dlog_decay_ptr, dlog_decay_t, dlog_decay_b, dbeta_ptr,
+                        dbeta_t, dbeta_b, dS0_ptr, ws_ptr, ws_bytes, stream=None) -> None:
+    _check(load().lstm_delta_backward(T, B, heads, key_heads, key_dim, value_dim, dtype, q_ptr, q_t, q_b, k_ptr, k_t, k_b, v_ptr, v_t, v_b,
+                                      log_decay_ptr, log_decay_t, log_decay_b, beta_ptr, beta_t, beta_b, lengths_ptr, scale, states_ptr,
+                                      dO_ptr, do_t, do_b, dST_ptr, dq_ptr, dq_t, dq_b, dk_ptr, dk_t, dk_b, dv_ptr, dv_t, dv_b,
+                                      dlog_decay_ptr, dlog_decay_t, dlog_decay_b, dbeta_ptr, dbeta_t, dbeta_b, dS0_ptr, ws_ptr, ws_bytes,
+                                      stream))
+
+
+def lstm_logprobs_workspace_bytes(M: int, V: int, top_n: int = 0) -> int:
+    return load().lstm_logprobs_workspace_bytes(M, V, top_n)
+
+
+def lstm_logprobs_forward(M, V, dtype, logits_ptr, ld, allowed_ptr, allowed_ld, token_ptr, logprob_ptr, rank_ptr, entropy_ptr, stats_ptr,
+                          top_n, top_token_ptr, top_logprob_ptr, ws_ptr, ws_bytes, stream=None) -> None:
+    _check(load().lstm_logprobs_forward(M, V, dtype, logits_ptr, ld, allowed_ptr, allowed_ld, token_ptr, logprob_ptr, rank_ptr, entropy_ptr,
+                                        stats_ptr, top_n, top_token_ptr, top_logprob_ptr, ws_ptr, ws_bytes, stream))
+
+
+def lstm_logprobs_backward(M, V, dtype, logits_ptr, ld, allowed_ptr, allowed_ld, token_ptr, stats_ptr, dlogprob_ptr, dentropy_ptr,
+                           dlogits_ptr, dlogits_ld, stream=None) -> None:
+    _check(load().lstm_logprobs_backward(M, V, dtype, logits_ptr, ld, allowed_ptr, allowed_ld, token_ptr, stats_ptr, dlogprob_ptr,
+                                         dentropy_ptr, dlogits_ptr, dlogits_ld, stream))
+
+
+def lstm_distill_workspace_bytes(M: int, V: int, K: int) -> int:
+    return load().lstm_distill_workspace_bytes(M, V, K)
+
+
+def lstm_distill_forward(M, V, K, dtype, logits_ptr, ld, top_token_ptr, top_token_ld, top_logit_ptr, top_logit_ld, teacher_lse_ptr,
+                         temperature, loss_ptr, stats_ptr, ws_ptr, ws_bytes, stream=None) -> None:
+    _check(load().lstm_distill_forward(M, V, K, dtype, logits_ptr, ld, top_token_ptr, top_token_ld, top_logit_ptr, top_logit_ld,
+                                       teacher_lse_ptr, temperature, loss_ptr, stats_ptr, ws_ptr, ws_bytes, stream))
+
+
+def lstm_distill_backward(M, V, K, dtype, logits_ptr, ld, top_token_ptr, top_token_ld, top_logit_ptr, top_logit_ld, teacher_lse_ptr,
+                          temperature, stats_ptr, dloss_ptr, dlogits_ptr, dlogits_ld, stream=None) -> None:
+    _check(load().lstm_distill_backward(M, V, K, dtype, logits_ptr, ld, top_token_ptr, top_token_ld, top_logit_ptr, top_logit_ld,
+                                        teacher_lse_ptr, temperature, stats_ptr, dloss_ptr, dlogits_ptr, dlogits_ld, stream))
 
 
 class Lstm:

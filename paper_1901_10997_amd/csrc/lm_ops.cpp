@@ -3,11 +3,12 @@
 #include "common.h"
 #include "lm_ops.h"
 
+#include <cfloat>
 #include <cstdio>
 
 using namespace l355;
 
-static_assert(LSTM_SCAN_STEPS == kScanSteps, "");
+static_assert(LSTM_SCAN_STEPS == kScanSteps && LSTM_DELTA_STEPS == kDeltaSteps, "");
 
 namespace {
 
@@ -102,6 +103,36 @@ bool matrix_ok(const void* p, int64_t ld, int rows, int cols, int dtype)
 {
     return !p || (of_type(p, dtype) && stride_ok(ld, rows > 1 ? cols : 0));
 }
+// The workspace of a call that has one
+int check_workspace(const char* entry, const void* ws, size_t got, size_t need)
+{
+    if (got < need) return small(entry, got, need);
+    if (!ws) return bad(entry, kNull);
+    return aligned(ws, 16) ? LSTM_OK : bad(entry, "the workspace is not 16-byte aligned");
+}
+// [T, B] rows of inputs, which may meet
+bool rows_ok(const void* p, int64_t t, int64_t b, int dtype) { return of_type(p, dtype) && stride_ok(t, 0) && stride_ok(b, 0); }
+// and of results, which may not
+bool results_ok(const void* p, int T, int B, int64_t t, int64_t b, int64_t width, int dtype) { return of_type(p, dtype) && apart(T, B, t, b, width); }
+
+bool delta_sizes_ok(int T, int B, int heads, int key_heads, int key_dim, int value_dim)
+{
+    return T >= 0 && T <= (1 << 30) && B >= 0 && B <= (1 << 24) && key_heads >= 1 && heads >= key_heads && heads <= (1 << 16) && heads % key_heads == 0 &&
+           key_dim >= 1 && key_dim <= kDeltaMaxKey && value_dim >= 1 && value_dim <= (1 << 16) && delta_fits(T, B, heads, key_dim, value_dim);
+}
+// What forward and backward take alike
+int check_delta(const char* entry, int dtype, float scale, const DeltaArgs& a)
+{
+    if (!is_type(dtype)) return bad(entry, kType);
+    if (!(scale >= -FLT_MAX && scale <= FLT_MAX)) return bad(entry, "scale is not finite");
+    if (a.T > 0 && a.B > 0 && (!a.q || !a.k || !a.v || !a.beta)) return bad(entry, kNull);
+    if (!rows_ok(a.q, a.q_t, a.q_b, dtype) || !rows_ok(a.k, a.k_t, a.k_b, dtype) || !rows_ok(a.v, a.v_t, a.v_b, dtype) ||
+        !rows_ok(a.beta, a.beta_t, a.beta_b, LSTM_F32) || (a.g && !rows_ok(a.g, a.g_t, a.g_b, LSTM_F32)))
+        return bad(entry, "a stride is negative or too large, or a pointer is not aligned to its element type");
+    if (!floats({a.lengths, a.states})) return bad(entry, kAlign);
+    return LSTM_OK;
+}
+
 bool eight_bits_ok(const void* p, int64_t ld, int cols) { return aligned(p, 16) && ld % 16 == 0 && stride_ok(ld, cols); }
 int blocks_of(int n) { return (n + kScaleCols - 1) / kScaleCols; }
 
@@ -272,6 +303,166 @@ int lstm_sample(int M, int V, int dtype, const void* logits, int64_t ld, const u
     if (!aligned(workspace, 16)) return bad(entry, "the workspace is not 16-byte aligned");
     const SampleArgs a = {M, V, dtype == LSTM_BF16, logits, ld, allowed, allowed_ld, temperature, top_k, top_p, min_p, u, token, prob, kept};
     return launched(entry, launch_sample, a, stream);
+}
+
+size_t lstm_delta_workspace_bytes(int T, int B, int heads, int key_heads, int key_dim, int value_dim, int backward)
+{
+    return delta_sizes_ok(T, B, heads, key_heads, key_dim, value_dim) ? delta_workspace_bytes(T, B, heads, key_heads, key_dim, value_dim, backward != 0) : 0;
+}
+
+int lstm_delta_forward(int T, int B, int heads, int key_heads, int key_dim, int value_dim, int dtype, const void* q, int64_t q_t,
+                       int64_t q_b, const void* k, int64_t k_t, int64_t k_b, const void* v, int64_t v_t, int64_t v_b,
+                       const float* log_decay, int64_t log_decay_t, int64_t log_decay_b, const float* beta, int64_t beta_t,
+                       int64_t beta_b, const int32_t* lengths, float scale, const float* S0, void* o, int64_t o_t, int64_t o_b,
+                       float* ST, float* states, void* workspace, size_t workspace_bytes, void* stream)
+{
+    static const char entry[] = "lstm_delta_forward";
+    if (!delta_sizes_ok(T, B, heads, key_heads, key_dim, value_dim)) return bad(entry, kSize);
+    DeltaArgs a = {};
+    a.T = T; a.B = B; a.heads = heads; a.key_heads = key_heads; a.Dk = key_dim; a.Dv = value_dim; a.bf16 = dtype == LSTM_BF16;
+    a.q = q; a.q_t = q_t; a.q_b = q_b; a.k = k; a.k_t = k_t; a.k_b = k_b; a.v = v; a.v_t = v_t; a.v_b = v_b;
+    a.g = log_decay; a.g_t = log_decay_t; a.g_b = log_decay_b; a.beta = beta; a.beta_t = beta_t; a.beta_b = beta_b;
+    a.lengths = lengths; a.scale = scale; a.S0 = S0; a.o = o; a.o_t = o_t; a.o_b = o_b; a.ST = ST; a.states = states; a.ws = (float*)workspace;
+    if (const int rc = check_delta(entry, dtype, scale, a)) return rc;
+    if (const int rc = check_workspace(entry, workspace, workspace_bytes, delta_workspace_bytes(T, B, heads, key_heads, key_dim, value_dim, false))) return rc;
+    if (B == 0) return LSTM_OK;
+    if (T > 0 && !o) return bad(entry, kNull);
+    if (!results_ok(o, T, B, o_t, o_b, (int64_t)heads * value_dim, dtype)) return bad(entry, "rows of o overlap, or it is not aligned to its element type");
+    if (!floats({S0, ST})) return bad(entry, kAlign);
+    return launched(entry, launch_delta_forward, a, stream);
+}
+
+int lstm_delta_backward(int T, int B, int heads, int key_heads, int key_dim, int value_dim, int dtype, const void* q, int64_t q_t,
+                        int64_t q_b, const void* k, int64_t k_t, int64_t k_b, const void* v, int64_t v_t, int64_t v_b,
+                        const float* log_decay, int64_t log_decay_t, int64_t log_decay_b, const float* beta, int64_t beta_t,
+                        int64_t beta_b, const int32_t* lengths, float scale, const float* states, const void* dO, int64_t do_t,
+                        int64_t do_b, const float* dST, void* dq, int64_t dq_t, int64_t dq_b, void* dk, int64_t dk_t, int64_t dk_b,
+                        void* dv, int64_t dv_t, int64_t dv_b, float* dlog_decay, int64_t dlog_decay_t, int64_t dlog_decay_b,
+                        float* dbeta, int64_t dbeta_t, int64_t dbeta_b, float* dS0, void* workspace, size_t workspace_bytes,
+                        void* stream)
+{
+    static const char entry[] = "lstm_delta_backward";
+    if (!delta_sizes_ok(T, B, heads, key_heads, key_dim, value_dim)) return bad(entry, kSize);
+    DeltaArgs a = {};
+    a.T = T; a.B = B; a.heads = heads; a.key_heads = key_heads; a.Dk = key_dim; a.Dv = value_dim; a.bf16 = dtype == LSTM_BF16;
+    a.q = q; a.q_t = q_t; a.q_b = q_b; a.k = k; a.k_t = k_t; a.k_b = k_b; a.v = v; a.v_t = v_t; a.v_b = v_b;
+    a.g = log_decay; a.g_t = log_decay_t; a.g_b = log_decay_b; a.beta = beta; a.beta_t = beta_t; a.beta_b = beta_b;
+    a.lengths = lengths; a.scale = scale; a.states = const_cast<float*>(states); a.dO = dO; a.do_t = do_t; a.do_b = do_b; a.dST = dST;
+    a.dq = dq; a.dq_t = dq_t; a.dq_b = dq_b; a.dk = dk; a.dk_t = dk_t; a.dk_b = dk_b; a.dv = dv; a.dv_t = dv_t; a.dv_b = dv_b;
+    a.dg = dlog_decay; a.dg_t = dlog_decay_t; a.dg_b = dlog_decay_b; a.dbeta = dbeta; a.dbeta_t = dbeta_t; a.dbeta_b = dbeta_b;
+    a.dS0 = dS0; a.ws = (float*)workspace;
+    if (const int rc = check_delta(entry, dtype, scale, a)) return rc;
+    if (const int rc = check_workspace(entry, workspace, workspace_bytes, delta_workspace_bytes(T, B, heads, key_heads, key_dim, value_dim, true))) return rc;
+    if (B == 0) return LSTM_OK;
+    if (T > 0 && (!states || !dO || !dq || !dk || !dv || !dbeta)) return bad(entry, kNull);
+    if (!rows_ok(dO, do_t, do_b, dtype)) return bad(entry, "a stride of dO is negative or too large, or it is not aligned to its element type");
+    const int64_t keys = (int64_t)key_heads * key_dim, values = (int64_t)heads * value_dim;
+    if (!results_ok(dq, T, B, dq_t, dq_b, keys, dtype) || !results_ok(dk, T, B, dk_t, dk_b, keys, dtype) ||
+        !results_ok(dv, T, B, dv_t, dv_b, values, dtype) || !results_ok(dbeta, T, B, dbeta_t, dbeta_b, heads, LSTM_F32) ||
+        (dlog_decay && !results_ok(dlog_decay, T, B, dlog_decay_t, dlog_decay_b, heads, LSTM_F32)))
+        return bad(entry, "rows of a result overlap, or it is not aligned to its element type");
+    if (!floats({dST, dS0})) return bad(entry, kAlign);
+    return launched(entry, launch_delta_backward, a, stream);
+}
+
+static bool top_ok(int top_n) { return top_n >= 0 && top_n <= kScoreMaxTop; }
+
+size_t lstm_logprobs_workspace_bytes(int M, int V, int top_n)
+{
+    return score_fits(M, V) && top_ok(top_n) ? std::max(kLeastWorkspace, score_workspace_bytes(M, V, top_n)) : 0;
+}
+
+// the rows that forward and backward take alike
+static int check_score(const char* entry, const ScoreArgs& a, int dtype)
+{
+    if (!score_fits(a.M, a.V)) return bad(entry, "V outside 1 .. 2^20, M outside 0 .. 2^22 - 1, or more than 2^24 pieces of 8192 logits");
+    if (!is_type(dtype)) return bad(entry, kType);
+    if (a.M > 0 && !a.logits) return bad(entry, kNull);
+    if (!matrix_ok(a.logits, a.ld, a.M, a.V, dtype) || !floats({a.token, a.logprob, a.rank, a.entropy, a.stats, a.top_token, a.top_logprob, a.dlogprob, a.dentropy}))
+        return bad(entry, "rows overlap, or a pointer is not aligned to its element type");
+    if (a.allowed && a.allowed_ld != 0 && !stride_ok(a.allowed_ld, a.V)) return bad(entry, "allowed_ld must be 0 or at least V");
+    return LSTM_OK;
+}
+
+int lstm_logprobs_forward(int M, int V, int dtype, const void* logits, int64_t ld, const uint8_t* allowed, int64_t allowed_ld,
+                          const int32_t* token, float* logprob, int32_t* rank, float* entropy, float* stats, int top_n,
+                          int32_t* top_token, float* top_logprob, void* workspace, size_t workspace_bytes, void* stream)
+{
+    static const char entry[] = "lstm_logprobs_forward";
+    ScoreArgs a = {};
+    a.M = M; a.V = V; a.bf16 = dtype == LSTM_BF16; a.logits = logits; a.ld = ld; a.allowed = allowed; a.allowed_ld = allowed_ld; a.token = token;
+    a.logprob = logprob; a.rank = rank; a.entropy = entropy; a.stats = stats; a.top_n = top_n; a.top_token = top_token; a.top_logprob = top_logprob;
+    a.ws = workspace;
+    if (const int rc = check_score(entry, a, dtype)) return rc;
+    if (!top_ok(top_n)) return bad(entry, "top_n outside 0 .. 64");
+    if (M > 0 && (((logprob || rank) && !token) || (top_n > 0 && (!top_token || !top_logprob)))) return bad(entry, kNull);
+    if (const int rc = check_workspace(entry, workspace, workspace_bytes, lstm_logprobs_workspace_bytes(M, V, top_n))) return rc;
+    if (M == 0) return LSTM_OK;
+    return launched(entry, launch_score_forward, a, stream);
+}
+
+int lstm_logprobs_backward(int M, int V, int dtype, const void* logits, int64_t ld, const uint8_t* allowed, int64_t allowed_ld,
+                           const int32_t* token, const float* stats, const float* dlogprob, const float* dentropy, void* dlogits,
+                           int64_t dlogits_ld, void* stream)
+{
+    static const char entry[] = "lstm_logprobs_backward";
+    ScoreArgs a = {};
+    a.M = M; a.V = V; a.bf16 = dtype == LSTM_BF16; a.logits = logits; a.ld = ld; a.allowed = allowed; a.allowed_ld = allowed_ld; a.token = token;
+    a.stats = const_cast<float*>(stats); a.dlogprob = dlogprob; a.dentropy = dentropy; a.dlogits = dlogits; a.dlogits_ld = dlogits_ld;
+    if (const int rc = check_score(entry, a, dtype)) return rc;
+    if (M > 0 && (!stats || !dlogits || (dlogprob && !token))) return bad(entry, kNull);
+    if (!matrix_ok(dlogits, dlogits_ld, M, V, dtype)) return bad(entry, "rows of dlogits overlap, or it is not aligned to its element type");
+    if (M == 0) return LSTM_OK;
+    return launched(entry, launch_score_backward, a, stream);
+}
+
+static int check_distill(const char* entry, const DistillArgs& a, int dtype)
+{
+    if (!score_fits(a.M, a.V)) return bad(entry, "V outside 1 .. 2^20, M outside 0 .. 2^22 - 1, or more than 2^24 pieces of 8192 logits");
+    if (a.K < 1 || a.K > kDistillMaxTop) return bad(entry, "K outside 1 .. 256");
+    if (!is_type(dtype)) return bad(entry, kType);
+    if (!(a.temperature >= 0x1p-20f && a.temperature <= 0x1p20f)) return bad(entry, "temperature outside 2^-20 .. 2^20");
+    if (a.M > 0 && (!a.logits || !a.top_token || !a.top_logit)) return bad(entry, kNull);
+    if (!matrix_ok(a.logits, a.ld, a.M, a.V, dtype) || !floats({a.top_token, a.top_logit, a.teacher_lse, a.loss, a.stats, a.dloss}))
+        return bad(entry, "rows overlap, or a pointer is not aligned to its element type");
+    if (a.M > 1 && (!stride_ok(a.top_token_ld, 0) || !stride_ok(a.top_logit_ld, 0))) return bad(entry, "a row length of the lists is negative or too large");
+    return LSTM_OK;
+}
+
+size_t lstm_distill_workspace_bytes(int M, int V, int K)
+{
+    return score_fits(M, V) && K >= 1 && K <= kDistillMaxTop ? std::max(kLeastWorkspace, distill_workspace_bytes(M, V)) : 0;
+}
+
+int lstm_distill_forward(int M, int V, int K, int dtype, const void* logits, int64_t ld, const int32_t* top_token, int64_t top_token_ld,
+                         const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, float temperature, float* loss,
+                         float* stats, void* workspace, size_t workspace_bytes, void* stream)
+{
+    static const char entry[] = "lstm_distill_forward";
+    DistillArgs a = {};
+    a.M = M; a.V = V; a.K = K; a.bf16 = dtype == LSTM_BF16; a.logits = logits; a.ld = ld; a.top_token = top_token; a.top_token_ld = top_token_ld;
+    a.top_logit = top_logit; a.top_logit_ld = top_logit_ld; a.teacher_lse = teacher_lse; a.temperature = temperature; a.loss = loss; a.stats = stats;
+    a.ws = workspace;
+    if (const int rc = check_distill(entry, a, dtype)) return rc;
+    if (const int rc = check_workspace(entry, workspace, workspace_bytes, lstm_distill_workspace_bytes(M, V, K))) return rc;
+    if (M == 0) return LSTM_OK;
+    return launched(entry, launch_distill_forward, a, stream);
+}
+
+int lstm_distill_backward(int M, int V, int K, int dtype, const void* logits, int64_t ld, const int32_t* top_token, int64_t top_token_ld,
+                          const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, float temperature,
+                          const float* stats, const float* dloss, void* dlogits, int64_t dlogits_ld, void* stream)
+{
+    static const char entry[] = "lstm_distill_backward";
+    DistillArgs a = {};
+    a.M = M; a.V = V; a.K = K; a.bf16 = dtype == LSTM_BF16; a.logits = logits; a.ld = ld; a.top_token = top_token; a.top_token_ld = top_token_ld;
+    a.top_logit = top_logit; a.top_logit_ld = top_logit_ld; a.teacher_lse = teacher_lse; a.temperature = temperature;
+    a.stats = const_cast<float*>(stats); a.dloss = dloss; a.dlogits = dlogits; a.dlogits_ld = dlogits_ld;
+    if (const int rc = check_distill(entry, a, dtype)) return rc;
+    if (M > 0 && (!stats || !dloss || !dlogits)) return bad(entry, kNull);
+    if (!matrix_ok(dlogits, dlogits_ld, M, V, dtype)) return bad(entry, "rows of dlogits overlap, or it is not aligned to its element type");
+    if (M == 0) return LSTM_OK;
+    return launched(entry, launch_distill_backward, a, stream);
 }
 
 }  // extern "C"

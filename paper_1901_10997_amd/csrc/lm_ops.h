@@ -1,4 +1,5 @@
-// Launchers of the operators around the cells (gated linear recurrence, RMS norm, 8-bit product, sampling); lm_ops.cpp
+// Launchers of the operators around the cells (gated linear recurrence and delta rule, RMS norm, 8-bit product, sampling, scores,
+// distillation); lm_ops.cpp
 // checks the arguments of the C entries and calls them.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -123,5 +124,83 @@ struct SampleArgs {
     int* kept;
 };
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
+
+// ---- gated delta rule (delta_kernels.hip)
+constexpr int kDeltaSteps = 64;             // steps of a block; the forward keeps the state in front of each
+constexpr int kDeltaMaxKey = 256;
+struct DeltaArgs {
+    int T, B, heads, key_heads, Dk, Dv, bf16;
+    const void *q, *k, *v;                  // [T, B, key_heads * Dk] twice, [T, B, heads * Dv]
+    int64_t q_t, q_b, k_t, k_b, v_t, v_b;
+    const float *g, *beta;                  // [T, B, heads]
+    int64_t g_t, g_b, beta_t, beta_b;
+    const int* lengths;
+    float scale;
+    const float* S0;                        // forward; [B, heads, Dk, Dv]
+    void* o;
+    int64_t o_t, o_b;
+    float* ST;
+    float* states;                          // written by the forward, read by the backward
+    const void* dO;                         // backward
+    int64_t do_t, do_b;
+    const float* dST;
+    void *dq, *dk, *dv;
+    int64_t dq_t, dq_b, dk_t, dk_b, dv_t, dv_b;
+    float *dg, *dbeta;
+    int64_t dg_t, dg_b, dbeta_t, dbeta_b;
+    float* dS0;
+    float* ws;
+};
+size_t delta_workspace_bytes(int T, int B, int heads, int key_heads, int Dk, int Dv, bool back);
+bool delta_fits(int T, int B, int heads, int Dk, int Dv);
+hipError_t launch_delta_forward(const DeltaArgs& a, hipStream_t s);
+hipError_t launch_delta_backward(const DeltaArgs& a, hipStream_t s);
+
+// ---- scores of tokens and the distillation loss (score_kernels.hip)
+constexpr int kScoreMaxTop = 64, kDistillMaxTop = 256;
+struct ScoreArgs {
+    int M, V, bf16;
+    const void* logits;
+    int64_t ld;
+    const uint8_t* allowed;
+    int64_t allowed_ld;
+    const int* token;
+    float* logprob;
+    int* rank;
+    float* entropy;
+    float* stats;                           // [M, 4]; written by the forward, read by the backward
+    int top_n;
+    int* top_token;
+    float* top_logprob;
+    const float* dlogprob;                  // backward
+    const float* dentropy;
+    void* dlogits;
+    int64_t dlogits_ld;
+    void* ws;
+};
+size_t score_workspace_bytes(int M, int V, int top_n);
+bool score_fits(int M, int V);
+hipError_t launch_score_forward(const ScoreArgs& a, hipStream_t s);
+hipError_t launch_score_backward(const ScoreArgs& a, hipStream_t s);
+struct DistillArgs {
+    int M, V, K, bf16;
+    const void* logits;
+    int64_t ld;
+    const int* top_token;
+    int64_t top_token_ld;
+    const float* top_logit;
+    int64_t top_logit_ld;
+    const float* teacher_lse;
+    float temperature;
+    float* loss;
+    float* stats;                           // [M, 4]; written by the forward, read by the backward
+    const float* dloss;                     // backward
+    void* dlogits;
+    int64_t dlogits_ld;
+    void* ws;
+};
+size_t distill_workspace_bytes(int M, int V);
+hipError_t launch_distill_forward(const DistillArgs& a, hipStream_t s);
+hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s);
 
 }  // namespace l355
