@@ -14,9 +14,14 @@
 //
 //     dU = P' dO + e K dS'     dR = X' dU     dv = b dR     dS = exp(G_last) dS' + scale Q' (y dO) - K' (y b dR)
 //
-// and leaves dS' and dR; the rest of the gradient again is made for all blocks at once (gradient).  A wave of 64 lanes holds
-// one value for each step of a block.  Running sums of g, and what is taken from each other of them, are in 64 bits: with
+// and leaves dS' and dR; the rest of the gradient again is made for all blocks at once (update, gradient).  A wave of 64 lanes
+// holds one value for each step of a block.  Running sums of g, and what is taken from each other of them, are in 64 bits: with
 // strong decay a sum over 64 steps has lost what the difference of two neighbours needs.
+//
+// Products.  The matrix instruction of bf16 is sixteen times as fast as that of fp32, so fp32 values are split into planes, each the
+// nearest bf16 to what those in front of it leave: three hold all 24 bits.  The product of planes i and j counts where i + j is below the
+// larger number of planes; what is left out is below 2^-24 (three planes) or 2^-16 (two) of the product.  Keys and queries in bf16 are one
+// plane.  Everything that reaches a state or an fp32 result has three; where a result is rounded to bf16 (2^-9) two do.
 #include "common.h"
 #include "elem.h"
 #include "lm_ops.h"
@@ -29,27 +34,116 @@ namespace {
 
 constexpr int C = kDeltaSteps;              // steps of a block, one for each lane
 constexpr int kWaves = 4;                   // of a workgroup; each takes 16 steps of a block
+constexpr int kThreads = 64 * kWaves;
 constexpr int kTile = 16;                   // columns of S of a workgroup
-constexpr int kCols = 20;                   // its row in LDS where columns lie side by side
-constexpr int kRow = C + 4;                 // row in LDS with a value for each step
-constexpr int kPrepared = 2 * C * C + 2 * C;   // X, P, y, e of a block
+constexpr int kRow = C + 4;                 // row of fp32 in LDS with a value for each step
+constexpr int kSteps = C + 8;               // row of a plane in LDS with a value for each step
 static_assert(C == 64 && kWaves * 16 == C, "");
 
-// The matrix instruction of fp32: lane (r, g) = (lane & 15, lane >> 4) gives rows r of A and columns r of B at k = g; four of
-// them take k = 4 g .. 4 g + 3 from a lane, in whatever order, so both operands are read four neighbouring k at a time.  Lane (r, g)
-// ends with rows 4 g .. 4 g + 3 of column r: what the next product takes as its B.
-__device__ __forceinline__ f32x4v mfma16(f32x4v a, f32x4v b, f32x4v c)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
-    return c;
-}
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint16_t u16;
+
+// planes of keys, queries and other operands of type E, and of what a result of that type is made from
+template <class E>
+constexpr int kPlanes = E::kBytes == 2 ? 1 : 3;
+template <class E>
+constexpr int kForResult = E::kBytes == 2 ? 2 : 3;
+
+constexpr f32x4v kZero4 = {0.f, 0.f, 0.f, 0.f};
 __device__ __forceinline__ f32x4v at4(const float* p) { return *(const f32x4v*)p; }
-// four values a row apart
-__device__ __forceinline__ f32x4v down4(const float* p, int ld) { return (f32x4v){p[0], p[ld], p[2 * ld], p[3 * ld]}; }
 __device__ __forceinline__ f32x4v scaled4(f32x4v v, float s) { return (f32x4v){v[0] * s, v[1] * s, v[2] * s, v[3] * s}; }
 __device__ __forceinline__ f32x4v times4(f32x4v a, f32x4v b) { return (f32x4v){a[0] * b[0], a[1] * b[1], a[2] * b[2], a[3] * b[3]}; }
-constexpr f32x4v kZero4 = {0.f, 0.f, 0.f, 0.f};
+
+// The matrix instruction: lane (r, g) = (lane & 15, lane >> 4) gives row r of A and column r of B at k = 8 g .. 8 g + 7 and ends with rows
+// 4 g .. 4 g + 3 of column r.  Where one product follows another, each order of planes has a sum of its own, so that they do not wait
+// for each other; where there are tiles enough, one holds all.
+template <int N>
+struct SumsOf {
+    f32x4v of[N];
+    __device__ __forceinline__ SumsOf()
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) of[i] = kZero4;
+    }
+    __device__ __forceinline__ f32x4v total() const
+    {
+        if constexpr (N == 1) return of[0];
+        else return of[0] + (of[1] + of[2]);
+    }
+};
+typedef SumsOf<3> Sums;
+typedef SumsOf<1> Sum;
+template <int N, int PA, int PB>
+__device__ __forceinline__ void multiply(SumsOf<N>& s, const bf16x8 (&a)[PA], const bf16x8 (&b)[PB])
+{
+    constexpr int kOrders = PA > PB ? PA : PB;
+#pragma unroll
+    for (int o = kOrders - 1; o >= 0; --o)
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+#pragma unroll
+            for (int j = 0; j < PB; ++j)
+                if (i + j == o) s.of[N == 1 ? 0 : o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], s.of[N == 1 ? 0 : o], 0, 0, 0);
+}
+// Planes in memory stand as the instruction takes them: tile after tile of 16 rows, of it step after step of 32 k, of it the eight values of
+// lane after lane.  (In rows, sixteen lanes that are served together met sixteen lines: the walk took 456 us for 128 blocks, 16 bytes
+// a clock.)
+constexpr int kFragment = 512;
+__device__ __forceinline__ int fragment_at(int tile, int steps, int step) { return (tile * steps + step) * kFragment; }
+// the lane's eight values of a fragment (or eight neighbouring k of a row in LDS), in planes `plane` elements apart
+template <int N>
+__device__ __forceinline__ void fragment(bf16x8 (&f)[N], const u16* p, int64_t plane)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = *(const bf16x8*)(p + i * plane);
+}
+// four values as planes
+template <int N>
+__device__ __forceinline__ void split4(f32x4v v, u32x2v (&out)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        out[i] = (u32x2v){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        if (i + 1 < N) {
+            v[0] -= bf16_lo(out[i][0]);
+            v[1] -= bf16_hi(out[i][0]);
+            v[2] -= bf16_lo(out[i][1]);
+            v[3] -= bf16_hi(out[i][1]);
+        }
+    }
+}
+template <int N>
+__device__ __forceinline__ void split8(f32x4v lo, f32x4v hi, bf16x8 (&out)[N])
+{
+    u32x2v l[N], h[N];
+    split4<N>(lo, l);
+    split4<N>(hi, h);
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i] = __builtin_bit_cast(bf16x8, (u32x4v){l[i][0], l[i][1], h[i][0], h[i][1]});
+}
+template <int N>
+__device__ __forceinline__ void store_split(f32x4v v, u16* p, int plane)
+{
+    u32x2v s[N];
+    split4<N>(v, s);
+#pragma unroll
+    for (int i = 0; i < N; ++i) *(u32x2v*)(p + i * plane) = s[i];
+}
+template <int N>
+__device__ __forceinline__ void store_split8(f32x4v lo, f32x4v hi, u16* p, int64_t plane)
+{
+    bf16x8 s[N];
+    split8<N>(lo, hi, s);
+#pragma unroll
+    for (int i = 0; i < N; ++i) *(bf16x8*)(p + i * plane) = s[i];
+}
+// A barrier that waits for LDS alone: what is under way from memory stays under way.
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+}
 
 // columns col .. col + 3 of a row that has `width` of them; 0 behind it
 template <class E>
@@ -88,40 +182,64 @@ __device__ __forceinline__ const typename E::T* row_of(const void* p, int64_t t_
 {
     return (const typename E::T*)p + t * t_stride + b * b_stride + first;
 }
-__device__ __forceinline__ int blocks_of(int T) { return (T + C - 1) / C; }
-__device__ __forceinline__ float* prepared_of(const DeltaArgs& a, int64_t block) { return a.ws + block * kPrepared; }
-__device__ __forceinline__ float* dstate_of(const DeltaArgs& a, int64_t block)
-{
-    return a.ws + (int64_t)blocks_of(a.T) * a.B * a.heads * kPrepared + block * a.Dk * a.Dv;
-}
-// dR of a block, and behind it e K dS'
-__device__ __forceinline__ float* dupdate_of(const DeltaArgs& a, int64_t block)
-{
-    return a.ws + (int64_t)blocks_of(a.T) * a.B * a.heads * (kPrepared + (int64_t)a.Dk * a.Dv) + block * 2 * C * a.Dv;
-}
-// dq and dk of a block and key head, while not all of its heads have been added
-__device__ __forceinline__ float* shared_of(const DeltaArgs& a, int64_t key_block)
-{
-    return a.ws + (int64_t)blocks_of(a.T) * a.B * a.heads * (kPrepared + (int64_t)(a.Dk + 2 * C) * a.Dv) + key_block * 2 * C * a.Dk;
-}
+
+// What prepare leaves in the workspace, in planes of fragments: for a block and key head K and Q, rows of steps, and K', Q', rows of key columns
+// (Q' for the gradient only); for a block and head X and P (or X, X' and P' for the gradient), then y and e.  Rows behind the end
+// and columns behind the key's are 0, so that the walks meet neither.  Then, for the gradient, fp32: dS', dR, e K dS', U, what
+// tiles of columns add to sums over a step's columns, and dq and dk of heads that share a key.
+template <class E, int DKP, bool BACK>
+struct Place {
+    static constexpr int kP = kPlanes<E>, kR = kForResult<E>;
+    static constexpr int64_t kMatrix = (int64_t)kP * C * DKP, kKeys = (BACK ? 4 : 3) * kMatrix;
+    static constexpr int64_t kHead = (BACK ? 9 : 3 + kR) * C * C + 4 * C;
+    static constexpr int kParts = 256;      // sums of a tile of columns: 64 each of three, and one
+    const DeltaArgs& a;
+    const int64_t key_blocks, head_blocks;
+    __host__ __device__ explicit Place(const DeltaArgs& args)
+        : a(args), key_blocks((int64_t)((args.T + C - 1) / C) * args.B * args.key_heads), head_blocks((int64_t)((args.T + C - 1) / C) * args.B * args.heads)
+    {
+    }
+    __host__ __device__ int tiles() const { return (a.Dv + kTile - 1) / kTile; }
+    __device__ u16* keys(const Block& k) const
+    {
+        return (u16*)a.ws + (((int64_t)k.c * a.B + k.b) * a.key_heads + k.h / (a.heads / a.key_heads)) * kKeys;
+    }
+    __device__ u16* K(const Block& k) const { return keys(k); }
+    __device__ u16* KT(const Block& k) const { return keys(k) + kMatrix; }
+    __device__ u16* Q(const Block& k) const { return keys(k) + 2 * kMatrix; }
+    __device__ u16* QT(const Block& k) const { return keys(k) + 3 * kMatrix; }
+    __device__ u16* X(const Block& k) const { return (u16*)a.ws + key_blocks * kKeys + k.index * kHead; }
+    __device__ u16* P(const Block& k) const { return X(k) + 3 * C * C; }
+    __device__ u16* XT(const Block& k) const { return X(k) + 3 * C * C; }
+    __device__ u16* PT(const Block& k) const { return X(k) + 6 * C * C; }
+    __device__ float* y(const Block& k) const { return (float*)(X(k) + kHead - 4 * C); }
+    __device__ float* e(const Block& k) const { return y(k) + C; }
+    __host__ __device__ int64_t first_floats() const { return (key_blocks * kKeys + head_blocks * kHead) / 2; }
+    __device__ float* floats() const { return a.ws + first_floats(); }
+    __device__ float* dS(const Block& k) const { return floats() + k.index * a.Dk * a.Dv; }
+    __host__ __device__ int64_t of_dS() const { return head_blocks * a.Dk * a.Dv; }
+    __device__ float* dR(const Block& k) const { return floats() + of_dS() + k.index * 3 * C * a.Dv; }
+    __device__ float* found(const Block& k) const { return dR(k) + C * a.Dv; }
+    __device__ float* U(const Block& k) const { return found(k) + C * a.Dv; }
+    __host__ __device__ int64_t to_parts() const { return of_dS() + head_blocks * 3 * C * a.Dv; }
+    __device__ float* parts(const Block& k, int tile) const { return floats() + to_parts() + (k.index * tiles() + tile) * kParts; }
+    __host__ __device__ int64_t to_shared() const { return to_parts() + head_blocks * tiles() * kParts; }
+    __device__ float* shared(const Block& k) const
+    {
+        return floats() + to_shared() + (((int64_t)k.c * a.B + k.b) * a.key_heads + k.h / (a.heads / a.key_heads)) * 2 * C * a.Dk;
+    }
+    __host__ __device__ int64_t to_sink() const { return BACK ? to_shared() + (a.heads > a.key_heads ? key_blocks * 2 * C * a.Dk : 0) : 0; }
+    // where lanes write that have nothing to write: a store without a branch leaves the count of what is under way known, so that
+    // nobody waits for more than it needs
+    __device__ float* sink() const { return floats() + to_sink(); }
+    __host__ size_t bytes() const { return (size_t)(first_floats() + to_sink() + 64) * sizeof(float); }
+};
 
 // Workgroups that read the same keys and queries follow each other on one XCD: hardware deals consecutive ones over eight.
 __device__ __forceinline__ unsigned by_xcd(unsigned blk, unsigned total)
 {
     const unsigned each = total / 8, more = total % 8, x = blk % 8, i = blk / 8;
     return x * each + min(x, more) + i;
-}
-
-// Rows t0 .. t0 + 63 of keys or queries in LDS, 0 behind the sequence's end and behind the row
-template <class E, int DKP>
-__device__ __forceinline__ void stage(const typename E::T* first, int64_t t_stride, int n, int width, float* to)
-{
-    constexpr int kPieces = DKP / 4;
-#pragma unroll 4
-    for (int p = threadIdx.x; p < C * kPieces; p += 64 * kWaves) {
-        const int row = p / kPieces, col = p % kPieces * 4;
-        *(f32x4v*)(to + row * (DKP + 4) + col) = row < n ? load4<E>(first + row * t_stride, col, width) : kZero4;
-    }
 }
 
 // A decay below exp(-10000) is 0 in fp32, and so is every product that has it; NaN stays NaN.
@@ -147,48 +265,134 @@ __device__ __forceinline__ float beta_at(const DeltaArgs& a, const Block& k, int
     return step < k.n ? *row_of<F32>(a.beta, a.beta_t, a.beta_b, k.t0 + step, k.b, k.h) : 0.f;
 }
 
-// X, P, y and e of every block.  X is built of blocks of 16: those on the diagonal by substitution, a column to a lane; then
-// X_ij = -X_ii sum_k L_ik X_kj, those one off the diagonal first.
-template <class E, int DKP>
-__global__ __launch_bounds__(64 * kWaves) void delta_prepare_kernel(DeltaArgs a)
+// The matrix instruction of fp32, in the same layout of rows, columns and results at k = 4 g .. 4 g + 3: for products of 16 by 16
+// blocks, whose result then is the next one's B as it stands.
+__device__ __forceinline__ f32x4v mfma16(f32x4v a, f32x4v b, f32x4v c)
 {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+__device__ __forceinline__ f32x4v down4(const float* p, int ld) { return (f32x4v){p[0], p[ld], p[2 * ld], p[3 * ld]}; }
+
+// Rows of keys or queries in LDS as they come: bf16 in rows of DKP + 8, fp32 in rows of DKP + 4; 0 behind the end and behind the row
+template <class E, int DKP>
+constexpr int kStaged = E::kBytes == 2 ? DKP + 8 : DKP + 4;
+template <class E, int DKP>
+__device__ __forceinline__ void stage(const typename E::T* first, int64_t t_stride, int n, int width, typename E::T* to)
+{
+    constexpr int kPieces = DKP / 4;
+#pragma unroll 4
+    for (int p = threadIdx.x; p < C * kPieces; p += kThreads) {
+        const int row = p / kPieces, col = p % kPieces * 4;
+        const f32x4v v = row < n ? load4<E>(first + row * t_stride, col, width) : kZero4;
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        store_n<E, 4>(to + row * kStaged<E, DKP> + col, f);
+    }
+}
+// Planes of a staged matrix and of its transpose
+template <class E, int DKP>
+__device__ __forceinline__ void write_planes(const typename E::T* from, u16* rows, u16* columns)
+{
+    constexpr int LD = kStaged<E, DKP>;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    if (rows)
+#pragma unroll 2
+        for (int f = w; f < C * DKP / kFragment; f += kWaves) {
+            const int at = (16 * (f / (DKP / 32)) + r) * LD + 32 * (f % (DKP / 32)) + 8 * g;
+            u16* const to = rows + f * kFragment + 8 * lane;
+            if constexpr (E::kBytes == 2) *(u32x4v*)to = *(const u32x4v*)(from + at);
+            else store_split8<3>(at4(from + at), at4(from + at + 4), to, C * DKP);
+        }
+    if (columns)
+#pragma unroll 2
+        for (int f = w; f < C * DKP / kFragment; f += kWaves) {
+            const typename E::T* const at = from + (32 * (f % 2) + 8 * g) * LD + 16 * (f / 2) + r;
+            u16* const to = columns + f * kFragment + 8 * lane;
+            typename E::T v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = at[i * LD];
+            if constexpr (E::kBytes == 2)
+                *(u32x4v*)to = (u32x4v){(uint32_t)v[0] | (uint32_t)v[1] << 16, (uint32_t)v[2] | (uint32_t)v[3] << 16, (uint32_t)v[4] | (uint32_t)v[5] << 16,
+                                        (uint32_t)v[6] | (uint32_t)v[7] << 16};
+            else store_split8<3>((f32x4v){v[0], v[1], v[2], v[3]}, (f32x4v){v[4], v[5], v[6], v[7]}, to, C * DKP);
+        }
+}
+// Planes of a matrix of 64 by 64 in LDS, or of its transpose
+template <int N, bool TRANSPOSED>
+__device__ __forceinline__ void write_square(const float* from, u16* to)
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int f = w; f < C * C / kFragment; f += kWaves) {
+        const int row = 16 * (f / 2) + r, col = 32 * (f % 2) + 8 * g;
+        u16* const out = to + f * kFragment + 8 * lane;
+        if constexpr (TRANSPOSED) store_split8<N>(down4(from + col * kRow + row, kRow), down4(from + (col + 4) * kRow + row, kRow), out, C * C);
+        else store_split8<N>(at4(from + row * kRow + col), at4(from + row * kRow + col + 4), out, C * C);
+    }
+}
+
+// X, P, y and e of every block, and the planes of keys and queries.  X is built of blocks of 16: those on the diagonal by substitution, a
+// column to a lane; then X_ij = -X_ii sum_k L_ik X_kj, those one off the diagonal first.
+template <class E, int DKP, bool BACK>
+__global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a)
+{
+    using T = typename E::T;
     extern __shared__ float lds[];
     __shared__ double Gs[C];
     __shared__ float betas[C];
-    constexpr int LD = DKP + 4;
-    float *const Ks = lds, *const Qs = lds + C * LD;
+    constexpr int LD = kStaged<E, DKP>;
+    T *const Ks = (T*)lds, *const Qs = Ks + C * LD;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const unsigned id = by_xcd(blockIdx.x, gridDim.x);
     const Block k = block_of(a, (int)(id / a.heads / a.B), (int)(id / a.heads % a.B), (int)(id % a.heads));
     if (k.n <= 0) return;
-    const int hk = k.h / (a.heads / a.key_heads);
+    const Place<E, DKP, BACK> at(a);
+    const int group = a.heads / a.key_heads, hk = k.h / group;
     stage<E, DKP>(row_of<E>(a.k, a.k_t, a.k_b, k.t0, k.b, (int64_t)hk * a.Dk), a.k_t, k.n, a.Dk, Ks);
     stage<E, DKP>(row_of<E>(a.q, a.q_t, a.q_b, k.t0, k.b, (int64_t)hk * a.Dk), a.q_t, k.n, a.Dk, Qs);
-    float* const out = prepared_of(a, k.index);
     if (w == 0) {
         const double G = running(a, k, lane);
         Gs[lane] = G;
         betas[lane] = beta_at(a, k, lane);
-        out[2 * C * C + lane] = expf((float)G);
-        out[2 * C * C + C + lane] = expf((float)(__shfl(G, 63) - G));
+        at.y(k)[lane] = expf((float)G);
+        at.e(k)[lane] = expf((float)(__shfl(G, 63) - G));
     }
     __syncthreads();
+    if (k.h % group == 0) {
+        write_planes<E, DKP>(Ks, at.K(k), at.KT(k));
+        write_planes<E, DKP>(Qs, at.Q(k), BACK ? at.QT(k) : nullptr);
+    }
     f32x4v kk[4], qk[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) kk[j] = qk[j] = kZero4;
-#pragma unroll 2
-    for (int d = 0; d < DKP; d += 16) {
-        const f32x4v ka = at4(Ks + (16 * w + r) * LD + d + 4 * g), qa = at4(Qs + (16 * w + r) * LD + d + 4 * g);
+    if constexpr (E::kBytes == 2) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (j > w) continue;
-            const f32x4v kb = at4(Ks + (16 * j + r) * LD + d + 4 * g);
-            kk[j] = mfma16(ka, kb, kk[j]);
-            qk[j] = mfma16(qa, kb, qk[j]);
+        for (int d = 0; d < DKP; d += 32) {
+            const bf16x8 ka = *(const bf16x8*)(Ks + (16 * w + r) * LD + d + 8 * g), qa = *(const bf16x8*)(Qs + (16 * w + r) * LD + d + 8 * g);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j > w) continue;
+                const bf16x8 kb = *(const bf16x8*)(Ks + (16 * j + r) * LD + d + 8 * g);
+                kk[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, kb, kk[j], 0, 0, 0);
+                qk[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qa, kb, qk[j], 0, 0, 0);
+            }
+        }
+    } else {
+#pragma unroll 2
+        for (int d = 0; d < DKP; d += 16) {
+            const f32x4v ka = at4(Ks + (16 * w + r) * LD + d + 4 * g), qa = at4(Qs + (16 * w + r) * LD + d + 4 * g);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j > w) continue;
+                const f32x4v kb = at4(Ks + (16 * j + r) * LD + d + 4 * g);
+                kk[j] = mfma16(ka, kb, kk[j]);
+                qk[j] = mfma16(qa, kb, qk[j]);
+            }
         }
     }
     __syncthreads();
-    float *const Ls = Ks, *const Xs = Qs;       // which are not needed any more
+    float *const Ls = lds, *const Xs = Ls + C * kRow, *const Ps = Xs + C * kRow;       // in place of what is not needed any more
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -202,7 +406,7 @@ __global__ __launch_bounds__(64 * kWaves) void delta_prepare_kernel(DeltaArgs a)
             }
             Ls[row * kRow + col] = l;
             Xs[row * kRow + col] = 0.f;
-            out[C * C + row * C + col] = p;
+            Ps[row * kRow + col] = p;
         }
     __syncthreads();
     if (lane < 16) {
@@ -216,6 +420,8 @@ __global__ __launch_bounds__(64 * kWaves) void delta_prepare_kernel(DeltaArgs a)
             Xs[(16 * w + i) * kRow + 16 * w + lane] = v;
         }
     }
+    if constexpr (BACK) write_square<3, true>(Ps, at.PT(k));
+    else write_square<kForResult<E>, false>(Ps, at.P(k));
 #pragma unroll
     for (int off = 1; off < 4; ++off) {
         __syncthreads();
@@ -229,104 +435,242 @@ __global__ __launch_bounds__(64 * kWaves) void delta_prepare_kernel(DeltaArgs a)
         for (int q = 0; q < 4; ++q) Xs[(16 * i + 4 * g + q) * kRow + 16 * j + r] = -sum[q];
     }
     __syncthreads();
-    for (int p = threadIdx.x; p < C * C / 4; p += 64 * kWaves)
-        *(f32x4v*)(out + p * 4) = at4(Xs + p / 16 * kRow + p % 16 * 4);
+    write_square<3, false>(Xs, at.X(k));
+    if constexpr (BACK) write_square<3, true>(Xs, at.XT(k));
 }
 
-// Forward: the walk over the blocks of one sequence and head, 16 columns of S.
-template <class E, int DKP>
-__global__ __launch_bounds__(64 * kWaves) void delta_walk_kernel(DeltaArgs a, int tiles)
-{
-    using T = typename E::T;
-    extern __shared__ float lds[];
-    constexpr int LD = DKP + 4, kParts = DKP / 64;      // tiles of 16 rows of S that a wave holds
-    float *const Ks = lds, *const Ss = Ks + C * LD, *const Rs = Ss + kTile * LD, *const Us = Rs + kTile * kRow, *const Es = Us + kTile * kRow;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const unsigned id = by_xcd(blockIdx.x, gridDim.x);
-    const int tile = (int)(id % tiles), h = (int)(id / tiles % a.heads), b = (int)(id / tiles / a.heads);
-    const int hk = h / (a.heads / a.key_heads), col = tile * kTile + r;
-    const bool live = col < a.Dv;
-    const int len = length_of(a, b);
-    const int64_t state = ((int64_t)b * a.heads + h) * a.Dk * a.Dv;
-    f32x4v S[kParts];
-#pragma unroll
-    for (int m = 0; m < kParts; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int d = 16 * (w * kParts + m) + 4 * g + i;
-            S[m][i] = a.S0 && live && d < a.Dk ? a.S0[state + (int64_t)d * a.Dv + col] : 0.f;
-        }
-    const int blocks = (len + C - 1) / C;
-    for (int c = 0; c < blocks; ++c) {
-        const Block k = block_of(a, c, b, h);
-        const float* const ready = prepared_of(a, k.index);
-        stage<E, DKP>(row_of<E>(a.k, a.k_t, a.k_b, k.t0, b, (int64_t)hk * a.Dk), a.k_t, k.n, a.Dk, Ks);
-#pragma unroll
-        for (int m = 0; m < kParts; ++m) *(f32x4v*)(Ss + r * LD + 16 * (w * kParts + m) + 4 * g) = S[m];
-        if (a.states) {
-            float* const to = a.states + ((int64_t)c * a.B * a.heads * a.Dk * a.Dv) + state;
-#pragma unroll
-            for (int m = 0; m < kParts; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int d = 16 * (w * kParts + m) + 4 * g + i;
-                    if (live && d < a.Dk) to[(int64_t)d * a.Dv + col] = S[m][i];
-                }
-        }
-        const int row = 16 * w + 4 * g;                 // the lane's four steps
-        const f32x4v y = at4(ready + 2 * C * C + row), e = at4(ready + 2 * C * C + C + row);
-        const float last = ready[2 * C * C + C - 1];
-        float beta[4], v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            beta[i] = beta_at(a, k, row + i);
-            v[i] = live && row + i < k.n ? E::load(row_of<E>(a.v, a.v_t, a.v_b, k.t0 + row + i, b, (int64_t)h * a.Dv + col)) : 0.f;
-        }
-        __syncthreads();
-        f32x4v ks = kZero4, qs = kZero4;
-        const T* const q_row = row_of<E>(a.q, a.q_t, a.q_b, k.t0 + 16 * w + r, b, (int64_t)hk * a.Dk);
-        const bool inside = 16 * w + r < k.n;
-#pragma unroll 4
-        for (int d = 0; d < DKP; d += 16) {
-            const f32x4v s = at4(Ss + r * LD + d + 4 * g);
-            ks = mfma16(at4(Ks + (16 * w + r) * LD + d + 4 * g), s, ks);
-            qs = mfma16(inside ? load4<E>(q_row, d + 4 * g, a.Dk) : kZero4, s, qs);
-        }
-        f32x4v R;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) R[i] = beta[i] * (v[i] - y[i] * ks[i]);
-        *(f32x4v*)(Rs + r * kRow + row) = R;
-        __syncthreads();
-        f32x4v U = kZero4;
-        for (int j = 0; j <= w; ++j) U = mfma16(at4(ready + (16 * w + r) * C + 16 * j + 4 * g), at4(Rs + r * kRow + 16 * j + 4 * g), U);
-        *(f32x4v*)(Us + r * kRow + row) = U;
-        *(f32x4v*)(Es + r * kRow + row) = times4(U, e);
-        __syncthreads();
-        f32x4v O;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) O[i] = a.scale * y[i] * qs[i];
-        for (int j = 0; j <= w; ++j) O = mfma16(at4(ready + C * C + (16 * w + r) * C + 16 * j + 4 * g), at4(Us + r * kRow + 16 * j + 4 * g), O);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (live && row + i < k.n)
-                E::store((T*)row_of<E>(a.o, a.o_t, a.o_b, k.t0 + row + i, b, (int64_t)h * a.Dv + col), O[i]);
-#pragma unroll
-        for (int m = 0; m < kParts; ++m) {
-            S[m] = scaled4(S[m], last);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                S[m] = mfma16(down4(Ks + (16 * j + 4 * g) * LD + 16 * (w * kParts + m) + r, LD), at4(Es + r * kRow + 16 * j + 4 * g), S[m]);
-        }
-        __syncthreads();
-    }
-    if (a.ST)
+// 16 columns of a state [Dk, Dv] as the accumulators of the workgroup hold them: wave w its rows 16 w DKP / 64 .., lane (r, g) four rows of
+// column r of each tile of 16
+template <int DKP>
+struct StateTile {
+    static constexpr int kParts = DKP / 64, LD = DKP + 8;
+    f32x4v v[kParts];
+    __device__ __forceinline__ void load(const float* from, const DeltaArgs& a, int w, int g, int col)
+    {
 #pragma unroll
         for (int m = 0; m < kParts; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int d = 16 * (w * kParts + m) + 4 * g + i;
-                if (live && d < a.Dk) a.ST[state + (int64_t)d * a.Dv + col] = S[m][i];
+                v[m][i] = from && col < a.Dv && d < a.Dk ? from[(int64_t)d * a.Dv + col] : 0.f;
             }
+    }
+    __device__ __forceinline__ void store(float* to, const DeltaArgs& a, int w, int g, int col) const
+    {
+#pragma unroll
+        for (int m = 0; m < kParts; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = 16 * (w * kParts + m) + 4 * g + i;
+                if (col < a.Dv && d < a.Dk) to[(int64_t)d * a.Dv + col] = v[m][i];
+            }
+    }
+    // without a branch: what the tile has more than the state goes to `sink`
+    __device__ __forceinline__ void store_all(float* to, float* sink, const DeltaArgs& a, int w, int g, int col) const
+    {
+#pragma unroll
+        for (int m = 0; m < kParts; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = 16 * (w * kParts + m) + 4 * g + i;
+                float* const p = col < a.Dv && d < a.Dk ? to + (int64_t)d * a.Dv + col : sink;
+                *p = v[m][i];
+            }
+    }
+    // planes of it in LDS, a row for each column
+    __device__ __forceinline__ void publish(u16* to, int w, int r, int g) const
+    {
+#pragma unroll
+        for (int m = 0; m < kParts; ++m) store_split<3>(v[m], to + r * LD + 16 * (w * kParts + m) + 4 * g, kTile * LD);
+    }
+};
+
+// Four steps of one column in rows of [T, B]: for each block's four, addresses that need one addition.  Steps behind the sequence's end
+// stand for the last one, and are 0 when taken; no load has a branch, and nothing waits for one here.
+template <class E>
+struct FourSteps {
+    typename E::T raw[4];
+    int64_t whole[4], last[4];
+    // n: steps of the last block
+    __device__ __forceinline__ void place(int row, int col, int64_t stride, int n)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            whole[i] = (row + i) * stride + col;
+            last[i] = min(row + i, n - 1) * stride + col;
+        }
+    }
+    __device__ __forceinline__ void load(const typename E::T* from, bool is_last)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = from[is_last ? last[i] : whole[i]];
+    }
+    __device__ __forceinline__ f32x4v take(int row, int n) const
+    {
+        f32x4v v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = row + i < n ? E::load(raw + i) : 0.f;
+        return v;
+    }
+};
+// Forward: the walk over the blocks of one sequence and head, 16 columns of S.  Keys, queries, X and P come from memory as the matrix
+// instruction takes them, those of the next block while this one is worked on; S, R and U pass through LDS in planes.
+//
+// Bound: the chain S -> R -> U -> S of a block, three products with a barrier behind each, by one wave on a SIMD; what is not on it (Q S, P U,
+// O and all loads) stands where the chain waits: Q S behind R's barrier, P U behind the next block's first.
+template <class E, int DKP, bool STATES>
+__global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) void delta_walk_kernel(DeltaArgs a, int tiles)
+{
+    using T = typename E::T;
+    constexpr int kP = kPlanes<E>, kR = kForResult<E>, LD = DKP + 8, kParts = DKP / 64, kK = DKP / 32;
+    __shared__ u16 Ss[3 * kTile * LD], Rs[3 * kTile * kSteps], Us[kR * kTile * kSteps], Es[3 * kTile * kSteps];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const unsigned id = by_xcd(blockIdx.x, gridDim.x);
+    const int tile = (int)(id % tiles), h = (int)(id / tiles % a.heads), b = (int)(id / tiles / a.heads);
+    const int col = tile * kTile + r, row = 16 * w + 4 * g;             // the lane's column and the first of its four steps
+    const bool live = col < a.Dv;
+    const int len = length_of(a, b), blocks = (len + C - 1) / C;
+    const int64_t state = ((int64_t)b * a.heads + h) * a.Dk * a.Dv, states_step = (int64_t)a.B * a.heads * a.Dk * a.Dv;
+    const Place<E, DKP, false> at(a);
+    StateTile<DKP> S;
+    S.load(a.S0 ? a.S0 + state : nullptr, a, w, g, col);
+    if (blocks > 0) {
+        // addresses: the same for all lanes, and a lane's own 32 bits
+        const Block first = {0, b, h, 0, 0, (int64_t)b * a.heads + h};
+        const int64_t keys_step = (int64_t)a.B * a.key_heads * at.kKeys, head_step = (int64_t)a.B * a.heads * at.kHead;
+        const u16 *K0 = at.K(first) + fragment_at(w, kK, 0), *Q0 = at.Q(first) + fragment_at(w, kK, 0), *KT0 = at.KT(first) + fragment_at(w * kParts, 2, 0),
+                  *X0 = at.X(first) + fragment_at(w, 2, 0), *P0 = at.P(first) + fragment_at(w, 2, 0);
+        const float* y0 = at.y(first);
+        const unsigned mine = 8 * lane;
+        const float* beta0 = row_of<F32>(a.beta, a.beta_t, a.beta_b, 0, b, h);
+        const T* v0 = row_of<E>(a.v, a.v_t, a.v_b, 0, b, (int64_t)h * a.Dv);
+        T* const o0 = (T*)row_of<E>(a.o, a.o_t, a.o_b, 0, b, (int64_t)h * a.Dv);
+        const int64_t o_at[4] = {row * a.o_t + col, (row + 1) * a.o_t + col, (row + 2) * a.o_t + col, (row + 3) * a.o_t + col};
+        float* const sink = at.sink() + lane;
+        bf16x8 K[kK][kP], Q[kK][kP], X[2][3], KT[kParts][2][kP], P[2][kR];
+        f32x4v y, e, O = kZero4;
+        FourSteps<E> v;
+        FourSteps<F32> beta;
+        float last;
+        const int rest = len - (blocks - 1) * C;        // steps of the last block
+        v.place(row, min(col, a.Dv - 1), a.v_t, rest);
+        beta.place(row, 0, a.beta_t, rest);
+        const auto load_keys = [&](int c) {
+#pragma unroll
+            for (int s = 0; s < kK; ++s) {
+                fragment<kP>(K[s], K0 + fragment_at(0, kK, s) + mine, C * DKP);
+                fragment<kP>(Q[s], Q0 + fragment_at(0, kK, s) + mine, C * DKP);
+            }
+            y = at4(y0 + row);
+            e = at4(y0 + C + row);
+            last = y0[C - 1];
+            v.load(v0, c == blocks - 1);
+            beta.load(beta0, c == blocks - 1);
+        };
+        const auto load_inverse = [&]() {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) fragment<3>(X[s], X0 + fragment_at(0, 2, s) + mine, C * C);
+        };
+        const auto load_columns = [&]() {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int m = 0; m < kParts; ++m) fragment<kP>(KT[m][s], KT0 + fragment_at(m, 2, s) + mine, C * DKP);
+        };
+        const auto load_pairs = [&]() {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) fragment<kR>(P[s], P0 + fragment_at(0, 2, s) + mine, C * C);
+        };
+        // O of a block whose U is in LDS
+        const auto finish = [&](int c) {
+            Sum pu;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                bf16x8 uf[kR];
+                fragment<kR>(uf, Us + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
+                multiply(pu, P[s], uf);
+            }
+            O += pu.total();
+            const int n = len - c * C;
+            T* const to = o0 + (int64_t)c * C * a.o_t;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) E::store(live && c >= 0 && row + i < n ? to + o_at[i] : (T*)sink, O[i]);
+        };
+        load_keys(0);
+        load_inverse();
+        load_columns();
+        load_pairs();
+        S.publish(Ss, w, r, g);
+        // No branch in here: where one followed a matrix instruction the compiler has left out the wait in front of its result (two of the
+        // eight instructions that lie between them elsewhere), and half of a result was what stood there before.
+#pragma unroll 1
+        for (int c = 0; c < blocks; ++c) {
+            if constexpr (STATES) S.store_all(a.states + c * states_step + state, sink, a, w, g, col);
+            lds_barrier();
+            Sum ks, qs, u;
+            bf16x8 f[kK][3];
+#pragma unroll
+            for (int s = 0; s < kK; ++s) fragment<3>(f[s], Ss + r * LD + 32 * s + 8 * g, kTile * LD);
+#pragma unroll
+            for (int s = 0; s < kK; ++s) multiply(ks, K[s], f[s]);
+            const int n = len - c * C;
+            const f32x4v b4 = beta.take(row, n), v4 = v.take(row, n), found = ks.total(), decay = e, y4 = y;
+            const float decayed = last;
+            f32x4v R;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) R[i] = b4[i] * (v4[i] - y4[i] * found[i]);
+            store_split<3>(R, Rs + r * kSteps + row, kTile * kSteps);
+            finish(c - 1);                      // in front of the first block of nothing, to nowhere
+            lds_barrier();
+            bf16x8 rf[2][3];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) fragment<3>(rf[s], Rs + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
+#pragma unroll
+            for (int s = 0; s < kK; ++s) {
+                if constexpr (kR == 2) {
+                    const bf16x8 two[2] = {f[s][0], f[s][1]};
+                    multiply(qs, Q[s], two);
+                } else {
+                    multiply(qs, Q[s], f[s]);
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) multiply(u, X[s], rf[s]);
+            const f32x4v U = u.total();
+            store_split<3>(times4(U, decay), Es + r * kSteps + row, kTile * kSteps);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) O[i] = qs.total()[i] * (a.scale * y4[i]);
+            lds_barrier();
+            bf16x8 ef[2][3];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) fragment<3>(ef[s], Es + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
+            store_split<kR>(U, Us + r * kSteps + row, kTile * kSteps);
+            const bool more = c + 1 < blocks;
+            K0 += more ? keys_step : 0;
+            Q0 += more ? keys_step : 0;
+            X0 += more ? head_step : 0;
+            y0 += more ? head_step / 2 : 0;
+            v0 += more ? C * a.v_t : 0;
+            beta0 += more ? C * a.beta_t : 0;
+            load_keys(more ? c + 1 : c);
+            load_inverse();
+            load_pairs();                       // of this block: used behind the next barrier
+            P0 += more ? head_step : 0;
+#pragma unroll
+            for (int m = 0; m < kParts; ++m) {
+                Sum sum;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) multiply(sum, KT[m][s], ef[s]);
+                S.v[m] = scaled4(S.v[m], decayed) + sum.total();
+            }
+            S.publish(Ss, w, r, g);
+            KT0 += more ? keys_step : 0;
+            load_columns();
+        }
+        lds_barrier();
+        finish(blocks - 1);
+    }
+    if (a.ST) S.store(a.ST + state, a, w, g, col);
     for (int64_t t = len + (threadIdx.x >> 4); t < a.T; t += 4 * kWaves)
         if (live) E::store((T*)row_of<E>(a.o, a.o_t, a.o_b, t, b, (int64_t)h * a.Dv + col), 0.f);
 }
@@ -419,106 +763,170 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a, int tiles)
             if (col + i < a.Dv) E::store((T*)row_of<E>(a.o, a.o_t, a.o_b, t, b, (int64_t)h * a.Dv) + col + i, 0.f);
 }
 
-// Gradient: the walk back over the blocks, 16 columns of dS.
+// Gradient: the walk back over the blocks, 16 columns of dS.  Its chain is dS' -> dU -> dR -> dS; Q' (y dO) stands where dR is
+// waited for.
 template <class E, int DKP>
-__global__ __launch_bounds__(64 * kWaves) void delta_walk_back_kernel(DeltaArgs a, int tiles)
+__global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) void delta_walk_back_kernel(DeltaArgs a, int tiles)
 {
     using T = typename E::T;
-    extern __shared__ float lds[];
-    constexpr int LD = DKP + 4, kParts = DKP / 64;
-    float *const Ks = lds, *const Qs = Ks + C * LD, *const Ds = Qs + C * LD, *const Os = Ds + kTile * LD, *const Us = Os + kTile * kRow,
-                 *const Zs = Us + kTile * kRow;
+    constexpr int kP = kPlanes<E>, LD = DKP + 8, kParts = DKP / 64, kK = DKP / 32;
+    __shared__ u16 Ds[3 * kTile * LD], Os[kP * kTile * kSteps], Us[3 * kTile * kSteps], Ys[3 * kTile * kSteps], Zs[3 * kTile * kSteps];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const unsigned id = by_xcd(blockIdx.x, gridDim.x);
     const int tile = (int)(id % tiles), h = (int)(id / tiles % a.heads), b = (int)(id / tiles / a.heads);
-    const int hk = h / (a.heads / a.key_heads), col = tile * kTile + r;
+    const int col = tile * kTile + r, row = 16 * w + 4 * g;
     const bool live = col < a.Dv;
-    const int len = length_of(a, b);
+    const int len = length_of(a, b), blocks = (len + C - 1) / C;
     const int64_t state = ((int64_t)b * a.heads + h) * a.Dk * a.Dv;
-    f32x4v dS[kParts];
+    const Place<E, DKP, true> at(a);
+    StateTile<DKP> dS;
+    dS.load(a.dST ? a.dST + state : nullptr, a, w, g, col);
+    if (blocks > 0) {
+        const Block behind = {blocks - 1, b, h, 0, 0, ((int64_t)(blocks - 1) * a.B + b) * a.heads + h};
+        const int64_t keys_step = (int64_t)a.B * a.key_heads * at.kKeys, head_step = (int64_t)a.B * a.heads * at.kHead;
+        const u16 *K0 = at.K(behind) + fragment_at(w, kK, 0), *KT0 = at.KT(behind) + fragment_at(w * kParts, 2, 0), *QT0 = at.QT(behind) + fragment_at(w * kParts, 2, 0),
+                  *XT0 = at.XT(behind) + fragment_at(w, 2, 0), *PT0 = at.PT(behind) + fragment_at(w, 2, 0);
+        const float* y0 = at.y(behind);
+        const unsigned mine = 8 * lane;
+        const float* beta0 = row_of<F32>(a.beta, a.beta_t, a.beta_b, (int64_t)behind.c * C, b, h);
+        const T* dO0 = row_of<E>(a.dO, a.do_t, a.do_b, (int64_t)behind.c * C, b, (int64_t)h * a.Dv);
+        T* const dv0 = (T*)row_of<E>(a.dv, a.dv_t, a.dv_b, 0, b, (int64_t)h * a.Dv);
+        const int64_t dv_at[4] = {row * a.dv_t + col, (row + 1) * a.dv_t + col, (row + 2) * a.dv_t + col, (row + 3) * a.dv_t + col};
+        float* const sink = at.sink() + lane;
+        bf16x8 K[kK][kP], PT[2][3], XT[2][3], KT[kParts][2][kP], QT[kParts][2][kP];
+        f32x4v y, e, dO, b4;
+        FourSteps<E> raw;
+        FourSteps<F32> beta;
+        float last;
+        const int rest = len - behind.c * C;
+        raw.place(row, min(col, a.Dv - 1), a.do_t, rest);
+        beta.place(row, 0, a.beta_t, rest);
+        const auto load_gates = [&]() {
+            y = at4(y0 + row);
+            e = at4(y0 + C + row);
+            last = y0[C - 1];
+        };
+        const auto load_keys = [&]() {
 #pragma unroll
-    for (int m = 0; m < kParts; ++m)
+            for (int s = 0; s < kK; ++s) fragment<kP>(K[s], K0 + fragment_at(0, kK, s) + mine, C * DKP);
+        };
+        const auto load_pairs = [&](bool is_last) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int d = 16 * (w * kParts + m) + 4 * g + i;
-            dS[m][i] = a.dST && live && d < a.Dk ? a.dST[state + (int64_t)d * a.Dv + col] : 0.f;
-        }
-    for (int c = (len + C - 1) / C - 1; c >= 0; --c) {
-        const Block k = block_of(a, c, b, h);
-        const float* const ready = prepared_of(a, k.index);
-        stage<E, DKP>(row_of<E>(a.k, a.k_t, a.k_b, k.t0, b, (int64_t)hk * a.Dk), a.k_t, k.n, a.Dk, Ks);
-        stage<E, DKP>(row_of<E>(a.q, a.q_t, a.q_b, k.t0, b, (int64_t)hk * a.Dk), a.q_t, k.n, a.Dk, Qs);
-        float *const behind = dstate_of(a, k.index), *const left = dupdate_of(a, k.index);
+            for (int s = 0; s < 2; ++s) fragment<3>(PT[s], PT0 + fragment_at(0, 2, s) + mine, C * C);
+            raw.load(dO0, is_last);
+            beta.load(beta0, is_last);
+        };
+        const auto load_inverse = [&]() {
 #pragma unroll
-        for (int m = 0; m < kParts; ++m) {
-            *(f32x4v*)(Ds + r * LD + 16 * (w * kParts + m) + 4 * g) = dS[m];
+            for (int s = 0; s < 2; ++s) fragment<3>(XT[s], XT0 + fragment_at(0, 2, s) + mine, C * C);
+        };
+        const auto load_columns = [&](bf16x8(&to)[kParts][2][kP], const u16* from) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int m = 0; m < kParts; ++m) fragment<kP>(to[m][s], from + fragment_at(m, 2, s) + mine, C * DKP);
+        };
+        Sum po;
+        const auto take_pairs = [&](int n) {    // of the block that comes next; its dO in LDS
+            dO = raw.take(row, n);
+            b4 = beta.take(row, n);
+            store_split<kP>(dO, Os + r * kSteps + row, kTile * kSteps);
+        };
+        const auto multiply_pairs = [&]() {
+            po = Sum();
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                bf16x8 f[kP];
+                fragment<kP>(f, Os + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
+                multiply(po, PT[s], f);
+            }
+        };
+        load_pairs(true);
+        load_gates();
+        load_keys();
+        load_inverse();
+        load_columns(QT, QT0);
+        load_columns(KT, KT0);
+        take_pairs(rest);
+        dS.publish(Ds, w, r, g);
+        // no branch in here, as in the walk forward
+#pragma unroll 1
+        for (int c = blocks - 1; c >= 0; --c) {
+            const int n = len - c * C;
+            Block k = behind;
+            k.index = ((int64_t)c * a.B + b) * a.heads + h;
+            dS.store_all(at.dS(k), sink, a, w, g, col);
+            const f32x4v dO4 = dO, beta4 = b4;
+            const bool more = c > 0;
+            lds_barrier();
+            bf16x8 f[kK][3];
+            Sum kd, dr;
+#pragma unroll
+            for (int s = 0; s < kK; ++s) fragment<3>(f[s], Ds + r * LD + 32 * s + 8 * g, kTile * LD);
+#pragma unroll
+            for (int s = 0; s < kK; ++s) multiply(kd, K[s], f[s]);
+            multiply_pairs();
+            const f32x4v found = times4(kd.total(), e), dU = found + po.total();
+            store_split<3>(dU, Us + r * kSteps + row, kTile * kSteps);
+            f32x4v yO, yb;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int d = 16 * (w * kParts + m) + 4 * g + i;
-                if (live && d < a.Dk) behind[(int64_t)d * a.Dv + col] = dS[m][i];
+                yO[i] = a.scale * y[i] * dO4[i];
+                yb[i] = -y[i] * beta4[i];
             }
-        }
-        const int row = 16 * w + 4 * g;
-        const f32x4v y = at4(ready + 2 * C * C + row), e = at4(ready + 2 * C * C + C + row);
-        const float last = ready[2 * C * C + C - 1];
-        float beta[4];
-        f32x4v dO;
+            const float decayed = last;
+            store_split<3>(yO, Ys + r * kSteps + row, kTile * kSteps);
+            lds_barrier();
+            bf16x8 uf[2][3], yf[2][3], zf[2][3];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            beta[i] = beta_at(a, k, row + i);
-            dO[i] = live && row + i < k.n ? E::load(row_of<E>(a.dO, a.do_t, a.do_b, k.t0 + row + i, b, (int64_t)h * a.Dv + col)) : 0.f;
-        }
-        *(f32x4v*)(Os + r * kRow + row) = dO;
-        __syncthreads();
-        f32x4v dU = kZero4;
-#pragma unroll 4
-        for (int d = 0; d < DKP; d += 16) dU = mfma16(at4(Ks + (16 * w + r) * LD + d + 4 * g), at4(Ds + r * LD + d + 4 * g), dU);
-        dU = times4(dU, e);
-        if (live)
+            for (int s = 0; s < 2; ++s) fragment<3>(uf[s], Us + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) left[(int64_t)(C + row + i) * a.Dv + col] = dU[i];
-        for (int j = w; j < 4; ++j)
-            dU = mfma16(down4(ready + C * C + (16 * j + 4 * g) * C + 16 * w + r, C), at4(Os + r * kRow + 16 * j + 4 * g), dU);
-        *(f32x4v*)(Us + r * kRow + row) = dU;
-        __syncthreads();
-        f32x4v dR = kZero4;
-        for (int j = w; j < 4; ++j) dR = mfma16(down4(ready + (16 * j + 4 * g) * C + 16 * w + r, C), at4(Us + r * kRow + 16 * j + 4 * g), dR);
-        f32x4v Z;
+            for (int s = 0; s < 2; ++s) fragment<3>(yf[s], Ys + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float dv = beta[i] * dR[i];
-            Z[i] = -y[i] * dv;
-            if (live) {
-                left[(int64_t)(row + i) * a.Dv + col] = dR[i];
-                if (row + i < k.n) E::store((T*)row_of<E>(a.dv, a.dv_t, a.dv_b, k.t0 + row + i, b, (int64_t)h * a.Dv + col), dv);
+            for (int s = 0; s < 2; ++s) multiply(dr, XT[s], uf[s]);
+            K0 -= more ? keys_step : 0;
+            PT0 -= more ? head_step : 0;
+            XT0 -= more ? head_step : 0;
+            y0 -= more ? head_step / 2 : 0;
+            dO0 -= more ? C * a.do_t : 0;
+            beta0 -= more ? C * a.beta_t : 0;
+            load_pairs(!more && blocks == 1);   // all blocks but the last are whole
+            load_gates();
+            load_keys();
+            Sum sums[kParts];
+#pragma unroll
+            for (int m = 0; m < kParts; ++m)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) multiply(sums[m], QT[m][s], yf[s]);
+            const f32x4v dR = dr.total();
+            store_split<3>(times4(yb, dR), Zs + r * kSteps + row, kTile * kSteps);
+            QT0 -= more ? keys_step : 0;
+            load_columns(QT, QT0);
+            load_inverse();
+            lds_barrier();
+#pragma unroll
+            for (int s = 0; s < 2; ++s) fragment<3>(zf[s], Zs + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
+#pragma unroll
+            for (int m = 0; m < kParts; ++m) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) multiply(sums[m], KT[m][s], zf[s]);
+                dS.v[m] = scaled4(dS.v[m], decayed) + sums[m].total();
             }
-        }
-        *(f32x4v*)(Zs + r * kRow + row) = Z;
-        __syncthreads();
-        f32x4v from_o[4];
+            dS.publish(Ds, w, r, g);
+            float *const left = at.dR(k) + (int64_t)row * a.Dv + col, *const f0 = at.found(k) + (int64_t)row * a.Dv + col;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            from_o[j] = times4(at4(Os + r * kRow + 16 * j + 4 * g), scaled4(at4(ready + 2 * C * C + 16 * j + 4 * g), a.scale));
-#pragma unroll
-        for (int m = 0; m < kParts; ++m) {
-            dS[m] = scaled4(dS[m], last);
-            const int d = 16 * (w * kParts + m) + r;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                dS[m] = mfma16(down4(Qs + (16 * j + 4 * g) * LD + d, LD), from_o[j], dS[m]);
-                dS[m] = mfma16(down4(Ks + (16 * j + 4 * g) * LD + d, LD), at4(Zs + r * kRow + 16 * j + 4 * g), dS[m]);
+            for (int i = 0; i < 4; ++i) {
+                float *const p = live ? left + (int64_t)i * a.Dv : sink, *const q = live ? f0 + (int64_t)i * a.Dv : sink;
+                *p = dR[i];
+                *q = found[i];
+                E::store(live && row + i < n ? dv0 + (int64_t)c * C * a.dv_t + dv_at[i] : (T*)sink, beta4[i] * dR[i]);
             }
+            KT0 -= more ? keys_step : 0;
+            load_columns(KT, KT0);
+            take_pairs(C);
         }
-        __syncthreads();
     }
-    if (a.dS0)
-#pragma unroll
-        for (int m = 0; m < kParts; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = 16 * (w * kParts + m) + 4 * g + i;
-                if (live && d < a.Dk) a.dS0[state + (int64_t)d * a.Dv + col] = dS[m][i];
-            }
+    if (a.dS0) dS.store(a.dS0 + state, a, w, g, col);
     for (int64_t t = len + (threadIdx.x >> 4); t < a.T; t += 4 * kWaves)
         if (live) E::store((T*)row_of<E>(a.dv, a.dv_t, a.dv_b, t, b, (int64_t)h * a.Dv + col), 0.f);
 }
@@ -535,7 +943,90 @@ __device__ __forceinline__ float row16_sum(float v)
 template <int N>
 __device__ __forceinline__ float row16_shifted(float v) { return dpp_move<0x110 + N>(v); }
 
-// What is left of a block's gradient, from the state S in front of it, dS' behind it and dR: with U made again,
+// U of every block again, from the state in front of it, 16 columns to a workgroup, and the columns' part of what sums over a
+// step's columns: dR.(v - y K S), -y b dR.(K S), U.(e K dS'); and of S.dS'.
+template <class E, int DKP>
+__global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int tiles)
+{
+    constexpr int kP = kPlanes<E>, LD = DKP + 8, kK = DKP / 32;
+    __shared__ u16 Ss[3 * kTile * LD], Rs[3 * kTile * kSteps];
+    __shared__ float dots[kWaves];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const unsigned id = by_xcd(blockIdx.x, gridDim.x);
+    const int tile = (int)(id % tiles), h = (int)(id / tiles % a.heads), b = (int)(id / tiles / a.heads % a.B), c = (int)(id / tiles / a.heads / a.B);
+    const int col = tile * kTile + r, row = 16 * w + 4 * g;
+    const bool live = col < a.Dv;
+    const Block k = block_of(a, c, b, h);
+    if (k.n <= 0) return;
+    const Place<E, DKP, true> at(a);
+    StateTile<DKP> S, dS;
+    S.load(a.states + k.index * a.Dk * a.Dv, a, w, g, col);
+    dS.load(at.dS(k), a, w, g, col);
+    S.publish(Ss, w, r, g);
+    float dot = 0.f, v[4], beta[4], dR[4], found[4];
+#pragma unroll
+    for (int m = 0; m < DKP / 64; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dot = fmaf(S.v[m][i], dS.v[m][i], dot);
+    const f32x4v y = at4(at.y(k) + row);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        beta[i] = beta_at(a, k, row + i);
+        v[i] = live && row + i < k.n ? E::load(row_of<E>(a.v, a.v_t, a.v_b, k.t0 + row + i, b, (int64_t)h * a.Dv + col)) : 0.f;
+        dR[i] = live ? at.dR(k)[(int64_t)(row + i) * a.Dv + col] : 0.f;
+        found[i] = live ? at.found(k)[(int64_t)(row + i) * a.Dv + col] : 0.f;
+    }
+    bf16x8 X[2][3];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) fragment<3>(X[s], at.X(k) + fragment_at(w, 2, s) + 8 * lane, C * C);
+    lds_barrier();
+    Sums ks;
+#pragma unroll
+    for (int s = 0; s < kK; ++s) {
+        bf16x8 f[3], K[kP];
+        fragment<3>(f, Ss + r * LD + 32 * s + 8 * g, kTile * LD);
+        fragment<kP>(K, at.K(k) + fragment_at(w, kK, s) + 8 * lane, C * DKP);
+        multiply(ks, K, f);
+    }
+    const f32x4v read = ks.total();
+    f32x4v R;
+    float db[4], from_front[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float miss = v[i] - y[i] * read[i];
+        R[i] = beta[i] * miss;
+        db[i] = dR[i] * miss;
+        from_front[i] = -y[i] * beta[i] * dR[i] * read[i];
+    }
+    store_split<3>(R, Rs + r * kSteps + row, kTile * kSteps);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) dot += __shfl_xor(dot, off);
+    if (lane == 0) dots[w] = dot;
+    lds_barrier();
+    Sums u;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        if (w < 2 && s == 1) continue;
+        bf16x8 f[3];
+        fragment<3>(f, Rs + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
+        multiply(u, X[s], f);
+    }
+    const f32x4v U = u.total();
+    float* const parts = at.parts(k, tile);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (live) at.U(k)[(int64_t)(row + i) * a.Dv + col] = U[i];
+        const float d = row16_sum(db[i]), f = row16_sum(from_front[i]), l = row16_sum(U[i] * found[i]);
+        if (r == 0) {
+            parts[row + i] = d;
+            parts[C + row + i] = f;
+            parts[2 * C + row + i] = l;
+        }
+    }
+    if (threadIdx.x == 0) parts[3 * C] = dots[0] + dots[1] + dots[2] + dots[3];
+}
+
+// What is left of a block's gradient, from the state S in front of it, dS' behind it, dR and U:
 //
 //     dP = D (scale dO U')     dA = -b D (dR U') below the diagonal      dq = scale y dO S' + dP K
 //     dk = e U dS'' - y b dR S' + dP' Q + (dA + dA') K                   db = dR.(v - y K S) - sum_j dR.U_j D k.k_j
@@ -543,27 +1034,28 @@ __device__ __forceinline__ float row16_shifted(float v) { return dpp_move<0x110 
 //            + sum_{j < t} U.(e K dS')_j + exp(G_last) S.dS'
 //
 // (each decay's own terms; as differences of what reaches two neighbouring G, what a strong decay leaves of dg would be lost).
-// A workgroup takes a block of one sequence and key head and goes through the heads that share it, 16 columns of S at a time.
+// A workgroup takes a block of one sequence and key head and goes through the heads that share it, 32 columns of S at a time, whose planes
+// the waves make together; a wave holds the results of 16 steps.
+constexpr int kWide = 32, kWideRow = kWide + 8;         // columns of a tile, and its row in LDS
+constexpr int kRowsAtOnce = 128;                        // of S and dS' in LDS
 template <class E, int DKP>
-__global__ __launch_bounds__(64 * kWaves) void delta_gradient_kernel(DeltaArgs a)
+__global__ __launch_bounds__(kThreads) void delta_gradient_kernel(DeltaArgs a)
 {
     using T = typename E::T;
     extern __shared__ float lds[];
-    constexpr int LD = DKP + 4, kParts = DKP / 16;
-    // keys (for a while queries) | S and dS', U, R of a tile of columns; in their place later dP and dA
-    float *const Ks = lds, *const Ss = Ks + C * LD, *const Ds = Ss + DKP * kCols, *const Us = Ds + DKP * kCols, *const Rs = Us + C * kCols;
-    float *const Ps = Ss, *const As = Ss + C * kRow;
+    constexpr int kP = kPlanes<E>, kR = kForResult<E>, kParts = DKP / 16, kRows = DKP < kRowsAtOnce ? DKP : kRowsAtOnce;
+    // S (three planes), dS' and U of a tile of columns; in their place later dP and dA
+    u16 *const Ss = (u16*)lds, *const Ds = Ss + 3 * kRows * kWideRow, *const Us = Ds + kR * kRows * kWideRow;
+    float *const Ps = lds, *const As = Ps + C * kRow;
     __shared__ double Gs[C];
-    __shared__ float ys[C], es[C], betas[C], overs[kWaves][C], fronts[C], backs[C], dbs[C], dots[kWaves];
+    __shared__ float ys[C], es[C], betas[C], overs[kWaves][C], fronts[C], dbs[C];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const unsigned id = by_xcd(blockIdx.x, gridDim.x);
     const int c = (int)(id / a.key_heads / a.B), b = (int)(id / a.key_heads % a.B), hk = (int)(id % a.key_heads), group = a.heads / a.key_heads;
     const int64_t t0 = (int64_t)c * C;
     const int n = (int)min((int64_t)length_of(a, b) - t0, (int64_t)C), rows = (int)min((int64_t)a.T - t0, (int64_t)C);
     const int row = 16 * w + 4 * g, mine = 16 * w + r;          // the lane's steps as results, and its step as first operand
-    float* const shared = shared_of(a, ((int64_t)c * a.B + b) * a.key_heads + hk);
-    const T* const k_first = row_of<E>(a.k, a.k_t, a.k_b, t0, b, (int64_t)hk * a.Dk);
-    const T* const q_first = row_of<E>(a.q, a.q_t, a.q_b, t0, b, (int64_t)hk * a.Dk);
+    const Place<E, DKP, true> at(a);
     for (int hh = 0; hh < group; ++hh) {
         const Block k = block_of(a, c, b, hk * group + hh);
         if (n <= 0) {
@@ -573,162 +1065,175 @@ __global__ __launch_bounds__(64 * kWaves) void delta_gradient_kernel(DeltaArgs a
             }
             continue;
         }
-        const float *const ready = prepared_of(a, k.index), *const behind = dstate_of(a, k.index), *const left = dupdate_of(a, k.index);
-        const float* const front = a.states + k.index * a.Dk * a.Dv;
-        stage<E, DKP>(k_first, a.k_t, n, a.Dk, Ks);
+        const float *const behind = at.dS(k), *const left = at.dR(k), *const updates = at.U(k), *const front = a.states + k.index * a.Dk * a.Dv;
         if (w == 0) {
             Gs[lane] = running(a, k, lane);
-            ys[lane] = ready[2 * C * C + lane];
-            es[lane] = ready[2 * C * C + C + lane];
+            ys[lane] = at.y(k)[lane];
+            es[lane] = at.e(k)[lane];
             betas[lane] = beta_at(a, k, lane);
         }
+        Sum dq[kParts], from_dS[kParts], from_dR[kParts], dP[4], dL[4];
+        for (int c0 = 0; c0 < a.Dv; c0 += kWide) {
+            bf16x8 dO[kP], dR[3], U[3];
+            {
+                const int c8 = c0 + 8 * g;
+                const bool has = mine < n;
+                const T* const o_row = row_of<E>(a.dO, a.do_t, a.do_b, t0 + mine, b, (int64_t)k.h * a.Dv);
+                split8<kP>(has ? load4<E>(o_row, c8, a.Dv) : kZero4, has ? load4<E>(o_row, c8 + 4, a.Dv) : kZero4, dO);
+                split8<3>(load4<F32>(left + (int64_t)mine * a.Dv, c8, a.Dv), load4<F32>(left + (int64_t)mine * a.Dv, c8 + 4, a.Dv), dR);
+                split8<3>(load4<F32>(updates + (int64_t)mine * a.Dv, c8, a.Dv), load4<F32>(updates + (int64_t)mine * a.Dv, c8 + 4, a.Dv), U);
+            }
+#pragma unroll
+            for (int d0 = 0; d0 < DKP; d0 += kRows) {
+                __syncthreads();
+                if (d0 == 0)
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) *(bf16x8*)(Us + (i * C + mine) * kWideRow + 8 * g) = U[i];
+#pragma unroll 4
+                for (int p = threadIdx.x; p < kRows * kWide / 4; p += kThreads) {
+                    const int d = p / (kWide / 4), from = p % (kWide / 4) * 4;
+                    const bool there = d0 + d < a.Dk;
+                    store_split<3>(there ? load4<F32>(front + (int64_t)(d0 + d) * a.Dv, c0 + from, a.Dv) : kZero4, Ss + d * kWideRow + from, kRows * kWideRow);
+                    store_split<kR>(there ? load4<F32>(behind + (int64_t)(d0 + d) * a.Dv, c0 + from, a.Dv) : kZero4, Ds + d * kWideRow + from, kRows * kWideRow);
+                }
+                __syncthreads();
+                bf16x8 Ur[kR], Rr[kR];
+#pragma unroll
+                for (int i = 0; i < kR; ++i) {
+                    Ur[i] = U[i];
+                    Rr[i] = dR[i];
+                }
+#pragma unroll
+                for (int m = 0; m < kRows / 16; ++m) {
+                    bf16x8 s[3], ds[kR], sr[kR];
+                    fragment<3>(s, Ss + (16 * m + r) * kWideRow + 8 * g, kRows * kWideRow);
+                    fragment<kR>(ds, Ds + (16 * m + r) * kWideRow + 8 * g, kRows * kWideRow);
+#pragma unroll
+                    for (int i = 0; i < kR; ++i) sr[i] = s[i];
+                    multiply(dq[d0 / 16 + m], dO, s);
+                    multiply(from_dR[d0 / 16 + m], Rr, sr);
+                    multiply(from_dS[d0 / 16 + m], Ur, ds);
+                }
+                if (d0 == 0)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (j > w) continue;
+                        bf16x8 u[3];
+                        fragment<3>(u, Us + (16 * j + r) * kWideRow + 8 * g, C * kWideRow);
+                        multiply(dP[j], dO, u);
+                        multiply(dL[j], dR, u);
+                    }
+            }
+        }
         __syncthreads();
-        f32x4v dP[4], dL[4], y, beta;
-        f32x4v dq[kParts], dk[kParts];
-#pragma unroll
-        for (int m = 0; m < kParts; ++m) dq[m] = dk[m] = kZero4;
-        float db[4], from_front[4], to_back[4], dot = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) dP[j] = dL[j] = kZero4;
+        f32x4v dq_sum[kParts], dk_sum[kParts], y, beta;
+        float from_front[4], db[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             y[i] = ys[row + i];
             beta[i] = betas[row + i];
-            db[i] = from_front[i] = to_back[i] = 0.f;
+            from_front[i] = db[i] = 0.f;
         }
-        const float y_mine = ys[mine], e_mine = es[mine], yb_mine = -y_mine * betas[mine];
-        for (int c0 = 0; c0 < a.Dv; c0 += kTile) {
-            __syncthreads();
-#pragma unroll
-            for (int p = threadIdx.x; p < DKP * 4; p += 64 * kWaves) {
-                const int d = p / 4, at = c0 + p % 4 * 4;
-                const f32x4v s = d < a.Dk ? load4<F32>(front + (int64_t)d * a.Dv, at, a.Dv) : kZero4;
-                const f32x4v ds = d < a.Dk ? load4<F32>(behind + (int64_t)d * a.Dv, at, a.Dv) : kZero4;
-                *(f32x4v*)(Ss + d * kCols + p % 4 * 4) = s;
-                *(f32x4v*)(Ds + d * kCols + p % 4 * 4) = ds;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) dot = fmaf(s[i], ds[i], dot);
-            }
-            const int col = c0 + r;
-            float v[4], dR[4], found[4];
+        // what the tiles of columns have added: lane 16 g + i of the wave the tiles i, i + 16, .. of its four steps
+        float to_back[4] = {}, dot = 0.f;
+        for (int tile = r; tile < at.tiles(); tile += 16) {
+            const float* const parts = at.parts(k, tile);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool there = col < a.Dv && row + i < n;
-                v[i] = there ? E::load(row_of<E>(a.v, a.v_t, a.v_b, t0 + row + i, b, (int64_t)k.h * a.Dv + col)) : 0.f;
-                dR[i] = there ? left[(int64_t)(row + i) * a.Dv + col] : 0.f;
-                found[i] = there ? left[(int64_t)(C + row + i) * a.Dv + col] : 0.f;
+                db[i] += parts[row + i];
+                from_front[i] += parts[C + row + i];
+                to_back[i] += parts[2 * C + row + i];
             }
-            const bool has = mine < n;
-            const f32x4v dO_mine = has ? scaled4(load4<E>(row_of<E>(a.dO, a.do_t, a.do_b, t0 + mine, b, (int64_t)k.h * a.Dv), c0 + 4 * g, a.Dv), a.scale) : kZero4;
-            const f32x4v dR_mine = has ? load4<F32>(left + (int64_t)mine * a.Dv, c0 + 4 * g, a.Dv) : kZero4;
-            __syncthreads();
-            f32x4v ks = kZero4;
-#pragma unroll 4
-            for (int d = 0; d < DKP; d += 16) ks = mfma16(at4(Ks + mine * LD + d + 4 * g), down4(Ss + (d + 4 * g) * kCols + r, kCols), ks);
-            f32x4v R;
+            dot += parts[3 * C];
+        }
+        const u16* const Q = at.Q(k);
+#pragma unroll
+        for (int m = 0; m < kParts; ++m) {
+            const f32x4v q4 = dq[m].total(), s4 = from_dS[m].total(), r4 = from_dR[m].total();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float miss = v[i] - y[i] * ks[i];
-                R[i] = beta[i] * miss;
-                db[i] = fmaf(dR[i], miss, db[i]);
-                from_front[i] = fmaf(-y[i] * beta[i] * dR[i], ks[i], from_front[i]);
-            }
-            *(f32x4v*)(Rs + r * kRow + row) = R;
-            __syncthreads();
-            f32x4v U = kZero4;
-            for (int j = 0; j <= w; ++j) U = mfma16(at4(ready + mine * C + 16 * j + 4 * g), at4(Rs + r * kRow + 16 * j + 4 * g), U);
+                float q = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                Us[(row + i) * kCols + r] = U[i];
-                to_back[i] = fmaf(U[i], found[i], to_back[i]);
+                for (int p = kP - 1; p >= 0; --p) q += __uint_as_float((uint32_t)Q[p * C * DKP + fragment_at(w, DKP / 32, m / 2) + 8 * (4 * g + i + 16 * (m % 2 * 2 + r / 8)) + r % 8] << 16);
+                dq_sum[m][i] = a.scale * y[i] * q4[i];
+                dk_sum[m][i] = es[row + i] * s4[i] - y[i] * beta[i] * r4[i];
+                from_front[i] = fmaf(q, dq_sum[m][i], from_front[i]);
             }
-            __syncthreads();
-            const f32x4v yO = scaled4(dO_mine, y_mine), eU = scaled4(at4(Us + mine * kCols + 4 * g), e_mine), Z = scaled4(dR_mine, yb_mine);
+        }
+        Sum kk[4], qk[4];
+        const u16* const K = at.K(k);
 #pragma unroll
-            for (int m = 0; m < kParts; ++m) {
-                const f32x4v s = at4(Ss + (16 * m + r) * kCols + 4 * g);
-                dq[m] = mfma16(yO, s, dq[m]);
-                dk[m] = mfma16(Z, s, dk[m]);
-                dk[m] = mfma16(eU, at4(Ds + (16 * m + r) * kCols + 4 * g), dk[m]);
-            }
+        for (int d = 0; d < DKP; d += 32) {
+            bf16x8 ka[kP], qa[kP];
+            fragment<kP>(ka, K + fragment_at(w, DKP / 32, d / 32) + 8 * lane, C * DKP);
+            fragment<kP>(qa, Q + fragment_at(w, DKP / 32, d / 32) + 8 * lane, C * DKP);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (j > w) continue;
-                const f32x4v u = at4(Us + (16 * j + r) * kCols + 4 * g);
-                dP[j] = mfma16(dO_mine, u, dP[j]);
-                dL[j] = mfma16(dR_mine, u, dL[j]);
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int m = 0; m < kParts; ++m) {
-                const int d = 16 * m + r;
-                const float q = row + i < n && d < a.Dk ? E::load(q_first + (row + i) * a.q_t + d) : 0.f;
-                from_front[i] = fmaf(q, dq[m][i], from_front[i]);
-            }
-        f32x4v kk[4], qk[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) kk[j] = qk[j] = kZero4;
-#pragma unroll 2
-        for (int d = 0; d < DKP; d += 16) {
-            const f32x4v ka = at4(Ks + mine * LD + d + 4 * g), qa = mine < n ? load4<E>(q_first + mine * a.q_t, d + 4 * g, a.Dk) : kZero4;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (j > w) continue;
-                const f32x4v kb = at4(Ks + (16 * j + r) * LD + d + 4 * g);
-                kk[j] = mfma16(ka, kb, kk[j]);
-                qk[j] = mfma16(qa, kb, qk[j]);
+                bf16x8 kb[kP];
+                fragment<kP>(kb, K + fragment_at(j, DKP / 32, d / 32) + 8 * lane, C * DKP);
+                multiply(kk[j], ka, kb);
+                multiply(qk[j], qa, kb);
             }
         }
         float in_front[4] = {};     // pairs of the lane's steps with all steps of the tiles in front of this one
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            const f32x4v kk4 = kk[j].total(), qk4 = qk[j].total(), dP4 = dP[j].total(), dL4 = dL[j].total();
             float over = 0.f;       // pairs that the decay at step 16 j + r lies between, of the lane's steps
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int at = row + i, other = 16 * j + r;
+                const int own = row + i, other = 16 * j + r;
                 float p = 0.f, l = 0.f, pair = 0.f;
-                if (j <= w && other <= at && at < n) {
-                    const float decay = expf((float)(Gs[at] - Gs[other]));
-                    p = decay * dP[j][i];
-                    if (other < at) {
-                        l = decay * dL[j][i];
-                        db[i] = fmaf(-l, kk[j][i], db[i]);
+                if (j <= w && other <= own && own < n) {
+                    const float decay = expf((float)(Gs[own] - Gs[other]));
+                    p = a.scale * decay * dP4[i];
+                    if (other < own) {
+                        l = decay * dL4[i];
+                        db[i] = fmaf(-l, kk4[i], db[i]);
                         l *= -beta[i];
-                        pair = fmaf(l, kk[j][i], p * qk[j][i]);
+                        pair = fmaf(l, kk4[i], p * qk4[i]);
                     }
                 }
-                if (j <= w) {
-                    Ps[at * kRow + other] = p;
-                    As[at * kRow + other] = l;
-                }
+                Ps[own * kRow + other] = p;
+                As[own * kRow + other] = l;
                 // over the steps in front of 16 j + r: the 16 of the tile by shifts along the row of lanes
                 float sum = row16_shifted<1>(pair);
                 sum += row16_shifted<1>(sum);
                 sum += row16_shifted<2>(sum);
                 sum += row16_shifted<4>(sum);
                 sum += row16_shifted<8>(sum);
-                if (other <= at) over += in_front[i] + sum;
+                if (other <= own) over += in_front[i] + sum;
                 in_front[i] += row16_sum(pair);
             }
             over += __shfl_xor(over, 16);
             over += __shfl_xor(over, 32);
             if (g == 0) overs[w][16 * j + r] = over;
         }
+        dot = row16_sum(dot);
+        float* const backs = ys;        // which everybody has read
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float f = row16_sum(from_front[i]), l = row16_sum(to_back[i]), d = row16_sum(db[i]);
             if (r == 0) {
                 fronts[row + i] = f;
-                backs[row + i] = l;
                 dbs[row + i] = d;
             }
+            to_back[i] = l;
         }
+        const float last = at.y(k)[C - 1];
+        __syncthreads();
+        if (r == 0)
 #pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) dot += __shfl_xor(dot, off);
-        if (lane == 0) dots[w] = dot;
+            for (int i = 0; i < 4; ++i) backs[row + i] = to_back[i];
+        bf16x8 both[2][kR], dPa[2][kR], dPt[2][kR];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int from = 32 * s + 8 * g;
+            split8<kR>(at4(As + mine * kRow + from) + down4(As + from * kRow + mine, kRow), at4(As + mine * kRow + from + 4) + down4(As + (from + 4) * kRow + mine, kRow), both[s]);
+            split8<kR>(at4(Ps + mine * kRow + from), at4(Ps + mine * kRow + from + 4), dPa[s]);
+            split8<kR>(down4(Ps + from * kRow + mine, kRow), down4(Ps + (from + 4) * kRow + mine, kRow), dPt[s]);
+        }
         __syncthreads();
         if (w == 0) {
             double from = fronts[lane], to = backs[lane], dg = (double)overs[0][lane] + overs[1][lane] + overs[2][lane] + overs[3][lane];
@@ -739,43 +1244,33 @@ __global__ __launch_bounds__(64 * kWaves) void delta_gradient_kernel(DeltaArgs a
                 if (lane >= off) to += before;
             }
             to = __shfl_up(to, 1);
-            dg += from + (lane > 0 ? to : 0.0) + (double)ys[C - 1] * ((double)dots[0] + dots[1] + dots[2] + dots[3]);
+            dg += from + (lane > 0 ? to : 0.0) + (double)last * dot;
             if (lane < rows) {
                 if (a.dg) *(float*)row_of<F32>(a.dg, a.dg_t, a.dg_b, t0 + lane, b, k.h) = lane < n ? (float)dg : 0.f;
                 *(float*)row_of<F32>(a.dbeta, a.dbeta_t, a.dbeta_b, t0 + lane, b, k.h) = lane < n ? dbs[lane] : 0.f;
             }
         }
-        f32x4v both[4];
+        const u16 *const KT = at.KT(k), *const QT = at.QT(k);
+        float* const shared = at.shared(k);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            both[j] = kZero4;
-            if (j <= w) both[j] += at4(As + mine * kRow + 16 * j + 4 * g);
-            if (j >= w) both[j] += down4(As + (16 * j + 4 * g) * kRow + mine, kRow);
-        }
-#pragma unroll 2
-        for (int m = 0; m < kParts; ++m)
+        for (int m = 0; m < kParts; ++m) {
+            Sum sq, sk;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f32x4v kb = down4(Ks + (16 * j + 4 * g) * LD + 16 * m + r, LD);
-                if (j <= w) dq[m] = mfma16(at4(Ps + mine * kRow + 16 * j + 4 * g), kb, dq[m]);
-                dk[m] = mfma16(both[j], kb, dk[m]);
+            for (int s = 0; s < 2; ++s) {
+                bf16x8 kt[kP], qt[kP];
+                fragment<kP>(kt, KT + fragment_at(m, 2, s) + 8 * lane, C * DKP);
+                fragment<kP>(qt, QT + fragment_at(m, 2, s) + 8 * lane, C * DKP);
+                multiply(sq, dPa[s], kt);
+                multiply(sk, both[s], kt);
+                multiply(sk, dPt[s], qt);
             }
-        __syncthreads();
-        stage<E, DKP>(q_first, a.q_t, n, a.Dk, Ks);
-        __syncthreads();
-#pragma unroll 2
-        for (int m = 0; m < kParts; ++m)
-            for (int j = w; j < 4; ++j)
-                dk[m] = mfma16(down4(Ps + (16 * j + 4 * g) * kRow + mine, kRow), down4(Ks + (16 * j + 4 * g) * LD + 16 * m + r, LD), dk[m]);
-        __syncthreads();
-#pragma unroll
-        for (int m = 0; m < kParts; ++m)
+            const int d = 16 * m + r;
+            const f32x4v q4 = dq_sum[m] + sq.total(), k4 = dk_sum[m] + sk.total();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int d = 16 * m + r;
                 if (d >= a.Dk || row + i >= rows) continue;
                 float* const part = shared + (row + i) * a.Dk + d;
-                float vq = row + i < n ? dq[m][i] : 0.f, vk = row + i < n ? dk[m][i] : 0.f;
+                float vq = row + i < n ? q4[i] : 0.f, vk = row + i < n ? k4[i] : 0.f;
                 if (hh > 0) {
                     vq += part[0];
                     vk += part[C * a.Dk];
@@ -788,9 +1283,11 @@ __global__ __launch_bounds__(64 * kWaves) void delta_gradient_kernel(DeltaArgs a
                     E::store((T*)row_of<E>(a.dk, a.dk_t, a.dk_b, t0 + row + i, b, (int64_t)hk * a.Dk + d), vk);
                 }
             }
+        }
+        __syncthreads();
     }
     if (n > 0) return;
-    for (int p = threadIdx.x; p < rows * a.Dk; p += 64 * kWaves) {
+    for (int p = threadIdx.x; p < rows * a.Dk; p += kThreads) {
         E::store((T*)row_of<E>(a.dq, a.dq_t, a.dq_b, t0 + p / a.Dk, b, (int64_t)hk * a.Dk + p % a.Dk), 0.f);
         E::store((T*)row_of<E>(a.dk, a.dk_t, a.dk_b, t0 + p / a.Dk, b, (int64_t)hk * a.Dk + p % a.Dk), 0.f);
     }
@@ -802,29 +1299,15 @@ constexpr int kFewSteps = 8;
 
 int64_t blocks(int T) { return (T + C - 1) / C; }
 
-template <class Kernel>
-hipError_t launch(Kernel kernel, int64_t grid, size_t lds_floats, const DeltaArgs& a, int tiles, hipStream_t s)
-{
-    const size_t lds = lds_floats * sizeof(float);
-    const hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWaves), lds, s, a, tiles);
-    return hipGetLastError();
-}
-template <class Kernel>
-hipError_t launch(Kernel kernel, int64_t grid, size_t lds_floats, const DeltaArgs& a, hipStream_t s)
-{
-    const size_t lds = lds_floats * sizeof(float);
-    const hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWaves), lds, s, a);
-    return hipGetLastError();
-}
-
-template <class E, int DKP>
+template <class E, int DKP, bool BACK>
 hipError_t prepare(const DeltaArgs& a, hipStream_t s)
 {
-    return launch(delta_prepare_kernel<E, DKP>, blocks(a.T) * a.B * a.heads, 2 * C * (DKP + 4), a, s);
+    const size_t lds = std::max<size_t>(2 * C * kStaged<E, DKP> * E::kBytes, 3 * C * kRow * sizeof(float));
+    const auto kernel = delta_prepare_kernel<E, DKP, BACK>;
+    const hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks(a.T) * a.B * a.heads)), dim3(kThreads), lds, s, a);
+    return hipGetLastError();
 }
 
 template <class E, int DKP>
@@ -835,38 +1318,59 @@ hipError_t forward(const DeltaArgs& a, hipStream_t s)
         hipLaunchKernelGGL((delta_step_kernel<E, DKP / 32>), dim3((unsigned)((int64_t)a.B * a.heads * tiles)), dim3(256), 0, s, a, tiles);
         return hipGetLastError();
     }
-    const hipError_t e = prepare<E, DKP>(a, s);
+    const hipError_t e = prepare<E, DKP, false>(a, s);
     if (e != hipSuccess) return e;
     const int tiles = (a.Dv + kTile - 1) / kTile;
-    return launch(delta_walk_kernel<E, DKP>, (int64_t)a.B * a.heads * tiles, (C + kTile) * (DKP + 4) + 3 * kTile * kRow, a, tiles, s);
+    const dim3 grid((unsigned)((int64_t)a.B * a.heads * tiles)), block(kThreads);
+    if (a.states) hipLaunchKernelGGL((delta_walk_kernel<E, DKP, true>), grid, block, 0, s, a, tiles);
+    else hipLaunchKernelGGL((delta_walk_kernel<E, DKP, false>), grid, block, 0, s, a, tiles);
+    return hipGetLastError();
 }
 
 template <class E, int DKP>
 hipError_t backward(const DeltaArgs& a, hipStream_t s)
 {
-    hipError_t e = a.T > 0 ? prepare<E, DKP>(a, s) : hipSuccess;
+    hipError_t e = a.T > 0 ? prepare<E, DKP, true>(a, s) : hipSuccess;
     if (e != hipSuccess) return e;
     const int tiles = (a.Dv + kTile - 1) / kTile;
-    e = launch(delta_walk_back_kernel<E, DKP>, (int64_t)a.B * a.heads * tiles, (2 * C + kTile) * (DKP + 4) + 3 * kTile * kRow, a, tiles, s);
-    if (e != hipSuccess || a.T == 0) return e;
-    const size_t tile = 2 * DKP * kCols + C * kCols + kTile * kRow;
-    return launch(delta_gradient_kernel<E, DKP>, blocks(a.T) * a.B * a.key_heads, C * (DKP + 4) + std::max<size_t>(tile, 2 * C * kRow), a, s);
+    hipLaunchKernelGGL((delta_walk_back_kernel<E, DKP>), dim3((unsigned)((int64_t)a.B * a.heads * tiles)), dim3(kThreads), 0, s, a, tiles);
+    if (a.T == 0) return hipGetLastError();
+    hipLaunchKernelGGL((delta_update_kernel<E, DKP>), dim3((unsigned)(blocks(a.T) * a.B * a.heads * tiles)), dim3(kThreads), 0, s, a, tiles);
+    constexpr int kRows = DKP < kRowsAtOnce ? DKP : kRowsAtOnce;
+    const size_t lds = std::max<size_t>(((3 + kForResult<E>)*kRows + 3 * C) * kWideRow * sizeof(u16), 2 * C * kRow * sizeof(float));
+    const auto kernel = delta_gradient_kernel<E, DKP>;
+    e = allow_dynamic_lds((const void*)kernel, lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks(a.T) * a.B * a.key_heads)), dim3(kThreads), lds, s, a);
+    return hipGetLastError();
+}
+
+template <class E, int DKP>
+size_t bytes_of(const DeltaArgs& a, bool back)
+{
+    return back ? Place<E, DKP, true>(a).bytes() : a.T <= kFewSteps ? 0 : Place<E, DKP, false>(a).bytes();
+}
+template <class E>
+size_t bytes_by_width(const DeltaArgs& a, bool back)
+{
+    return a.Dk <= 64 ? bytes_of<E, 64>(a, back) : a.Dk <= 128 ? bytes_of<E, 128>(a, back) : bytes_of<E, 256>(a, back);
 }
 
 }  // namespace
 
+// what either type asks for
 size_t delta_workspace_bytes(int T, int B, int heads, int key_heads, int Dk, int Dv, bool back)
 {
-    const size_t each = back ? kPrepared + (size_t)(Dk + 2 * C) * Dv : T <= kFewSteps ? 0 : kPrepared;
-    const size_t shared = back && heads > key_heads ? (size_t)key_heads * 2 * C * Dk : 0;
-    return std::max<size_t>(256, (size_t)blocks(T) * B * (heads * each + shared) * sizeof(float));
+    DeltaArgs a = {};
+    a.T = T; a.B = B; a.heads = heads; a.key_heads = key_heads; a.Dk = Dk; a.Dv = Dv;
+    return std::max<size_t>(256, std::max(bytes_by_width<F32>(a, back), bytes_by_width<Bf16>(a, back)));
 }
 
-// a grid's threads have to stay under 2^32, and what the workspace needs under 2^60
+// a grid's threads have to stay under 2^32
 bool delta_fits(int T, int B, int heads, int Dk, int Dv)
 {
     const int64_t of_state = (int64_t)B * heads * ((Dv + kTile - 1) / kTile);
-    return (int64_t)B * heads < (1 << 24) && of_state < (1 << 24) && blocks(T) * B * heads < (1 << 24);
+    return (int64_t)B * heads < (1 << 24) && of_state < (1 << 24) && blocks(T) * of_state < (1 << 24);
 }
 
 template <class E>
