@@ -557,15 +557,16 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
         beta.place(row, 0, a.beta_t, rest);
         const auto load_keys = [&](int c) {
 #pragma unroll
-            for (int s = 0; s < kK; ++s) {
-                fragment<kP>(K[s], K0 + fragment_at(0, kK, s) + mine, C * DKP);
-                fragment<kP>(Q[s], Q0 + fragment_at(0, kK, s) + mine, C * DKP);
-            }
+            for (int s = 0; s < kK; ++s) fragment<kP>(K[s], K0 + fragment_at(0, kK, s) + mine, C * DKP);
+            v.load(v0, c == blocks - 1);
+            beta.load(beta0, c == blocks - 1);
+        };
+        const auto load_queries = [&]() {
+#pragma unroll
+            for (int s = 0; s < kK; ++s) fragment<kP>(Q[s], Q0 + fragment_at(0, kK, s) + mine, C * DKP);
             y = at4(y0 + row);
             e = at4(y0 + C + row);
             last = y0[C - 1];
-            v.load(v0, c == blocks - 1);
-            beta.load(beta0, c == blocks - 1);
         };
         const auto load_inverse = [&]() {
 #pragma unroll
@@ -597,6 +598,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
             for (int i = 0; i < 4; ++i) E::store(live && c >= 0 && row + i < n ? to + o_at[i] : (T*)sink, O[i]);
         };
         load_keys(0);
+        load_queries();
         load_inverse();
         load_columns();
         load_pairs();
@@ -614,6 +616,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
 #pragma unroll
             for (int s = 0; s < kK; ++s) multiply(ks, K[s], f[s]);
             const int n = len - c * C;
+            const bool more = c + 1 < blocks;
             const f32x4v b4 = beta.take(row, n), v4 = v.take(row, n), found = ks.total(), decay = e, y4 = y;
             const float decayed = last;
             f32x4v R;
@@ -622,6 +625,13 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
             store_split<3>(R, Rs + r * kSteps + row, kTile * kSteps);
             finish(c - 1);                      // in front of the first block of nothing, to nowhere
             lds_barrier();
+            // of the next block what this one has done with, each as soon as that is so
+            K0 += more ? keys_step : 0;
+            v0 += more ? C * a.v_t : 0;
+            beta0 += more ? C * a.beta_t : 0;
+            load_keys(more ? c + 1 : c);
+            load_pairs();                       // of this block: taken behind the next one's first barrier
+            P0 += more ? head_step : 0;
             bf16x8 rf[2][3];
 #pragma unroll
             for (int s = 0; s < 2; ++s) fragment<3>(rf[s], Rs + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
@@ -645,17 +655,11 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
 #pragma unroll
             for (int s = 0; s < 2; ++s) fragment<3>(ef[s], Es + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
             store_split<kR>(U, Us + r * kSteps + row, kTile * kSteps);
-            const bool more = c + 1 < blocks;
-            K0 += more ? keys_step : 0;
             Q0 += more ? keys_step : 0;
             X0 += more ? head_step : 0;
             y0 += more ? head_step / 2 : 0;
-            v0 += more ? C * a.v_t : 0;
-            beta0 += more ? C * a.beta_t : 0;
-            load_keys(more ? c + 1 : c);
+            load_queries();
             load_inverse();
-            load_pairs();                       // of this block: used behind the next barrier
-            P0 += more ? head_step : 0;
 #pragma unroll
             for (int m = 0; m < kParts; ++m) {
                 Sum sum;
