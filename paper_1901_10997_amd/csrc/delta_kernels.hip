@@ -159,6 +159,32 @@ __device__ __forceinline__ f32x4v load4(const typename E::T* row, int col, int w
     return (f32x4v){v[0], v[1], v[2], v[3]};
 }
 
+// The same without a branch, so that loads that follow each other are under way together.  WHOLE: width is a multiple of 4, and four
+// columns move at once; else one by one, those behind the row standing for its last.
+template <class E, bool WHOLE>
+__device__ __forceinline__ f32x4v fetch4(const typename E::T* row, int col, int width)
+{
+    float v[4];
+    if constexpr (WHOLE) {
+        load_n<E, 4, true>(row + min(col, width - 4), v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = col < width ? v[i] : 0.f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = E::load(row + min(col + i, width - 1));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = col + i < width ? v[i] : 0.f;
+    }
+    return (f32x4v){v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ f32x4v if4(bool c, f32x4v v) { return (f32x4v){c ? v[0] : 0.f, c ? v[1] : 0.f, c ? v[2] : 0.f, c ? v[3] : 0.f}; }
+// columns col .. col + 3 of a row of the workspace, which is padded; those behind `width` are 0 whatever stands there
+__device__ __forceinline__ f32x4v padded4(const float* row, int col, int width)
+{
+    const f32x4v v = at4(row + col);
+    return (f32x4v){col < width ? v[0] : 0.f, col + 1 < width ? v[1] : 0.f, col + 2 < width ? v[2] : 0.f, col + 3 < width ? v[3] : 0.f};
+}
+
 // Where a workgroup is: block c of sequence b and head h, `n` steps of it inside the sequence
 struct Block {
     int c, b, h, n;
@@ -216,12 +242,13 @@ struct Place {
     __device__ float* e(const Block& k) const { return y(k) + C; }
     __host__ __device__ int64_t first_floats() const { return (key_blocks * kKeys + head_blocks * kHead) / 2; }
     __device__ float* floats() const { return a.ws + first_floats(); }
-    __device__ float* dS(const Block& k) const { return floats() + k.index * a.Dk * a.Dv; }
-    __host__ __device__ int64_t of_dS() const { return head_blocks * a.Dk * a.Dv; }
-    __device__ float* dR(const Block& k) const { return floats() + of_dS() + k.index * 3 * C * a.Dv; }
-    __device__ float* found(const Block& k) const { return dR(k) + C * a.Dv; }
-    __device__ float* U(const Block& k) const { return found(k) + C * a.Dv; }
-    __host__ __device__ int64_t to_parts() const { return of_dS() + head_blocks * 3 * C * a.Dv; }
+    __host__ __device__ int row() const { return (a.Dv + 31) / 32 * 32; }       // of the fp32 matrices
+    __device__ float* dS(const Block& k) const { return floats() + k.index * a.Dk * row(); }
+    __host__ __device__ int64_t of_dS() const { return head_blocks * a.Dk * row(); }
+    __device__ float* dR(const Block& k) const { return floats() + of_dS() + k.index * 3 * C * row(); }
+    __device__ float* found(const Block& k) const { return dR(k) + C * row(); }
+    __device__ float* U(const Block& k) const { return found(k) + C * row(); }
+    __host__ __device__ int64_t to_parts() const { return of_dS() + head_blocks * 3 * C * row(); }
     __device__ float* parts(const Block& k, int tile) const { return floats() + to_parts() + (k.index * tiles() + tile) * kParts; }
     __host__ __device__ int64_t to_shared() const { return to_parts() + head_blocks * tiles() * kParts; }
     __device__ float* shared(const Block& k) const
@@ -278,14 +305,14 @@ __device__ __forceinline__ f32x4v down4(const float* p, int ld) { return (f32x4v
 // Rows of keys or queries in LDS as they come: bf16 in rows of DKP + 8, fp32 in rows of DKP + 4; 0 behind the end and behind the row
 template <class E, int DKP>
 constexpr int kStaged = E::kBytes == 2 ? DKP + 8 : DKP + 4;
-template <class E, int DKP>
+template <class E, int DKP, bool WHOLE>
 __device__ __forceinline__ void stage(const typename E::T* first, int64_t t_stride, int n, int width, typename E::T* to)
 {
     constexpr int kPieces = DKP / 4;
-#pragma unroll 4
+#pragma unroll 8
     for (int p = threadIdx.x; p < C * kPieces; p += kThreads) {
         const int row = p / kPieces, col = p % kPieces * 4;
-        const f32x4v v = row < n ? load4<E>(first + row * t_stride, col, width) : kZero4;
+        const f32x4v v = if4(row < n, fetch4<E, WHOLE>(first + min(row, n - 1) * t_stride, col, width));
         const float f[4] = {v[0], v[1], v[2], v[3]};
         store_n<E, 4>(to + row * kStaged<E, DKP> + col, f);
     }
@@ -334,7 +361,7 @@ __device__ __forceinline__ void write_square(const float* from, u16* to)
 
 // X, P, y and e of every block, and the planes of keys and queries.  X is built of blocks of 16: those on the diagonal by substitution, a
 // column to a lane; then X_ij = -X_ii sum_k L_ik X_kj, those one off the diagonal first.
-template <class E, int DKP, bool BACK>
+template <class E, int DKP, bool BACK, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a)
 {
     using T = typename E::T;
@@ -349,8 +376,8 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a)
     if (k.n <= 0) return;
     const Place<E, DKP, BACK> at(a);
     const int group = a.heads / a.key_heads, hk = k.h / group;
-    stage<E, DKP>(row_of<E>(a.k, a.k_t, a.k_b, k.t0, k.b, (int64_t)hk * a.Dk), a.k_t, k.n, a.Dk, Ks);
-    stage<E, DKP>(row_of<E>(a.q, a.q_t, a.q_b, k.t0, k.b, (int64_t)hk * a.Dk), a.q_t, k.n, a.Dk, Qs);
+    stage<E, DKP, WHOLE>(row_of<E>(a.k, a.k_t, a.k_b, k.t0, k.b, (int64_t)hk * a.Dk), a.k_t, k.n, a.Dk, Ks);
+    stage<E, DKP, WHOLE>(row_of<E>(a.q, a.q_t, a.q_b, k.t0, k.b, (int64_t)hk * a.Dk), a.q_t, k.n, a.Dk, Qs);
     if (w == 0) {
         const double G = running(a, k, lane);
         Gs[lane] = G;
@@ -445,15 +472,20 @@ template <int DKP>
 struct StateTile {
     static constexpr int kParts = DKP / 64, LD = DKP + 8;
     f32x4v v[kParts];
-    __device__ __forceinline__ void load(const float* from, const DeltaArgs& a, int w, int g, int col)
+    // of rows of `ld`, without a branch between the loads
+    __device__ __forceinline__ void load(const float* from, int ld, const DeltaArgs& a, int w, int g, int col)
     {
+#pragma unroll
+        for (int m = 0; m < kParts; ++m) v[m] = kZero4;
+        if (!from) return;
 #pragma unroll
         for (int m = 0; m < kParts; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = 16 * (w * kParts + m) + 4 * g + i;
-                v[m][i] = from && col < a.Dv && d < a.Dk ? from[(int64_t)d * a.Dv + col] : 0.f;
-            }
+            for (int i = 0; i < 4; ++i) v[m][i] = from[(int64_t)min(16 * (w * kParts + m) + 4 * g + i, a.Dk - 1) * ld + min(col, a.Dv - 1)];
+#pragma unroll
+        for (int m = 0; m < kParts; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[m][i] = col < a.Dv && 16 * (w * kParts + m) + 4 * g + i < a.Dk ? v[m][i] : 0.f;
     }
     __device__ __forceinline__ void store(float* to, const DeltaArgs& a, int w, int g, int col) const
     {
@@ -466,14 +498,14 @@ struct StateTile {
             }
     }
     // without a branch: what the tile has more than the state goes to `sink`
-    __device__ __forceinline__ void store_all(float* to, float* sink, const DeltaArgs& a, int w, int g, int col) const
+    __device__ __forceinline__ void store_all(float* to, int ld, float* sink, const DeltaArgs& a, int w, int g, int col) const
     {
 #pragma unroll
         for (int m = 0; m < kParts; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int d = 16 * (w * kParts + m) + 4 * g + i;
-                float* const p = col < a.Dv && d < a.Dk ? to + (int64_t)d * a.Dv + col : sink;
+                float* const p = col < a.Dv && d < a.Dk ? to + d * ld + col : sink;
                 *p = v[m][i];
             }
     }
@@ -533,7 +565,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
     const int64_t state = ((int64_t)b * a.heads + h) * a.Dk * a.Dv, states_step = (int64_t)a.B * a.heads * a.Dk * a.Dv;
     const Place<E, DKP, false> at(a);
     StateTile<DKP> S;
-    S.load(a.S0 ? a.S0 + state : nullptr, a, w, g, col);
+    S.load(a.S0 ? a.S0 + state : nullptr, a.Dv, a, w, g, col);
     if (blocks > 0) {
         // addresses: the same for all lanes, and a lane's own 32 bits
         const Block first = {0, b, h, 0, 0, (int64_t)b * a.heads + h};
@@ -607,7 +639,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
         // eight instructions that lie between them elsewhere), and half of a result was what stood there before.
 #pragma unroll 1
         for (int c = 0; c < blocks; ++c) {
-            if constexpr (STATES) S.store_all(a.states + c * states_step + state, sink, a, w, g, col);
+            if constexpr (STATES) S.store_all(a.states + c * states_step + state, a.Dv, sink, a, w, g, col);
             lds_barrier();
             Sum ks, qs, u;
             bf16x8 f[kK][3];
@@ -784,7 +816,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
     const int64_t state = ((int64_t)b * a.heads + h) * a.Dk * a.Dv;
     const Place<E, DKP, true> at(a);
     StateTile<DKP> dS;
-    dS.load(a.dST ? a.dST + state : nullptr, a, w, g, col);
+    dS.load(a.dST ? a.dST + state : nullptr, a.Dv, a, w, g, col);
     if (blocks > 0) {
         const Block behind = {blocks - 1, b, h, 0, 0, ((int64_t)(blocks - 1) * a.B + b) * a.heads + h};
         const int64_t keys_step = (int64_t)a.B * a.key_heads * at.kKeys, head_step = (int64_t)a.B * a.heads * at.kHead;
@@ -797,6 +829,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
         T* const dv0 = (T*)row_of<E>(a.dv, a.dv_t, a.dv_b, 0, b, (int64_t)h * a.Dv);
         const int64_t dv_at[4] = {row * a.dv_t + col, (row + 1) * a.dv_t + col, (row + 2) * a.dv_t + col, (row + 3) * a.dv_t + col};
         float* const sink = at.sink() + lane;
+        const int ld = at.row();
         bf16x8 K[kK][kP], PT[2][3], XT[2][3], KT[kParts][2][kP], QT[kParts][2][kP];
         f32x4v y, e, dO, b4;
         FourSteps<E> raw;
@@ -859,7 +892,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
             const int n = len - c * C;
             Block k = behind;
             k.index = ((int64_t)c * a.B + b) * a.heads + h;
-            dS.store_all(at.dS(k), sink, a, w, g, col);
+            dS.store_all(at.dS(k), ld, sink, a, w, g, col);
             const f32x4v dO4 = dO, beta4 = b4;
             const bool more = c > 0;
             lds_barrier();
@@ -917,12 +950,11 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
                 dS.v[m] = scaled4(dS.v[m], decayed) + sums[m].total();
             }
             dS.publish(Ds, w, r, g);
-            float *const left = at.dR(k) + (int64_t)row * a.Dv + col, *const f0 = at.found(k) + (int64_t)row * a.Dv + col;
+            float *const left = at.dR(k) + row * ld + col, *const f0 = at.found(k) + row * ld + col;     // a tile's columns are all there
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float *const p = live ? left + (int64_t)i * a.Dv : sink, *const q = live ? f0 + (int64_t)i * a.Dv : sink;
-                *p = dR[i];
-                *q = found[i];
+                left[i * ld] = dR[i];
+                f0[i * ld] = found[i];
                 E::store(live && row + i < n ? dv0 + (int64_t)c * C * a.dv_t + dv_at[i] : (T*)sink, beta4[i] * dR[i]);
             }
             KT0 -= more ? keys_step : 0;
@@ -964,33 +996,45 @@ __global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int
     if (k.n <= 0) return;
     const Place<E, DKP, true> at(a);
     StateTile<DKP> S, dS;
-    S.load(a.states + k.index * a.Dk * a.Dv, a, w, g, col);
-    dS.load(at.dS(k), a, w, g, col);
+    const int ld = at.row();
+    FourSteps<E> raw;
+    FourSteps<F32> raw_beta;
+    raw.place(row, min(col, a.Dv - 1), a.v_t, k.n);
+    raw_beta.place(row, 0, a.beta_t, k.n);
+    S.load(a.states + k.index * a.Dk * a.Dv, a.Dv, a, w, g, col);
+    dS.load(at.dS(k), ld, a, w, g, col);
+    raw.load(row_of<E>(a.v, a.v_t, a.v_b, k.t0, b, (int64_t)h * a.Dv), true);
+    raw_beta.load(row_of<F32>(a.beta, a.beta_t, a.beta_b, k.t0, b, h), true);
+    float dot = 0.f, dR[4], found[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        dR[i] = at.dR(k)[(row + i) * ld + col];
+        found[i] = at.found(k)[(row + i) * ld + col];
+    }
+    bf16x8 K[kK][kP], X[2][3];
+#pragma unroll
+    for (int s = 0; s < kK; ++s) fragment<kP>(K[s], at.K(k) + fragment_at(w, kK, s) + 8 * lane, C * DKP);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) fragment<3>(X[s], at.X(k) + fragment_at(w, 2, s) + 8 * lane, C * C);
+    const f32x4v y = at4(at.y(k) + row);
     S.publish(Ss, w, r, g);
-    float dot = 0.f, v[4], beta[4], dR[4], found[4];
 #pragma unroll
     for (int m = 0; m < DKP / 64; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) dot = fmaf(S.v[m][i], dS.v[m][i], dot);
-    const f32x4v y = at4(at.y(k) + row);
+    const f32x4v v = raw.take(row, k.n), beta = raw_beta.take(row, k.n);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        beta[i] = beta_at(a, k, row + i);
-        v[i] = live && row + i < k.n ? E::load(row_of<E>(a.v, a.v_t, a.v_b, k.t0 + row + i, b, (int64_t)h * a.Dv + col)) : 0.f;
-        dR[i] = live ? at.dR(k)[(int64_t)(row + i) * a.Dv + col] : 0.f;
-        found[i] = live ? at.found(k)[(int64_t)(row + i) * a.Dv + col] : 0.f;
+        dR[i] = live ? dR[i] : 0.f;
+        found[i] = live ? found[i] : 0.f;
     }
-    bf16x8 X[2][3];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) fragment<3>(X[s], at.X(k) + fragment_at(w, 2, s) + 8 * lane, C * C);
     lds_barrier();
     Sums ks;
 #pragma unroll
     for (int s = 0; s < kK; ++s) {
-        bf16x8 f[3], K[kP];
+        bf16x8 f[3];
         fragment<3>(f, Ss + r * LD + 32 * s + 8 * g, kTile * LD);
-        fragment<kP>(K, at.K(k) + fragment_at(w, kK, s) + 8 * lane, C * DKP);
-        multiply(ks, K, f);
+        multiply(ks, K[s], f);
     }
     const f32x4v read = ks.total();
     f32x4v R;
@@ -1010,7 +1054,6 @@ __global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int
     Sums u;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        if (w < 2 && s == 1) continue;
         bf16x8 f[3];
         fragment<3>(f, Rs + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
         multiply(u, X[s], f);
@@ -1019,7 +1062,7 @@ __global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int
     float* const parts = at.parts(k, tile);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (live) at.U(k)[(int64_t)(row + i) * a.Dv + col] = U[i];
+        at.U(k)[(row + i) * ld + col] = U[i];
         const float d = row16_sum(db[i]), f = row16_sum(from_front[i]), l = row16_sum(U[i] * found[i]);
         if (r == 0) {
             parts[row + i] = d;
@@ -1042,7 +1085,7 @@ __global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int
 // the waves make together; a wave holds the results of 16 steps.
 constexpr int kWide = 32, kWideRow = kWide + 8;         // columns of a tile, and its row in LDS
 constexpr int kRowsAtOnce = 128;                        // of S and dS' in LDS
-template <class E, int DKP>
+template <class E, int DKP, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void delta_gradient_kernel(DeltaArgs a)
 {
     using T = typename E::T;
@@ -1060,6 +1103,7 @@ __global__ __launch_bounds__(kThreads) void delta_gradient_kernel(DeltaArgs a)
     const int n = (int)min((int64_t)length_of(a, b) - t0, (int64_t)C), rows = (int)min((int64_t)a.T - t0, (int64_t)C);
     const int row = 16 * w + 4 * g, mine = 16 * w + r;          // the lane's steps as results, and its step as first operand
     const Place<E, DKP, true> at(a);
+    const int ld = at.row();
     for (int hh = 0; hh < group; ++hh) {
         const Block k = block_of(a, c, b, hk * group + hh);
         if (n <= 0) {
@@ -1082,10 +1126,12 @@ __global__ __launch_bounds__(kThreads) void delta_gradient_kernel(DeltaArgs a)
             {
                 const int c8 = c0 + 8 * g;
                 const bool has = mine < n;
-                const T* const o_row = row_of<E>(a.dO, a.do_t, a.do_b, t0 + mine, b, (int64_t)k.h * a.Dv);
-                split8<kP>(has ? load4<E>(o_row, c8, a.Dv) : kZero4, has ? load4<E>(o_row, c8 + 4, a.Dv) : kZero4, dO);
-                split8<3>(load4<F32>(left + (int64_t)mine * a.Dv, c8, a.Dv), load4<F32>(left + (int64_t)mine * a.Dv, c8 + 4, a.Dv), dR);
-                split8<3>(load4<F32>(updates + (int64_t)mine * a.Dv, c8, a.Dv), load4<F32>(updates + (int64_t)mine * a.Dv, c8 + 4, a.Dv), U);
+                const T* const o_row = row_of<E>(a.dO, a.do_t, a.do_b, t0 + min(mine, n - 1), b, (int64_t)k.h * a.Dv);
+                const f32x4v o0 = fetch4<E, WHOLE>(o_row, c8, a.Dv), o1 = fetch4<E, WHOLE>(o_row, c8 + 4, a.Dv), l0 = padded4(left + mine * ld, c8, a.Dv),
+                             l1 = padded4(left + mine * ld, c8 + 4, a.Dv), u0 = padded4(updates + mine * ld, c8, a.Dv), u1 = padded4(updates + mine * ld, c8 + 4, a.Dv);
+                split8<kP>(if4(has, o0), if4(has, o1), dO);
+                split8<3>(l0, l1, dR);
+                split8<3>(u0, u1, U);
             }
 #pragma unroll
             for (int d0 = 0; d0 < DKP; d0 += kRows) {
@@ -1093,12 +1139,20 @@ __global__ __launch_bounds__(kThreads) void delta_gradient_kernel(DeltaArgs a)
                 if (d0 == 0)
 #pragma unroll
                     for (int i = 0; i < 3; ++i) *(bf16x8*)(Us + (i * C + mine) * kWideRow + 8 * g) = U[i];
-#pragma unroll 4
-                for (int p = threadIdx.x; p < kRows * kWide / 4; p += kThreads) {
-                    const int d = p / (kWide / 4), from = p % (kWide / 4) * 4;
+                constexpr int kEach = kRows * kWide / 4 / kThreads;
+                f32x4v s4[kEach], ds4[kEach];
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int p = threadIdx.x + i * kThreads, d = min(d0 + p / (kWide / 4), a.Dk - 1), from = c0 + p % (kWide / 4) * 4;
+                    s4[i] = fetch4<F32, WHOLE>(front + (int64_t)d * a.Dv, from, a.Dv);
+                    ds4[i] = padded4(behind + d * ld, from, a.Dv);
+                }
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int p = threadIdx.x + i * kThreads, d = p / (kWide / 4), from = p % (kWide / 4) * 4;
                     const bool there = d0 + d < a.Dk;
-                    store_split<3>(there ? load4<F32>(front + (int64_t)(d0 + d) * a.Dv, c0 + from, a.Dv) : kZero4, Ss + d * kWideRow + from, kRows * kWideRow);
-                    store_split<kR>(there ? load4<F32>(behind + (int64_t)(d0 + d) * a.Dv, c0 + from, a.Dv) : kZero4, Ds + d * kWideRow + from, kRows * kWideRow);
+                    store_split<3>(if4(there, s4[i]), Ss + d * kWideRow + from, kRows * kWideRow);
+                    store_split<kR>(if4(there, ds4[i]), Ds + d * kWideRow + from, kRows * kWideRow);
                 }
                 __syncthreads();
                 bf16x8 Ur[kR], Rr[kR];
@@ -1307,7 +1361,7 @@ template <class E, int DKP, bool BACK>
 hipError_t prepare(const DeltaArgs& a, hipStream_t s)
 {
     const size_t lds = std::max<size_t>(2 * C * kStaged<E, DKP> * E::kBytes, 3 * C * kRow * sizeof(float));
-    const auto kernel = delta_prepare_kernel<E, DKP, BACK>;
+    const auto kernel = a.Dk % 4 == 0 ? delta_prepare_kernel<E, DKP, BACK, true> : delta_prepare_kernel<E, DKP, BACK, false>;
     const hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks(a.T) * a.B * a.heads)), dim3(kThreads), lds, s, a);
@@ -1342,7 +1396,7 @@ hipError_t backward(const DeltaArgs& a, hipStream_t s)
     hipLaunchKernelGGL((delta_update_kernel<E, DKP>), dim3((unsigned)(blocks(a.T) * a.B * a.heads * tiles)), dim3(kThreads), 0, s, a, tiles);
     constexpr int kRows = DKP < kRowsAtOnce ? DKP : kRowsAtOnce;
     const size_t lds = std::max<size_t>(((3 + kForResult<E>)*kRows + 3 * C) * kWideRow * sizeof(u16), 2 * C * kRow * sizeof(float));
-    const auto kernel = delta_gradient_kernel<E, DKP>;
+    const auto kernel = a.Dv % 4 == 0 ? delta_gradient_kernel<E, DKP, true> : delta_gradient_kernel<E, DKP, false>;
     e = allow_dynamic_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks(a.T) * a.B * a.key_heads)), dim3(kThreads), lds, s, a);
