@@ -145,6 +145,9 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" : : : "memory");
 }
 
+// Keeps the loads of a later turn of an unrolled loop out of the turns in front of it, where their registers would not be there.
+__device__ __forceinline__ void one_by_one() { asm volatile("" : : : "memory"); }
+
 // columns col .. col + 3 of a row that has `width` of them; 0 behind it
 template <class E>
 __device__ __forceinline__ f32x4v load4(const typename E::T* row, int col, int width)
@@ -1081,106 +1084,125 @@ __global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int
 //            + sum_{j < t} U.(e K dS')_j + exp(G_last) S.dS'
 //
 // (each decay's own terms; as differences of what reaches two neighbouring G, what a strong decay leaves of dg would be lost).
-// A workgroup takes a block of one sequence and key head and goes through the heads that share it, 32 columns of S at a time, whose planes
-// the waves make together; a wave holds the results of 16 steps.
+// A workgroup of eight waves takes a block of one sequence and key head and goes through the heads that share it, 32 columns of S at a time,
+// whose planes its threads make together while the next ones are on their way.  Waves w and w + 4 hold the results of the same 16 steps, each
+// for every other 64 key columns' half; of the pairs of steps the first makes dP, the second dA.
+constexpr int kGradientWaves = 8, kGradientThreads = 64 * kGradientWaves;
 constexpr int kWide = 32, kWideRow = kWide + 8;         // columns of a tile, and its row in LDS
 constexpr int kRowsAtOnce = 128;                        // of S and dS' in LDS
 template <class E, int DKP, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void delta_gradient_kernel(DeltaArgs a)
+__global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(DeltaArgs a)
 {
     using T = typename E::T;
     extern __shared__ float lds[];
-    constexpr int kP = kPlanes<E>, kR = kForResult<E>, kParts = DKP / 16, kRows = DKP < kRowsAtOnce ? DKP : kRowsAtOnce;
+    constexpr int kP = kPlanes<E>, kR = kForResult<E>, kRows = DKP < kRowsAtOnce ? DKP : kRowsAtOnce, kTurns = DKP / kRows;
+    constexpr int kParts = DKP / 32, kEach = kRows / 32;        // tiles of 16 key columns of a wave, those of a turn
+    constexpr int kLoads = kRows * kWide / 4 / kGradientThreads;
     // S (three planes), dS' and U of a tile of columns; in their place later dP and dA
     u16 *const Ss = (u16*)lds, *const Ds = Ss + 3 * kRows * kWideRow, *const Us = Ds + kR * kRows * kWideRow;
     float *const Ps = lds, *const As = Ps + C * kRow;
     __shared__ double Gs[C];
-    __shared__ float ys[C], es[C], betas[C], overs[kWaves][C], fronts[C], dbs[C];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    __shared__ float ys[C], es[C], betas[C], overs[kGradientWaves][C], fronts[2][C], backs[C], dbs[2][C];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3, half = wave >> 2, r = lane & 15, g = lane >> 4;
     const unsigned id = by_xcd(blockIdx.x, gridDim.x);
     const int c = (int)(id / a.key_heads / a.B), b = (int)(id / a.key_heads % a.B), hk = (int)(id % a.key_heads), group = a.heads / a.key_heads;
     const int64_t t0 = (int64_t)c * C;
     const int n = (int)min((int64_t)length_of(a, b) - t0, (int64_t)C), rows = (int)min((int64_t)a.T - t0, (int64_t)C);
+    if (n <= 0) {       // behind the sequence's end
+        for (int p = threadIdx.x; p < rows * a.Dk; p += kGradientThreads) {
+            E::store((T*)row_of<E>(a.dq, a.dq_t, a.dq_b, t0 + p / a.Dk, b, (int64_t)hk * a.Dk + p % a.Dk), 0.f);
+            E::store((T*)row_of<E>(a.dk, a.dk_t, a.dk_b, t0 + p / a.Dk, b, (int64_t)hk * a.Dk + p % a.Dk), 0.f);
+        }
+        for (int p = threadIdx.x; p < rows * group; p += kGradientThreads) {
+            if (a.dg) *(float*)row_of<F32>(a.dg, a.dg_t, a.dg_b, t0 + p / group, b, hk * group + p % group) = 0.f;
+            *(float*)row_of<F32>(a.dbeta, a.dbeta_t, a.dbeta_b, t0 + p / group, b, hk * group + p % group) = 0.f;
+        }
+        return;
+    }
     const int row = 16 * w + 4 * g, mine = 16 * w + r;          // the lane's steps as results, and its step as first operand
     const Place<E, DKP, true> at(a);
-    const int ld = at.row();
+    const int ld = at.row(), wides = (a.Dv + kWide - 1) / kWide;
+    // tile m of the wave in turn d0 stands for the key columns from here on
+    const auto key_column = [&](int turn, int m) { return turn * kRows + 16 * (half * kEach + m); };
     for (int hh = 0; hh < group; ++hh) {
         const Block k = block_of(a, c, b, hk * group + hh);
-        if (n <= 0) {
-            if (w == 0 && lane < rows) {
-                if (a.dg) *(float*)row_of<F32>(a.dg, a.dg_t, a.dg_b, t0 + lane, b, k.h) = 0.f;
-                *(float*)row_of<F32>(a.dbeta, a.dbeta_t, a.dbeta_b, t0 + lane, b, k.h) = 0.f;
-            }
-            continue;
-        }
         const float *const behind = at.dS(k), *const left = at.dR(k), *const updates = at.U(k), *const front = a.states + k.index * a.Dk * a.Dv;
-        if (w == 0) {
+        const T* const o_row = row_of<E>(a.dO, a.do_t, a.do_b, t0 + min(mine, n - 1), b, (int64_t)k.h * a.Dv);
+        if (wave == 0) {
             Gs[lane] = running(a, k, lane);
             ys[lane] = at.y(k)[lane];
             es[lane] = at.e(k)[lane];
             betas[lane] = beta_at(a, k, lane);
         }
-        Sum dq[kParts], from_dS[kParts], from_dR[kParts], dP[4], dL[4];
-        for (int c0 = 0; c0 < a.Dv; c0 += kWide) {
-            bf16x8 dO[kP], dR[3], U[3];
-            {
-                const int c8 = c0 + 8 * g;
-                const bool has = mine < n;
-                const T* const o_row = row_of<E>(a.dO, a.do_t, a.do_b, t0 + min(mine, n - 1), b, (int64_t)k.h * a.Dv);
-                const f32x4v o0 = fetch4<E, WHOLE>(o_row, c8, a.Dv), o1 = fetch4<E, WHOLE>(o_row, c8 + 4, a.Dv), l0 = padded4(left + mine * ld, c8, a.Dv),
-                             l1 = padded4(left + mine * ld, c8 + 4, a.Dv), u0 = padded4(updates + mine * ld, c8, a.Dv), u1 = padded4(updates + mine * ld, c8 + 4, a.Dv);
-                split8<kP>(if4(has, o0), if4(has, o1), dO);
-                split8<3>(l0, l1, dR);
-                split8<3>(u0, u1, U);
+        Sum dq[kParts], from_dS[kParts], from_dR[kParts], pairs[4];     // pairs: dO U' or dR U'
+        f32x4v s4[kLoads], ds4[kLoads], u4, o4[2], l4[2];
+        const auto fetch_states = [&](int turn) {
+            const int c0 = turn / kTurns * kWide, d0 = turn % kTurns * kRows;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int p = threadIdx.x + i * kGradientThreads, d = min(d0 + p / (kWide / 4), a.Dk - 1), from = c0 + p % (kWide / 4) * 4;
+                s4[i] = fetch4<F32, WHOLE>(front + (int64_t)d * a.Dv, from, a.Dv);
+                ds4[i] = padded4(behind + d * ld, from, a.Dv);
             }
+        };
+        const auto fetch_rows = [&](int wide) {
+            const int c8 = wide * kWide + 8 * g;
+            o4[0] = fetch4<E, WHOLE>(o_row, c8, a.Dv);
+            o4[1] = fetch4<E, WHOLE>(o_row, c8 + 4, a.Dv);
+            l4[0] = padded4(left + mine * ld, c8, a.Dv);
+            l4[1] = padded4(left + mine * ld, c8 + 4, a.Dv);
+            u4 = padded4(updates + threadIdx.x / (kWide / 4) * ld, wide * kWide + threadIdx.x % (kWide / 4) * 4, a.Dv);
+        };
+        static_assert(C * kWide / 4 == kGradientThreads, "");
+        fetch_states(0);
+        fetch_rows(0);
+        for (int wide = 0; wide < wides; ++wide) {
+            bf16x8 dO[kP], dR[3], U[kR];
 #pragma unroll
-            for (int d0 = 0; d0 < DKP; d0 += kRows) {
-                __syncthreads();
-                if (d0 == 0)
-#pragma unroll
-                    for (int i = 0; i < 3; ++i) *(bf16x8*)(Us + (i * C + mine) * kWideRow + 8 * g) = U[i];
-                constexpr int kEach = kRows * kWide / 4 / kThreads;
-                f32x4v s4[kEach], ds4[kEach];
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    const int p = threadIdx.x + i * kThreads, d = min(d0 + p / (kWide / 4), a.Dk - 1), from = c0 + p % (kWide / 4) * 4;
-                    s4[i] = fetch4<F32, WHOLE>(front + (int64_t)d * a.Dv, from, a.Dv);
-                    ds4[i] = padded4(behind + d * ld, from, a.Dv);
+            for (int turn = 0; turn < kTurns; ++turn) {
+                lds_barrier();
+                if (turn == 0) {
+                    split8<kP>(if4(mine < n, o4[0]), if4(mine < n, o4[1]), dO);
+                    split8<3>(l4[0], l4[1], dR);
+                    store_split<3>(u4, Us + threadIdx.x / (kWide / 4) * kWideRow + threadIdx.x % (kWide / 4) * 4, C * kWideRow);
                 }
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    const int p = threadIdx.x + i * kThreads, d = p / (kWide / 4), from = p % (kWide / 4) * 4;
-                    const bool there = d0 + d < a.Dk;
+                for (int i = 0; i < kLoads; ++i) {
+                    const int p = threadIdx.x + i * kGradientThreads, d = p / (kWide / 4), from = p % (kWide / 4) * 4;
+                    const bool there = turn * kRows + d < a.Dk;
                     store_split<3>(if4(there, s4[i]), Ss + d * kWideRow + from, kRows * kWideRow);
                     store_split<kR>(if4(there, ds4[i]), Ds + d * kWideRow + from, kRows * kWideRow);
                 }
-                __syncthreads();
-                bf16x8 Ur[kR], Rr[kR];
-#pragma unroll
-                for (int i = 0; i < kR; ++i) {
-                    Ur[i] = U[i];
-                    Rr[i] = dR[i];
-                }
-#pragma unroll
-                for (int m = 0; m < kRows / 16; ++m) {
-                    bf16x8 s[3], ds[kR], sr[kR];
-                    fragment<3>(s, Ss + (16 * m + r) * kWideRow + 8 * g, kRows * kWideRow);
-                    fragment<kR>(ds, Ds + (16 * m + r) * kWideRow + 8 * g, kRows * kWideRow);
-#pragma unroll
-                    for (int i = 0; i < kR; ++i) sr[i] = s[i];
-                    multiply(dq[d0 / 16 + m], dO, s);
-                    multiply(from_dR[d0 / 16 + m], Rr, sr);
-                    multiply(from_dS[d0 / 16 + m], Ur, ds);
-                }
-                if (d0 == 0)
+                fetch_states(min(wide * kTurns + turn + 1, wides * kTurns - 1));
+                if (turn == 0) fetch_rows(min(wide + 1, wides - 1));
+                lds_barrier();
+                if (turn == 0) {
+                    fragment<kR>(U, Us + mine * kWideRow + 8 * g, C * kWideRow);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        if (j > w) continue;
+                        if (kP > 1) one_by_one();
                         bf16x8 u[3];
                         fragment<3>(u, Us + (16 * j + r) * kWideRow + 8 * g, C * kWideRow);
-                        multiply(dP[j], dO, u);
-                        multiply(dL[j], dR, u);
+                        if (half == 0) multiply(pairs[j], dO, u);
+                        else multiply(pairs[j], dR, u);
                     }
+                }
+                bf16x8 Rr[kR];
+#pragma unroll
+                for (int i = 0; i < kR; ++i) Rr[i] = dR[i];
+#pragma unroll
+                for (int m = 0; m < kEach; ++m) {
+                    if (kP > 1) one_by_one();
+                    bf16x8 s[3], ds[kR], sr[kR];
+                    const int at_row = (16 * (half * kEach + m) + r) * kWideRow + 8 * g;
+                    fragment<3>(s, Ss + at_row, kRows * kWideRow);
+                    fragment<kR>(ds, Ds + at_row, kRows * kWideRow);
+#pragma unroll
+                    for (int i = 0; i < kR; ++i) sr[i] = s[i];
+                    multiply(dq[turn * kEach + m], dO, s);
+                    multiply(from_dR[turn * kEach + m], Rr, sr);
+                    multiply(from_dS[turn * kEach + m], U, ds);
+                }
             }
         }
         __syncthreads();
@@ -1192,98 +1214,98 @@ __global__ __launch_bounds__(kThreads) void delta_gradient_kernel(DeltaArgs a)
             beta[i] = betas[row + i];
             from_front[i] = db[i] = 0.f;
         }
-        // what the tiles of columns have added: lane 16 g + i of the wave the tiles i, i + 16, .. of its four steps
+        // what the tiles of columns have added: lane 16 g + i of the first wave the tiles i, i + 16, .. of its four steps
         float to_back[4] = {}, dot = 0.f;
-        for (int tile = r; tile < at.tiles(); tile += 16) {
-            const float* const parts = at.parts(k, tile);
+        if (half == 0)
+            for (int tile = r; tile < at.tiles(); tile += 16) {
+                const float* const parts = at.parts(k, tile);
+                const f32x4v d4 = at4(parts + row), f4 = at4(parts + C + row), l4 = at4(parts + 2 * C + row);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                db[i] += parts[row + i];
-                from_front[i] += parts[C + row + i];
-                to_back[i] += parts[2 * C + row + i];
+                for (int i = 0; i < 4; ++i) {
+                    db[i] += d4[i];
+                    from_front[i] += f4[i];
+                    to_back[i] += l4[i];
+                }
+                dot += parts[3 * C];
             }
-            dot += parts[3 * C];
-        }
-        const u16* const Q = at.Q(k);
+        const u16 *const Q = at.Q(k), *const K = at.K(k);
 #pragma unroll
         for (int m = 0; m < kParts; ++m) {
+            one_by_one();
             const f32x4v q4 = dq[m].total(), s4 = from_dS[m].total(), r4 = from_dR[m].total();
+            const int d = key_column(m / kEach, m % kEach) + r;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float q = 0.f;
 #pragma unroll
-                for (int p = kP - 1; p >= 0; --p) q += __uint_as_float((uint32_t)Q[p * C * DKP + fragment_at(w, DKP / 32, m / 2) + 8 * (4 * g + i + 16 * (m % 2 * 2 + r / 8)) + r % 8] << 16);
+                for (int p = kP - 1; p >= 0; --p)
+                    q += __uint_as_float((uint32_t)Q[p * C * DKP + fragment_at(w, DKP / 32, d / 32) + 8 * (4 * g + i + d % 32 / 8 * 16) + d % 8] << 16);
                 dq_sum[m][i] = a.scale * y[i] * q4[i];
                 dk_sum[m][i] = es[row + i] * s4[i] - y[i] * beta[i] * r4[i];
                 from_front[i] = fmaf(q, dq_sum[m][i], from_front[i]);
             }
         }
-        Sum kk[4], qk[4];
-        const u16* const K = at.K(k);
+        // q.k for the first wave, k.k for the second
+        Sum dots[4];
+        const u16* const own = half == 0 ? Q : K;
 #pragma unroll
-        for (int d = 0; d < DKP; d += 32) {
-            bf16x8 ka[kP], qa[kP];
-            fragment<kP>(ka, K + fragment_at(w, DKP / 32, d / 32) + 8 * lane, C * DKP);
-            fragment<kP>(qa, Q + fragment_at(w, DKP / 32, d / 32) + 8 * lane, C * DKP);
+        for (int s = 0; s < DKP / 32; ++s) {
+            one_by_one();
+            bf16x8 fa[kP];
+            fragment<kP>(fa, own + fragment_at(w, DKP / 32, s) + 8 * lane, C * DKP);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (j > w) continue;
-                bf16x8 kb[kP];
-                fragment<kP>(kb, K + fragment_at(j, DKP / 32, d / 32) + 8 * lane, C * DKP);
-                multiply(kk[j], ka, kb);
-                multiply(qk[j], qa, kb);
+                bf16x8 fb[kP];
+                fragment<kP>(fb, K + fragment_at(j, DKP / 32, s) + 8 * lane, C * DKP);
+                multiply(dots[j], fa, fb);
             }
         }
         float in_front[4] = {};     // pairs of the lane's steps with all steps of the tiles in front of this one
+        float* const square = half == 0 ? Ps : As;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const f32x4v kk4 = kk[j].total(), qk4 = qk[j].total(), dP4 = dP[j].total(), dL4 = dL[j].total();
+            const f32x4v dots4 = dots[j].total(), pairs4 = pairs[j].total();
             float over = 0.f;       // pairs that the decay at step 16 j + r lies between, of the lane's steps
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int own = row + i, other = 16 * j + r;
-                float p = 0.f, l = 0.f, pair = 0.f;
-                if (j <= w && other <= own && own < n) {
-                    const float decay = expf((float)(Gs[own] - Gs[other]));
-                    p = a.scale * decay * dP4[i];
-                    if (other < own) {
-                        l = decay * dL4[i];
-                        db[i] = fmaf(-l, kk4[i], db[i]);
-                        l *= -beta[i];
-                        pair = fmaf(l, kk4[i], p * qk4[i]);
+                const int step = row + i, other = 16 * j + r;
+                float v = 0.f, pair = 0.f;
+                if (other <= step - half && step < n) {         // the first wave has the diagonal too
+                    v = expf((float)(Gs[step] - Gs[other])) * pairs4[i];
+                    if (half == 0) {
+                        v *= a.scale;
+                    } else {
+                        db[i] = fmaf(-v, dots4[i], db[i]);
+                        v *= -beta[i];
                     }
+                    if (other < step) pair = v * dots4[i];
                 }
-                Ps[own * kRow + other] = p;
-                As[own * kRow + other] = l;
+                square[step * kRow + other] = v;
                 // over the steps in front of 16 j + r: the 16 of the tile by shifts along the row of lanes
                 float sum = row16_shifted<1>(pair);
                 sum += row16_shifted<1>(sum);
                 sum += row16_shifted<2>(sum);
                 sum += row16_shifted<4>(sum);
                 sum += row16_shifted<8>(sum);
-                if (other <= own) over += in_front[i] + sum;
+                if (other <= step) over += in_front[i] + sum;
                 in_front[i] += row16_sum(pair);
             }
             over += __shfl_xor(over, 16);
             over += __shfl_xor(over, 32);
-            if (g == 0) overs[w][16 * j + r] = over;
+            if (g == 0) overs[wave][16 * j + r] = over;
         }
         dot = row16_sum(dot);
-        float* const backs = ys;        // which everybody has read
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float f = row16_sum(from_front[i]), l = row16_sum(to_back[i]), d = row16_sum(db[i]);
             if (r == 0) {
-                fronts[row + i] = f;
-                dbs[row + i] = d;
+                fronts[half][row + i] = f;
+                dbs[half][row + i] = d;
+                if (half == 0) backs[row + i] = l;
             }
-            to_back[i] = l;
         }
-        const float last = at.y(k)[C - 1];
+        const float last = ys[C - 1];
         __syncthreads();
-        if (r == 0)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) backs[row + i] = to_back[i];
         bf16x8 both[2][kR], dPa[2][kR], dPt[2][kR];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -1292,9 +1314,10 @@ __global__ __launch_bounds__(kThreads) void delta_gradient_kernel(DeltaArgs a)
             split8<kR>(at4(Ps + mine * kRow + from), at4(Ps + mine * kRow + from + 4), dPa[s]);
             split8<kR>(down4(Ps + from * kRow + mine, kRow), down4(Ps + (from + 4) * kRow + mine, kRow), dPt[s]);
         }
-        __syncthreads();
-        if (w == 0) {
-            double from = fronts[lane], to = backs[lane], dg = (double)overs[0][lane] + overs[1][lane] + overs[2][lane] + overs[3][lane];
+        if (wave == 0) {
+            double from = (double)fronts[0][lane] + fronts[1][lane], to = backs[lane], dg = 0.0;
+#pragma unroll
+            for (int i = 0; i < kGradientWaves; ++i) dg += overs[i][lane];
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) {
                 const double after = __shfl_down(from, off), before = __shfl_up(to, off);
@@ -1305,24 +1328,25 @@ __global__ __launch_bounds__(kThreads) void delta_gradient_kernel(DeltaArgs a)
             dg += from + (lane > 0 ? to : 0.0) + (double)last * dot;
             if (lane < rows) {
                 if (a.dg) *(float*)row_of<F32>(a.dg, a.dg_t, a.dg_b, t0 + lane, b, k.h) = lane < n ? (float)dg : 0.f;
-                *(float*)row_of<F32>(a.dbeta, a.dbeta_t, a.dbeta_b, t0 + lane, b, k.h) = lane < n ? dbs[lane] : 0.f;
+                *(float*)row_of<F32>(a.dbeta, a.dbeta_t, a.dbeta_b, t0 + lane, b, k.h) = lane < n ? dbs[0][lane] + dbs[1][lane] : 0.f;
             }
         }
         const u16 *const KT = at.KT(k), *const QT = at.QT(k);
         float* const shared = at.shared(k);
 #pragma unroll
         for (int m = 0; m < kParts; ++m) {
+            one_by_one();
             Sum sq, sk;
+            const int first = key_column(m / kEach, m % kEach), d = first + r;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 bf16x8 kt[kP], qt[kP];
-                fragment<kP>(kt, KT + fragment_at(m, 2, s) + 8 * lane, C * DKP);
-                fragment<kP>(qt, QT + fragment_at(m, 2, s) + 8 * lane, C * DKP);
+                fragment<kP>(kt, KT + fragment_at(first / 16, 2, s) + 8 * lane, C * DKP);
+                fragment<kP>(qt, QT + fragment_at(first / 16, 2, s) + 8 * lane, C * DKP);
                 multiply(sq, dPa[s], kt);
                 multiply(sk, both[s], kt);
                 multiply(sk, dPt[s], qt);
             }
-            const int d = 16 * m + r;
             const f32x4v q4 = dq_sum[m] + sq.total(), k4 = dk_sum[m] + sk.total();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -1343,11 +1367,6 @@ __global__ __launch_bounds__(kThreads) void delta_gradient_kernel(DeltaArgs a)
             }
         }
         __syncthreads();
-    }
-    if (n > 0) return;
-    for (int p = threadIdx.x; p < rows * a.Dk; p += kThreads) {
-        E::store((T*)row_of<E>(a.dq, a.dq_t, a.dq_b, t0 + p / a.Dk, b, (int64_t)hk * a.Dk + p % a.Dk), 0.f);
-        E::store((T*)row_of<E>(a.dk, a.dk_t, a.dk_b, t0 + p / a.Dk, b, (int64_t)hk * a.Dk + p % a.Dk), 0.f);
     }
 }
 
@@ -1399,7 +1418,7 @@ hipError_t backward(const DeltaArgs& a, hipStream_t s)
     const auto kernel = a.Dv % 4 == 0 ? delta_gradient_kernel<E, DKP, true> : delta_gradient_kernel<E, DKP, false>;
     e = allow_dynamic_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks(a.T) * a.B * a.key_heads)), dim3(kThreads), lds, s, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks(a.T) * a.B * a.key_heads)), dim3(kGradientThreads), lds, s, a);
     return hipGetLastError();
 }
 
