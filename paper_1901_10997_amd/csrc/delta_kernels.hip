@@ -162,29 +162,35 @@ __device__ __forceinline__ f32x4v load4(const typename E::T* row, int col, int w
     return (f32x4v){v[0], v[1], v[2], v[3]};
 }
 
-// The same without a branch, so that loads that follow each other are under way together.  WHOLE: width is a multiple of 4, and four
-// columns move at once; else one by one, those behind the row standing for its last.
+// The same in two steps, without a branch and with nothing that waits in the first, so that loads that follow each other, and what is
+// worked on meanwhile, do not wait for them.  WHOLE: width is a multiple of 4, and four columns move at once; else one by one, those
+// behind the row standing for its last.
 template <class E, bool WHOLE>
-__device__ __forceinline__ f32x4v fetch4(const typename E::T* row, int col, int width)
-{
-    float v[4];
-    if constexpr (WHOLE) {
-        load_n<E, 4, true>(row + min(col, width - 4), v);
+struct Four {
+    using T = typename E::T;
+    T raw[4];
+    __device__ __forceinline__ void load(const T* row, int col, int width)
+    {
+        if constexpr (WHOLE) {
+            if constexpr (E::kBytes == 4) __builtin_memcpy(raw, (const f32x4v_any*)(row + min(col, width - 4)), 16);
+            else __builtin_memcpy(raw, (const u32x2v_any*)(row + min(col, width - 4)), 8);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = col < width ? v[i] : 0.f;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = E::load(row + min(col + i, width - 1));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = col + i < width ? v[i] : 0.f;
+            for (int i = 0; i < 4; ++i) raw[i] = row[min(col + i, width - 1)];
+        }
     }
-    return (f32x4v){v[0], v[1], v[2], v[3]};
-}
+    __device__ __forceinline__ f32x4v take(int col, int width) const
+    {
+        f32x4v v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (WHOLE ? col : col + i) < width ? E::load(raw + i) : 0.f;
+        return v;
+    }
+};
 __device__ __forceinline__ f32x4v if4(bool c, f32x4v v) { return (f32x4v){c ? v[0] : 0.f, c ? v[1] : 0.f, c ? v[2] : 0.f, c ? v[3] : 0.f}; }
-// columns col .. col + 3 of a row of the workspace, which is padded; those behind `width` are 0 whatever stands there
-__device__ __forceinline__ f32x4v padded4(const float* row, int col, int width)
+// of a row of the workspace, which is padded: columns behind `width` are 0 whatever stands there
+__device__ __forceinline__ f32x4v within4(f32x4v v, int col, int width)
 {
-    const f32x4v v = at4(row + col);
     return (f32x4v){col < width ? v[0] : 0.f, col + 1 < width ? v[1] : 0.f, col + 2 < width ? v[2] : 0.f, col + 3 < width ? v[3] : 0.f};
 }
 
@@ -312,12 +318,22 @@ template <class E, int DKP, bool WHOLE>
 __device__ __forceinline__ void stage(const typename E::T* first, int64_t t_stride, int n, int width, typename E::T* to)
 {
     constexpr int kPieces = DKP / 4;
-#pragma unroll 8
-    for (int p = threadIdx.x; p < C * kPieces; p += kThreads) {
-        const int row = p / kPieces, col = p % kPieces * 4;
-        const f32x4v v = if4(row < n, fetch4<E, WHOLE>(first + min(row, n - 1) * t_stride, col, width));
-        const float f[4] = {v[0], v[1], v[2], v[3]};
-        store_n<E, 4>(to + row * kStaged<E, DKP> + col, f);
+    constexpr int kEach = WHOLE && C * kPieces / kThreads > 8 ? 8 : C * kPieces / kThreads / (WHOLE ? 1 : 2);
+#pragma unroll 1
+    for (int p0 = threadIdx.x; p0 < C * kPieces; p0 += kEach * kThreads) {
+        Four<E, WHOLE> v[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int p = p0 + i * kThreads;
+            v[i].load(first + min(p / kPieces, n - 1) * t_stride, p % kPieces * 4, width);
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int p = p0 + i * kThreads, row = p / kPieces, col = p % kPieces * 4;
+            const f32x4v s = if4(row < n, v[i].take(col, width));
+            const float f[4] = {s[0], s[1], s[2], s[3]};
+            store_n<E, 4>(to + row * kStaged<E, DKP> + col, f);
+        }
     }
 }
 // Planes of a staged matrix and of its transpose
@@ -1135,23 +1151,25 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
             betas[lane] = beta_at(a, k, lane);
         }
         Sum dq[kParts], from_dS[kParts], from_dR[kParts], pairs[4];     // pairs: dO U' or dR U'
-        f32x4v s4[kLoads], ds4[kLoads], u4, o4[2], l4[2];
+        Four<F32, WHOLE> s4[kLoads];
+        Four<E, WHOLE> o4[2];
+        f32x4v ds4[kLoads], u4, l4[2];
         const auto fetch_states = [&](int turn) {
             const int c0 = turn / kTurns * kWide, d0 = turn % kTurns * kRows;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int p = threadIdx.x + i * kGradientThreads, d = min(d0 + p / (kWide / 4), a.Dk - 1), from = c0 + p % (kWide / 4) * 4;
-                s4[i] = fetch4<F32, WHOLE>(front + (int64_t)d * a.Dv, from, a.Dv);
-                ds4[i] = padded4(behind + d * ld, from, a.Dv);
+                s4[i].load(front + (int64_t)d * a.Dv, from, a.Dv);
+                ds4[i] = at4(behind + d * ld + from);
             }
         };
         const auto fetch_rows = [&](int wide) {
             const int c8 = wide * kWide + 8 * g;
-            o4[0] = fetch4<E, WHOLE>(o_row, c8, a.Dv);
-            o4[1] = fetch4<E, WHOLE>(o_row, c8 + 4, a.Dv);
-            l4[0] = padded4(left + mine * ld, c8, a.Dv);
-            l4[1] = padded4(left + mine * ld, c8 + 4, a.Dv);
-            u4 = padded4(updates + threadIdx.x / (kWide / 4) * ld, wide * kWide + threadIdx.x % (kWide / 4) * 4, a.Dv);
+            o4[0].load(o_row, c8, a.Dv);
+            o4[1].load(o_row, c8 + 4, a.Dv);
+            l4[0] = at4(left + mine * ld + c8);
+            l4[1] = at4(left + mine * ld + c8 + 4);
+            u4 = at4(updates + threadIdx.x / (kWide / 4) * ld + wide * kWide + threadIdx.x % (kWide / 4) * 4);
         };
         static_assert(C * kWide / 4 == kGradientThreads, "");
         fetch_states(0);
@@ -1162,37 +1180,39 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
             for (int turn = 0; turn < kTurns; ++turn) {
                 lds_barrier();
                 if (turn == 0) {
-                    split8<kP>(if4(mine < n, o4[0]), if4(mine < n, o4[1]), dO);
-                    split8<3>(l4[0], l4[1], dR);
-                    store_split<3>(u4, Us + threadIdx.x / (kWide / 4) * kWideRow + threadIdx.x % (kWide / 4) * 4, C * kWideRow);
+                    const int c8 = wide * kWide + 8 * g, cu = wide * kWide + threadIdx.x % (kWide / 4) * 4;
+                    split8<kP>(if4(mine < n, o4[0].take(c8, a.Dv)), if4(mine < n, o4[1].take(c8 + 4, a.Dv)), dO);
+                    split8<3>(within4(l4[0], c8, a.Dv), within4(l4[1], c8 + 4, a.Dv), dR);
+                    store_split<3>(within4(u4, cu, a.Dv), Us + threadIdx.x / (kWide / 4) * kWideRow + threadIdx.x % (kWide / 4) * 4, C * kWideRow);
                 }
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
                     const int p = threadIdx.x + i * kGradientThreads, d = p / (kWide / 4), from = p % (kWide / 4) * 4;
                     const bool there = turn * kRows + d < a.Dk;
-                    store_split<3>(if4(there, s4[i]), Ss + d * kWideRow + from, kRows * kWideRow);
-                    store_split<kR>(if4(there, ds4[i]), Ds + d * kWideRow + from, kRows * kWideRow);
+                    store_split<3>(if4(there, s4[i].take(wide * kWide + from, a.Dv)), Ss + d * kWideRow + from, kRows * kWideRow);
+                    store_split<kR>(if4(there, within4(ds4[i], wide * kWide + from, a.Dv)), Ds + d * kWideRow + from, kRows * kWideRow);
                 }
                 fetch_states(min(wide * kTurns + turn + 1, wides * kTurns - 1));
                 if (turn == 0) fetch_rows(min(wide + 1, wides - 1));
                 lds_barrier();
                 if (turn == 0) {
                     fragment<kR>(U, Us + mine * kWideRow + 8 * g, C * kWideRow);
+                    const auto multiply_pairs = [&](const auto& first) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (kP > 1) one_by_one();
-                        bf16x8 u[3];
-                        fragment<3>(u, Us + (16 * j + r) * kWideRow + 8 * g, C * kWideRow);
-                        if (half == 0) multiply(pairs[j], dO, u);
-                        else multiply(pairs[j], dR, u);
-                    }
+                        for (int j = 0; j < 4; ++j) {
+                            bf16x8 u[3];
+                            fragment<3>(u, Us + (16 * j + r) * kWideRow + 8 * g, C * kWideRow);
+                            multiply(pairs[j], first, u);
+                        }
+                    };
+                    if (half == 0) multiply_pairs(dO);
+                    else multiply_pairs(dR);
                 }
                 bf16x8 Rr[kR];
 #pragma unroll
                 for (int i = 0; i < kR; ++i) Rr[i] = dR[i];
 #pragma unroll
                 for (int m = 0; m < kEach; ++m) {
-                    if (kP > 1) one_by_one();
                     bf16x8 s[3], ds[kR], sr[kR];
                     const int at_row = (16 * (half * kEach + m) + r) * kWideRow + 8 * g;
                     fragment<3>(s, Ss + at_row, kRows * kWideRow);
@@ -1231,7 +1251,7 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
         const u16 *const Q = at.Q(k), *const K = at.K(k);
 #pragma unroll
         for (int m = 0; m < kParts; ++m) {
-            one_by_one();
+            if (kP > 1 || m % 2 == 0) one_by_one();
             const f32x4v q4 = dq[m].total(), s4 = from_dS[m].total(), r4 = from_dR[m].total();
             const int d = key_column(m / kEach, m % kEach) + r;
 #pragma unroll
@@ -1250,7 +1270,7 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
         const u16* const own = half == 0 ? Q : K;
 #pragma unroll
         for (int s = 0; s < DKP / 32; ++s) {
-            one_by_one();
+            if (kP > 1 || s % 4 == 0) one_by_one();
             bf16x8 fa[kP];
             fragment<kP>(fa, own + fragment_at(w, DKP / 32, s) + 8 * lane, C * DKP);
 #pragma unroll
@@ -1260,26 +1280,29 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
                 multiply(dots[j], fa, fb);
             }
         }
+        // dP is scale D (dO U'); dA is -b D (dR U'), and D (dR U') k.k is taken from db
+        float by[4];
+        double G4[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            by[i] = half == 0 ? a.scale : -beta[i];
+            G4[i] = Gs[row + i];
+        }
+        const float of_beta = half == 0 ? 0.f : -1.f;
         float in_front[4] = {};     // pairs of the lane's steps with all steps of the tiles in front of this one
         float* const square = half == 0 ? Ps : As;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const f32x4v dots4 = dots[j].total(), pairs4 = pairs[j].total();
+            const double G = Gs[16 * j + r];
             float over = 0.f;       // pairs that the decay at step 16 j + r lies between, of the lane's steps
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int step = row + i, other = 16 * j + r;
-                float v = 0.f, pair = 0.f;
-                if (other <= step - half && step < n) {         // the first wave has the diagonal too
-                    v = expf((float)(Gs[step] - Gs[other])) * pairs4[i];
-                    if (half == 0) {
-                        v *= a.scale;
-                    } else {
-                        db[i] = fmaf(-v, dots4[i], db[i]);
-                        v *= -beta[i];
-                    }
-                    if (other < step) pair = v * dots4[i];
-                }
+                const bool there = other <= step - half && step < n;        // the first wave has the diagonal too
+                const float decayed = there ? expf((float)(G4[i] - G)) * pairs4[i] : 0.f, v = decayed * by[i];
+                db[i] = fmaf(of_beta * decayed, dots4[i], db[i]);
+                const float pair = other < step ? v * dots4[i] : 0.f;
                 square[step * kRow + other] = v;
                 // over the steps in front of 16 j + r: the 16 of the tile by shifts along the row of lanes
                 float sum = row16_shifted<1>(pair);
@@ -1335,7 +1358,7 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
         float* const shared = at.shared(k);
 #pragma unroll
         for (int m = 0; m < kParts; ++m) {
-            one_by_one();
+            if (kP > 1 || m % 4 == 0) one_by_one();
             Sum sq, sk;
             const int first = key_column(m / kEach, m % kEach), d = first + r;
 #pragma unroll
