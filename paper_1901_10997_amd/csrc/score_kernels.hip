@@ -9,10 +9,17 @@
 //     gradient: dl_j = dloss heat (s_j - t_j) in the list, dloss heat s_j (1 - t_r / s_r) outside it
 //
 // A workgroup takes a row or a segment of it with its logits in registers, so that the maximum, the sums and the alternatives
-// read them once; where a row has several segments a second launch joins them.  Terms are fp32, their sums fp64: the entropy
-// of a row that is nearly sure is what is left of two sums.
+// read them once; where a row has several segments a second launch joins them.
 //
-// Top alternatives: the n-th largest of the 256 threads' own largest logits is a border that n logits reach, and only n threads
+// Weights are 2^(l k - o) with k = log2(e) / heat in fp32 and o = k max l rounded: one fused multiply-add and the hardware's exponential, its
+// argument off by half a step of itself, which a weight of 2^-t turns into t 2^-25 of itself.  What k and o have been rounded by is the same for
+// a whole row and is put right in 64 bits: with e = k* / k - 1 (k* the exact one) and c = o (1 + e) - k* max l the sum over exp(d) is
+// 2^c (sum + e ln 2 mean), mean being the sum of weight times exponent.  (An exponential of the difference in fp32, with what its product loses put
+// in, and every sum in 64 bits took 62.7 us for 4096 rows of 10 000 bf16.)  Rows whose o is 2^20 or more take the differences.
+// A clamp of the exponent at -200, whose weight is 0, takes in minus infinity and, where such tokens do not exist, NaN.
+// Up to eight weights are added in fp32, those sums in fp64.
+//
+// Top alternatives: threads in groups; the n-th largest of the groups' own largest logits is a border that n logits reach, and only n groups
 // hold logits that reach it; these are put in order by counting who is in front of whom.  A logit and its index make one key, so
 // no two are equal.
 #include "common.h"
@@ -26,27 +33,38 @@ namespace l355 {
 namespace {
 
 typedef unsigned long long u64;
-constexpr int kThreads = 256, kScoreWaves = kThreads / 64;
-constexpr int kMostSegments = 64;           // of a row
+constexpr int kThreads = 256;               // of the kernels that join and that make gradients
+constexpr int kGroups = 256;                // of threads, in the choice of alternatives
 constexpr int kSweep = 8192;                // logits of a workgroup in the gradients
-constexpr float kNone = -__builtin_inff();
+constexpr float kNone = -__builtin_inff(), kNothing = -200.f;
+constexpr double kLog2e = 1.4426950408889634, kLn2 = 0.6931471805599453;
 
-constexpr double kLog2e = 1.4426950408889634;
-
-// exp(c d) for d <= 0: 2 to the power of d k, k = c log2 e as the sum of two floats, with what the product's rounding lost put in
-// afterwards (without, d = -20 would be off by 1e-6).  Minus infinity gives 0, NaN stays.
-struct Exp {
-    float hi, lo;
-    __device__ __forceinline__ explicit Exp(double c) : hi((float)(c * kLog2e)), lo((float)(c * kLog2e - (double)(float)(c * kLog2e))) {}
-    __device__ __forceinline__ float operator()(float d) const
-    {
-        d = d < -1e30f ? -1e30f : d;
-        const float t = d * hi, lost = fmaf(d, lo, fmaf(d, hi, -t)), x = __builtin_amdgcn_exp2f(t);
-        return fmaf(x * lost, 0.6931471805599453f, x);
-    }
-};
 // l - biggest; 0 for an infinite logit that is the biggest
 __device__ __forceinline__ float below(float l, float biggest) { return l == biggest ? 0.f : l - biggest; }
+
+// The exponents l k - o of a row, and what their rounding adds up to
+struct Exponents {
+    float k, o;
+    double e, c;
+    bool usual;             // k biggest is small enough for c to be what rounding leaves (64 bits hold it to 2^-32)
+    __device__ __forceinline__ Exponents(double exact, float biggest)
+    {
+        k = (float)exact;
+        o = k * biggest;
+        usual = fabsf(o) < 0x1p20f;
+        e = exact / (double)k - 1.0;
+        c = (double)o * (1.0 + e) - exact * (double)biggest;
+    }
+    __device__ __forceinline__ float of(float l) const { return fmaxf(fmaf(l, k, -o), kNothing); }
+    // NaN stays
+    __device__ __forceinline__ float or_nan(float l) const
+    {
+        const float t = fmaf(l, k, -o);
+        return t < kNothing ? kNothing : t;
+    }
+};
+// exp(scale d) for d <= 0, rows that are not usual; NaN stays
+__device__ __forceinline__ float far_weight(float d, float scale) { return expf(d * scale); }
 
 __device__ __forceinline__ float wave_max(float v)
 {
@@ -62,36 +80,46 @@ __device__ __forceinline__ T wave_add(T v)
     return v;
 }
 // over the workgroup, in every thread
+template <int WAVES>
 struct Shared {
-    float f[kScoreWaves];
-    double d[kScoreWaves];
-    int i[kScoreWaves];
+    float f[WAVES];
+    double d[WAVES], d2[WAVES];
+    int i[WAVES];
 };
-__device__ __forceinline__ float group_max(float v, Shared& sh)
+template <int WAVES>
+__device__ __forceinline__ float group_max(float v, Shared<WAVES>& sh)
 {
     v = wave_max(v);
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) sh.f[threadIdx.x >> 6] = v;
     __syncthreads();
-    return fmaxf(fmaxf(sh.f[0], sh.f[1]), fmaxf(sh.f[2], sh.f[3]));
+    v = sh.f[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v = fmaxf(v, sh.f[w]);
+    return v;
 }
-__device__ __forceinline__ double group_add(double v, Shared& sh)
+// three sums in one go
+template <int WAVES>
+__device__ __forceinline__ void group_add(double& a, double& b, int& c, Shared<WAVES>& sh)
 {
-    v = wave_add(v);
+    a = wave_add(a);
+    b = wave_add(b);
+    c = wave_add(c);
+    if ((threadIdx.x & 63) == 0) {
+        sh.d[threadIdx.x >> 6] = a;
+        sh.d2[threadIdx.x >> 6] = b;
+        sh.i[threadIdx.x >> 6] = c;
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.d[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (sh.d[0] + sh.d[1]) + (sh.d[2] + sh.d[3]);
+    a = sh.d[0];
+    b = sh.d2[0];
+    c = sh.i[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+        a += sh.d[w];
+        b += sh.d2[w];
+        c += sh.i[w];
+    }
 }
-__device__ __forceinline__ int group_add(int v, Shared& sh)
-{
-    v = wave_add(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.i[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (sh.i[0] + sh.i[1]) + (sh.i[2] + sh.i[3]);
-}
-static_assert(kScoreWaves == 4, "");
 
 // W neighbouring logits from col on; what lies behind the row is minus infinity
 template <class E>
@@ -119,24 +147,21 @@ __device__ __forceinline__ void store_wide(typename E::T* row, int col, int V, c
             if (col + e < V) E::store(row + col + e, v[e]);
     }
 }
-// a byte for each of them that does not exist becomes minus infinity, and so does NaN
+// a byte for each of them that does not exist becomes minus infinity
 template <class E>
 __device__ __forceinline__ void leave_out(const uint8_t* allowed, int col, int V, float* v)
 {
     constexpr int W = kWide<E>;
-    if (allowed) {
-        if (col + W <= V) {
-            uint32_t word[W / 4];
-            __builtin_memcpy(word, allowed + col, W);
+    if (!allowed) return;
+    if (col + W <= V) {
+        uint32_t word[W / 4];
+        __builtin_memcpy(word, allowed + col, W);
 #pragma unroll
-            for (int e = 0; e < W; ++e) v[e] = word[e / 4] >> (e % 4 * 8) & 0xff ? v[e] : kNone;
-        } else {
+        for (int e = 0; e < W; ++e) v[e] = word[e / 4] >> (e % 4 * 8) & 0xff ? v[e] : kNone;
+    } else {
 #pragma unroll
-            for (int e = 0; e < W; ++e) v[e] = col + e < V && allowed[col + e] ? v[e] : kNone;
-        }
+        for (int e = 0; e < W; ++e) v[e] = col + e < V && allowed[col + e] ? v[e] : kNone;
     }
-#pragma unroll
-    for (int e = 0; e < W; ++e) v[e] = v[e] == v[e] ? v[e] : kNone;
 }
 // that of one token, none where it does not exist
 template <class E>
@@ -146,10 +171,10 @@ __device__ __forceinline__ float logit_of(const typename E::T* row, const uint8_
     return v == v && (!allowed || allowed[token]) ? v : kNone;
 }
 
-// Key of a token: larger for a larger logit, then for a smaller index; 0 for one that does not exist.  -0 is 0.
+// Key of a token: larger for a larger logit, then for a smaller index; 0 for one that does not exist (NaN among them).  -0 is 0.
 __device__ __forceinline__ u64 key_of(float v, int col)
 {
-    if (v == kNone) return 0;
+    if (!(v > kNone)) return 0;
     const uint32_t u = __float_as_uint(v + 0.f), ordered = u >> 31 ? ~u : u | 0x80000000u;
     return (u64)ordered << 32 | (uint32_t)~col;
 }
@@ -160,40 +185,48 @@ __device__ __forceinline__ float logit_of_key(u64 key)
 }
 __device__ __forceinline__ int token_of_key(u64 key) { return (int)~(uint32_t)key; }
 
+// LIST: the most keys that can reach the border: those of kScoreMaxTop groups
+template <int LIST>
 struct TopShared {
-    u64 most[kThreads];
-    u64 list[kScoreMaxTop * 64];
+    u64 most[kGroups];
+    u64 list[LIST];
     u64 first[kScoreMaxTop];
     u64 border;
     int count;
 };
 // The n largest keys of the workgroup, in order, in sh.first (0 where there are fewer).  `most`: the thread's largest key;
-// each(f): calls f with its keys, at most 64.
-template <class Each>
-__device__ __forceinline__ void top_keys(int n, u64 most, TopShared& sh, Each each)
+// each(f): calls f with its keys.
+template <int THREADS, int LIST, class Each>
+__device__ __forceinline__ void top_keys(int n, u64 most, TopShared<LIST>& sh, Each each)
 {
+    constexpr int kOf = THREADS / kGroups;      // neighbouring threads of a group: 1 or 4
     const int tid = threadIdx.x;
-    __syncthreads();
-    sh.most[tid] = most;
+    u64 group = most;
+#pragma unroll
+    for (int off = 1; off < kOf; off <<= 1) group = max(group, __shfl_xor(group, off));
+    if (tid % kOf == 0) sh.most[tid / kOf] = group;
     if (tid == 0) {
         sh.border = 0;
         sh.count = 0;
     }
     if (tid < n) sh.first[tid] = 0;
     __syncthreads();
-    int front = 0;
+    if (tid < kGroups) {
+        const u64 mine = sh.most[tid];
+        int front = 0;
 #pragma unroll 8
-    for (int i = 0; i < kThreads; ++i) front += sh.most[i] > most;
-    if (most && front == n - 1) sh.border = most;
+        for (int i = 0; i < kGroups; ++i) front += sh.most[i] > mine;
+        if (mine && front == n - 1) sh.border = mine;
+    }
     __syncthreads();
     const u64 border = sh.border;
     if (most && most >= border)
-        each([&](u64 key) {
+        each(border, [&](u64 key) {
             if (key && key >= border) sh.list[atomicAdd(&sh.count, 1)] = key;
         });
     __syncthreads();
     const int count = sh.count;
-    for (int i = tid; i < count; i += kThreads) {
+    for (int i = tid; i < count; i += THREADS) {
         const u64 key = sh.list[i];
         int place = 0;
         for (int j = 0; j < count; ++j) place += sh.list[j] > key;
@@ -209,12 +242,12 @@ struct Part {
     int front;              // tokens in front of the given one
 };
 
-__device__ __forceinline__ void finish_row(const ScoreArgs& a, int m, const Part& p, bool given, float mine, const TopShared* top)
+__device__ __forceinline__ void finish_row(const ScoreArgs& a, int m, const Part& p, bool given, float mine, const u64* first)
 {
     const bool some = p.biggest > kNone;
     const double log_sum = some ? log(p.sum) : 0.0;
-    const double entropy = some ? log_sum - p.mean / p.sum : 0.0;
     if (threadIdx.x == 0) {
+        const double entropy = some ? log_sum - p.mean / p.sum : 0.0;
         if (a.logprob) a.logprob[m] = !given ? 0.f : mine > kNone ? (float)((double)below(mine, p.biggest) - log_sum) : kNone;
         if (a.rank) a.rank[m] = given ? p.front : -1;
         if (a.entropy) a.entropy[m] = (float)entropy;
@@ -226,8 +259,8 @@ __device__ __forceinline__ void finish_row(const ScoreArgs& a, int m, const Part
             s[3] = some ? (float)(1.0 / p.sum) : 0.f;
         }
     }
-    if (top && (int)threadIdx.x < a.top_n) {
-        const u64 key = top->first[threadIdx.x];
+    if (first && (int)threadIdx.x < a.top_n) {
+        const u64 key = first[threadIdx.x];
         const int64_t at = (int64_t)m * a.top_n + threadIdx.x;
         a.top_token[at] = key ? token_of_key(key) : -1;
         a.top_logprob[at] = key ? (float)((double)below(logit_of_key(key), p.biggest) - log_sum) : kNone;
@@ -237,70 +270,123 @@ __device__ __forceinline__ void finish_row(const ScoreArgs& a, int m, const Part
 __device__ __forceinline__ Part* parts_of(void* ws) { return (Part*)ws; }
 __device__ __forceinline__ u64* keys_of(void* ws, int M, int segs) { return (u64*)(parts_of(ws) + (int64_t)M * segs); }
 
-template <class E, int VPT, bool TOP>
-__global__ __launch_bounds__(kThreads) void score_kernel(ScoreArgs a, int segs)
+// The largest number below v (of zero, the smallest negative one)
+__device__ __forceinline__ float just_below(float v)
 {
-    constexpr int W = kWide<E>;
-    __shared__ Shared sh;
-    __shared__ std::conditional_t<TOP, TopShared, int> top;
-    const int m = (int)(blockIdx.x / segs), seg = (int)(blockIdx.x % segs), first = seg * VPT * kThreads;
+    if (v == 0.f) return __uint_as_float(0x80000001u);
+    const uint32_t u = __float_as_uint(v);
+    return v == kNone ? v : __uint_as_float(u >> 31 ? u + 1 : u - 1);
+}
+
+template <class E, int VPT, int THREADS, bool TOP>
+__global__ __launch_bounds__(THREADS) void score_kernel(ScoreArgs a, int segs)
+{
+    constexpr int W = kWide<E>, kChunks = VPT / W, kChunk = THREADS * W, kList = kScoreMaxTop * THREADS / kGroups * VPT;
+    __shared__ Shared<THREADS / 64> sh;
+    extern __shared__ u64 top_lds[];
+    const int m = (int)(blockIdx.x / segs), seg = (int)(blockIdx.x % segs), first = seg * VPT * THREADS, tid = threadIdx.x;
     const typename E::T* const row = (const typename E::T*)a.logits + (int64_t)m * a.ld;
     const uint8_t* const allowed = a.allowed ? a.allowed + (int64_t)m * a.allowed_ld : nullptr;
     const int token = a.token ? a.token[m] : -1;
     const bool given = token >= 0 && token < a.V;
     const float mine = given ? logit_of<E>(row, allowed, token) : kNone;
+    const int chunks = min(kChunks, (a.V - first + kChunk - 1) / kChunk);       // that the row has; the same in all threads
     float v[VPT], biggest = kNone;
 #pragma unroll
-    for (int c = 0; c < VPT / W; ++c) load_wide<E>(row, first + (c * kThreads + (int)threadIdx.x) * W, a.V, v + c * W);
+    for (int c = 0; c < kChunks; ++c)
+        if (c < chunks) load_wide<E>(row, first + (c * THREADS + tid) * W, a.V, v + c * W);
 #pragma unroll
-    for (int c = 0; c < VPT / W; ++c) leave_out<E>(allowed, first + (c * kThreads + (int)threadIdx.x) * W, a.V, v + c * W);
+    for (int c = 0; c < kChunks; ++c)
+        if (c < chunks) {
+            leave_out<E>(allowed, first + (c * THREADS + tid) * W, a.V, v + c * W);
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) biggest = fmaxf(biggest, v[i]);
+            for (int i = 0; i < W; ++i) biggest = fmaxf(biggest, v[c * W + i]);
+        }
     const float own = biggest;
-    const auto col_of = [&](int i) { return first + (i / W * kThreads + (int)threadIdx.x) * W + i % W; };
     Part p;
     p.biggest = biggest = group_max(biggest, sh);
     p.sum = p.mean = 0.0;
     int front = 0;
-    if (biggest > kNone) {
-        const Exp e(1.0);
+    const Exponents x(kLog2e, biggest);
+    if (x.usual) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const float d = below(v[i], biggest), x = e(d);
-            p.sum += x;
-            p.mean += x > 0.f ? x * d : 0.f;
-        }
-        if (given)
+        for (int c = 0; c < kChunks; ++c)
+            if (c < chunks) {
+                float sum = 0.f, mean = 0.f;
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) front += v[i] > mine || (v[i] == mine && v[i] > kNone && col_of(i) < token);
+                for (int i = 0; i < W; ++i) {
+                    const float t = x.of(v[c * W + i]), w = __builtin_amdgcn_exp2f(t);
+                    sum += w;
+                    mean = fmaf(w, t, mean);
+                }
+                p.sum += sum;
+                p.mean += mean;
+            }
+        const double scale = exp2(x.c), s = p.sum, t = p.mean;
+        p.sum = scale * (s + x.e * kLn2 * t);
+        p.mean = scale * kLn2 * (t * (1.0 + x.e) + x.c * s);
+    } else if (biggest > kNone) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+            if (c < chunks)
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const float d = below(v[c * W + i], biggest), w = v[c * W + i] > kNone ? far_weight(d, 1.f) : 0.f;
+                    p.sum += w;
+                    p.mean += w > 0.f ? w * d : 0.f;
+                }
     }
-    p.sum = group_add(p.sum, sh);
-    p.mean = group_add(p.mean, sh);
-    p.front = group_add(front, sh);
+    if (given) {
+        // equal logits count in front of the token, so that there the border is just below it; the chunk that holds the token one by one
+        const float before = just_below(mine);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+            if (c < chunks) {
+                const int col = first + (c * THREADS + tid) * W;
+                const float border = mine > kNone && col + W <= token ? before : mine;
+#pragma unroll
+                for (int i = 0; i < W; ++i) front += v[c * W + i] > border;
+                if (mine > kNone && col < token && token < col + W)
+#pragma unroll
+                    for (int i = 0; i < W; ++i) front += v[c * W + i] == mine && col + i < token;
+            }
+    }
+    group_add(p.sum, p.mean, front, sh);
+    p.front = front;
+    TopShared<kList>& top = *(TopShared<kList>*)top_lds;
     if constexpr (TOP) {
         int at = 0;
 #pragma unroll
-        for (int i = VPT - 1; i >= 0; --i) at = v[i] == own ? col_of(i) : at;
-        top_keys(a.top_n, key_of(own, at), top, [&](auto take) {
+        for (int c = kChunks - 1; c >= 0; --c)
+            if (c < chunks)
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) take(key_of(v[i], col_of(i)));
+                for (int i = W - 1; i >= 0; --i) at = v[c * W + i] == own ? first + (c * THREADS + tid) * W + i : at;
+        top_keys<THREADS>(a.top_n, key_of(own, at), top, [&](u64 border, auto take) {
+            const float least = border ? logit_of_key(border) : kNone;
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+                if (c < chunks)
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+                        if (v[c * W + i] >= least) take(key_of(v[c * W + i], first + (c * THREADS + tid) * W + i));
         });
     }
     if (segs == 1) {
-        if constexpr (TOP) finish_row(a, m, p, given, mine, &top);
-        else finish_row(a, m, p, given, mine, nullptr);
+        finish_row(a, m, p, given, mine, TOP ? top.first : nullptr);
         return;
     }
-    if (threadIdx.x == 0) parts_of(a.ws)[blockIdx.x] = p;
+    if (tid == 0) parts_of(a.ws)[blockIdx.x] = p;
     if constexpr (TOP)
-        if ((int)threadIdx.x < a.top_n) keys_of(a.ws, a.M, segs)[(int64_t)blockIdx.x * a.top_n + threadIdx.x] = top.first[threadIdx.x];
+        if (tid < a.top_n) keys_of(a.ws, a.M, segs)[(int64_t)blockIdx.x * a.top_n + tid] = top.first[tid];
 }
 
+constexpr int kMostSegments = 128;          // of a row
+constexpr int kJoinList = kMostSegments * kScoreMaxTop;
 template <class E, bool TOP>
 __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs a, int segs)
 {
-    __shared__ Shared sh;
-    __shared__ std::conditional_t<TOP, TopShared, int> top;
+    __shared__ Shared<kThreads / 64> sh;
+    extern __shared__ u64 top_lds[];
     const int m = blockIdx.x, tid = threadIdx.x;
     Part p = {0.0, 0.0, kNone, 0};
     if (tid < segs) p = parts_of(a.ws)[(int64_t)m * segs + tid];
@@ -310,28 +396,24 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs a, int s
         p.mean = f > 0.0 ? f * (p.mean + p.sum * d) : 0.0;
         p.sum *= f;
     }
-    p.sum = group_add(p.sum, sh);
-    p.mean = group_add(p.mean, sh);
-    p.front = group_add(p.front, sh);
+    group_add(p.sum, p.mean, p.front, sh);
     p.biggest = biggest;
     const int token = a.token ? a.token[m] : -1;
     const bool given = token >= 0 && token < a.V;
     const float mine = given ? logit_of<E>((const typename E::T*)a.logits + (int64_t)m * a.ld, a.allowed ? a.allowed + (int64_t)m * a.allowed_ld : nullptr, token)
                              : kNone;
+    TopShared<kJoinList>& top = *(TopShared<kJoinList>*)top_lds;
     if constexpr (TOP) {
         const u64* const keys = keys_of(a.ws, a.M, segs) + (int64_t)m * segs * a.top_n;
-        const int count = segs * a.top_n;       // at most 64 for each thread
+        const int count = segs * a.top_n;
         u64 most = 0;
         for (int i = tid; i < count; i += kThreads) most = max(most, keys[i]);
-        top_keys(a.top_n, most, top, [&](auto take) {
+        top_keys<kThreads>(a.top_n, most, top, [&](u64, auto take) {
             for (int i = tid; i < count; i += kThreads) take(keys[i]);
         });
-        finish_row(a, m, p, given, mine, &top);
-    } else {
-        finish_row(a, m, p, given, mine, nullptr);
     }
+    finish_row(a, m, p, given, mine, TOP ? top.first : nullptr);
 }
-static_assert(kMostSegments * kScoreMaxTop <= 64 * kThreads, "");
 
 template <class E>
 __global__ __launch_bounds__(kThreads) void score_gradient_kernel(ScoreArgs a, int segs)
@@ -342,24 +424,43 @@ __global__ __launch_bounds__(kThreads) void score_gradient_kernel(ScoreArgs a, i
     typename E::T* const to = (typename E::T*)a.dlogits + (int64_t)m * a.dlogits_ld;
     const uint8_t* const allowed = a.allowed ? a.allowed + (int64_t)m * a.allowed_ld : nullptr;
     const float* const stats = a.stats + 4 * (int64_t)m;
-    const float biggest = stats[0], log_sum = stats[1], entropy = stats[2], per_sum = stats[3];
+    const float biggest = stats[0], log_sum = stats[1], entropy = stats[2];
     const int token = a.token ? a.token[m] : -1;
     const bool given = token >= 0 && token < a.V;
     const float dlogprob = given && a.dlogprob ? a.dlogprob[m] : 0.f, dentropy = a.dentropy ? a.dentropy[m] : 0.f;
-    const Exp e(1.0);
+    const Exponents x(kLog2e, biggest);
+    // log p = ln 2 (t + c) - log S up to e t, which is below a step of it; p = 2^t 2^c / S; bracket = constant + t slope
+    const float per_sum = (float)(exp2(x.c) * (double)stats[3]);
+    const float slope = dentropy * (float)kLn2, constant = dlogprob + dentropy * (float)(kLn2 * x.c - (double)log_sum + (double)entropy);
+    if (x.usual) {
 #pragma unroll 2
+        for (int col = first + (int)threadIdx.x * W; col < end; col += kThreads * W) {
+            float v[W], g[W];
+            load_wide<E>(row, col, a.V, v);
+            leave_out<E>(allowed, col, a.V, v);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float t = x.of(v[i]);
+                g[i] = -(__builtin_amdgcn_exp2f(t) * per_sum) * fmaf(t, slope, constant);
+            }
+            if (col <= token && token < col + W)
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+                    if (col + i == token && v[i] > kNone) g[i] += dlogprob;
+            store_wide<E>(to, col, a.V, g);
+        }
+        return;
+    }
     for (int col = first + (int)threadIdx.x * W; col < end; col += kThreads * W) {
         float v[W];
         load_wide<E>(row, col, a.V, v);
         leave_out<E>(allowed, col, a.V, v);
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            const float d = below(v[i], biggest), p = e(d) * per_sum;
-            float g = dlogprob;
-            if (a.dentropy) g = p > 0.f ? fmaf(dentropy, d - log_sum + entropy, g) : 0.f;
-            g *= -p;
-            if (col + i == token) g += dlogprob;
-            v[i] = v[i] > kNone ? g : 0.f;
+            const bool exists = v[i] > kNone;
+            const float d = exists ? below(v[i], biggest) : kNone, p = exists ? far_weight(d, 1.f) * stats[3] : 0.f;
+            const float bracket = p > 0.f ? fmaf(dentropy, d - log_sum + entropy, dlogprob) : 0.f;
+            v[i] = exists ? (col + i == token ? dlogprob : 0.f) - p * bracket : 0.f;
         }
         store_wide<E>(to, col, a.V, v);
     }
@@ -370,183 +471,260 @@ __global__ __launch_bounds__(kThreads) void score_gradient_kernel(ScoreArgs a, i
 struct RestPart {
     double sum;             // of exp((l - biggest) / heat) over the words outside the list
     float biggest;
+    int twice;              // a word may stand in the list twice
 };
+constexpr int kOfLane = kDistillMaxTop / 64;
 
-// Word j of a row's list.  A word that is outside the vocabulary, or an earlier one again, does not count.
+// Word j of a row's list, as far as it counts: one that is outside the vocabulary, or an earlier one again, does not.
 struct Listed {
     int token;
     bool counts;
     double logit;           // the teacher's, over the heat
 };
-__device__ __forceinline__ Listed listed(const DistillArgs& a, int m, int* tokens)
+__device__ __forceinline__ Listed listed(const DistillArgs& a, int m, int j)
 {
-    const int j = threadIdx.x;
     Listed w = {-1, false, 0.0};
     if (j < a.K) {
         w.token = a.top_token[m * a.top_token_ld + j];
         w.counts = w.token >= 0 && w.token < a.V;
         w.logit = (double)a.top_logit[m * a.top_logit_ld + j] / (double)a.temperature;
     }
-    tokens[j] = w.token;
-    __syncthreads();
-    for (int i = 0; i < j && j < a.K; ++i) w.counts &= tokens[i] != w.token;
     return w;
 }
-__device__ __forceinline__ float group_max_or_nan(float v, Shared& sh)
+// looks through the list in front of word j
+__device__ __forceinline__ bool again(const DistillArgs& a, int m, int j, int token)
 {
-    const double n = group_add(v != v ? 1.0 : 0.0, sh);
-    v = group_max(v, sh);
-    return n > 0.0 ? __builtin_nanf("") : v;
+    bool found = false;
+    for (int i = 0; i < j; ++i) found |= a.top_token[m * a.top_token_ld + i] == token;
+    return found;
+}
+// the largest, NaN where one is
+__device__ __forceinline__ float wave_max_or_nan(float v)
+{
+    const bool bad = __ballot(v != v) != 0;
+    v = wave_max(v);
+    return bad ? __builtin_nanf("") : v;
 }
 
+// The loss of a row, by one wave: lane i has words i, i + 64, ..
 template <class E>
-__device__ void finish_loss(const DistillArgs& a, int m, RestPart rest, Shared& sh, int* tokens)
+__device__ void finish_loss(const DistillArgs& a, int m, const RestPart& rest)
 {
-    const Listed w = listed(a, m, tokens);
+    const int lane = threadIdx.x & 63;
     const double heat = a.temperature, per = 1.0 / heat;
-    const float l = w.counts ? E::load((const typename E::T*)a.logits + (int64_t)m * a.ld + w.token) : kNone;
-    const float biggest = fmaxf(group_max(l, sh), rest.biggest);
+    const typename E::T* const row = (const typename E::T*)a.logits + (int64_t)m * a.ld;
+    Listed w[kOfLane];
+    float l[kOfLane], biggest = kNone, most = kNone;
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < kOfLane; ++i) w[i] = listed(a, m, lane + 64 * i);
+    if (rest.twice)
+#pragma unroll
+        for (int i = 0; i < kOfLane; ++i) w[i].counts = w[i].counts && !again(a, m, lane + 64 * i, w[i].token);
+#pragma unroll
+    for (int i = 0; i < kOfLane; ++i) {
+        l[i] = w[i].counts ? E::load(row + w[i].token) : kNone;
+        biggest = fmaxf(biggest, l[i]);
+        count += w[i].counts;
+    }
+    biggest = fmaxf(wave_max(biggest), rest.biggest);
+    count = wave_add(count);
     // the student
-    const double d = (double)below(l, biggest) * per;
-    const double in_list = group_add(w.counts ? exp(d) : 0.0, sh);
-    const double outside = rest.sum > 0.0 || rest.sum != rest.sum ? rest.sum * exp((double)below(rest.biggest, biggest) * per) : 0.0;
-    const double sum = biggest == kNone ? (double)__builtin_nanf("") : in_list + outside, log_sum = log(sum);      // no logits: 0 / 0
+    const bool some_rest = rest.sum > 0.0 || rest.sum != rest.sum;
+    const double rest_d = (double)below(rest.biggest, biggest) * per;
+    double d[kOfLane], in_list = 0.0;
+#pragma unroll
+    for (int i = 0; i < kOfLane; ++i) {
+        d[i] = (double)below(l[i], biggest) * per;
+        in_list += w[i].counts ? exp(d[i]) : 0.0;
+    }
+    in_list = wave_add(in_list);
+    const double sum = biggest == kNone ? (double)__builtin_nanf("") : in_list + (some_rest ? rest.sum * exp(rest_d) : 0.0);        // no logits: 0 / 0
+    const double log_sum = log(sum);
     // the log of the share of what is outside, which may be too small for a number of its own
-    const double log_rest = rest.sum > 0.0 || rest.sum != rest.sum ? log(rest.sum) + (double)below(rest.biggest, biggest) * per : (double)kNone;
+    const double log_rest = some_rest ? log(rest.sum) + rest_d : (double)kNone;
     // the teacher
-    const int count = group_add((int)w.counts, sh);
-    double norm = 0.0, t_rest = 0.0, log_t = (double)kNone, log_norm = 0.0;
+    double norm = 0.0, log_norm = 0.0, t_rest = 0.0, in_teacher = 0.0, loss = 0.0;
     if (a.teacher_lse) {
         norm = a.teacher_lse[m];
-        log_t = w.logit - norm;
     } else {
-        const float most = group_max_or_nan(w.counts ? (float)(w.logit * heat) : kNone, sh);
-        log_norm = log(group_add(w.counts ? exp(w.logit - (double)most * per) : 0.0, sh));
-        log_t = w.logit - (double)most * per - log_norm;
+#pragma unroll
+        for (int i = 0; i < kOfLane; ++i) most = w[i].counts && !(w[i].logit * heat <= (double)most) ? (float)(w[i].logit * heat) : most;
+        norm = (double)wave_max_or_nan(most) * per;
+        double z = 0.0;
+#pragma unroll
+        for (int i = 0; i < kOfLane; ++i) z += w[i].counts ? exp(w[i].logit - norm) : 0.0;
+        log_norm = log(wave_add(z));
     }
-    const double t = w.counts ? exp(log_t) : 0.0;
+#pragma unroll
+    for (int i = 0; i < kOfLane; ++i) {
+        const double log_t = w[i].logit - norm - log_norm, t = w[i].counts ? exp(log_t) : 0.0;
+        in_teacher += t;
+        loss += w[i].counts && t != 0.0 ? t * (log_t - (d[i] - log_sum)) : 0.0;
+    }
+    loss = wave_add(loss);
     if (a.teacher_lse) {
-        const double left = 1.0 - group_add(t, sh);
+        const double left = 1.0 - wave_add(in_teacher);
         t_rest = left < 0.0 ? 0.0 : left;
     }
-    double loss = group_add(w.counts && t != 0.0 ? t * (log_t - (d - log_sum)) : 0.0, sh);
-    if (threadIdx.x != 0) return;
+    if (lane != 0) return;
     // what a word outside the list gets, as a factor of its s; where that would leave the range of fp32 the logarithm of what is
     // taken from it over exp(d) instead, which is then above 1
     double factor = 1.0;
     if (!a.teacher_lse && count == 0) {
         factor = loss = 0.0;        // no teacher in this row
     } else if (t_rest != 0.0) {
-        loss += t_rest * (log(t_rest) - (log_rest - log_sum));
         const double r = log(t_rest) - (log_rest - log_sum);
+        loss += t_rest * r;
         factor = r < 40.0 ? 1.0 - exp(r) : r != r ? r : log(t_rest) - log_rest;
     }
     if (a.loss) a.loss[m] = (float)(loss * heat * heat);
     if (a.stats) {
         float* const s = a.stats + 4 * (int64_t)m;
         s[0] = biggest;
-        s[1] = (float)(1.0 / sum);
+        s[1] = (float)(rest.twice ? -1.0 / sum : 1.0 / sum);       // its sign says whether a word may stand in the list twice
         s[2] = (float)factor;
         s[3] = (float)log_norm;
     }
 }
 
-template <class E, int VPT>
-__global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a, int segs)
+template <class E, int VPT, int THREADS>
+__global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int segs)
 {
-    constexpr int W = kWide<E>;
-    __shared__ Shared sh;
-    __shared__ int tokens[kThreads];
-    __shared__ uint32_t in_list[VPT * kThreads / 32];
-    const int m = (int)(blockIdx.x / segs), seg = (int)(blockIdx.x % segs), first = seg * VPT * kThreads, tid = threadIdx.x;
+    constexpr int W = kWide<E>, kChunks = VPT / W, kChunk = THREADS * W;
+    __shared__ Shared<THREADS / 64> sh;
+    __shared__ uint32_t in_list[VPT * THREADS / 32];
+    __shared__ int twice;
+    const int m = (int)(blockIdx.x / segs), seg = (int)(blockIdx.x % segs), first = seg * VPT * THREADS, tid = threadIdx.x;
     const typename E::T* const row = (const typename E::T*)a.logits + (int64_t)m * a.ld;
-    for (int i = tid; i < VPT * kThreads / 32; i += kThreads) in_list[i] = 0;
+    const int chunks = min(kChunks, (a.V - first + kChunk - 1) / kChunk);
     float v[VPT], biggest = kNone;
+    const int word = tid < a.K ? a.top_token[m * a.top_token_ld + tid] : -1, at = word - first;
 #pragma unroll
-    for (int c = 0; c < VPT / W; ++c) load_wide<E>(row, first + (c * kThreads + tid) * W, a.V, v + c * W);
+    for (int c = 0; c < kChunks; ++c)
+        if (c < chunks) load_wide<E>(row, first + (c * THREADS + tid) * W, a.V, v + c * W);
+    for (int i = tid; i < VPT * THREADS / 32; i += THREADS) in_list[i] = 0;
+    if (tid == 0) twice = 0;
     __syncthreads();
-    if (tid < a.K) {
-        const int at = a.top_token[m * a.top_token_ld + tid] - first;
-        if (at >= 0 && at < VPT * kThreads) atomicOr(in_list + at / 32, 1u << at % 32);
-    }
+    if (word >= 0 && at >= 0 && at < VPT * THREADS && atomicOr(in_list + at / 32, 1u << at % 32) >> at % 32 & 1) twice = 1;
     __syncthreads();
 #pragma unroll
-    for (int c = 0; c < VPT / W; ++c) {
-        const int at = (c * kThreads + tid) * W;
-        const uint32_t bits = in_list[at / 32] >> at % 32;
+    for (int c = 0; c < kChunks; ++c)
+        if (c < chunks) {
+            const int place = (c * THREADS + tid) * W;
+            const uint32_t bits = in_list[place / 32] >> place % 32;
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            v[c * W + i] = bits >> i & 1 ? kNone : v[c * W + i];
-            biggest = fmaxf(biggest, v[c * W + i]);
+            for (int i = 0; i < W; ++i) {
+                v[c * W + i] = bits >> i & 1 ? kNone : v[c * W + i];
+                biggest = fmaxf(biggest, v[c * W + i]);
+            }
         }
-    }
-    RestPart p;
-    p.biggest = group_max(biggest, sh);
-    double sum = 0.0;
-    const Exp e(1.0 / (double)a.temperature);
+    RestPart p = {0.0, group_max(biggest, sh), twice};
+    double unused = 0.0;
+    int none = 0;
+    const Exponents x(kLog2e / (double)a.temperature, p.biggest);
+    if (x.usual) {
+        double mean = 0.0;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const float x = e(below(v[i], p.biggest));
-        sum += v[i] == kNone ? 0.f : x;
+        for (int c = 0; c < kChunks; ++c)
+            if (c < chunks) {
+                float sum = 0.f, t_sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const float t = x.or_nan(v[c * W + i]), w = __builtin_amdgcn_exp2f(t);
+                    sum += w;
+                    t_sum = fmaf(w, t, t_sum);
+                }
+                p.sum += sum;
+                mean += t_sum;
+            }
+        p.sum = exp2(x.c) * (p.sum + x.e * kLn2 * mean);
+    } else {
+        const float per = 1.f / a.temperature;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+            if (c < chunks)
+#pragma unroll
+                for (int i = 0; i < W; ++i) p.sum += v[c * W + i] == kNone ? 0.f : far_weight(below(v[c * W + i], p.biggest), per);
     }
-    p.sum = group_add(sum, sh);
-    if (segs == 1) finish_loss<E>(a, m, p, sh, tokens);
-    else if (tid == 0) ((RestPart*)a.ws)[blockIdx.x] = p;
+    group_add(p.sum, unused, none, sh);
+    if (segs > 1) {
+        if (tid == 0) ((RestPart*)a.ws)[blockIdx.x] = p;
+    } else if (tid < 64) {
+        finish_loss<E>(a, m, p);
+    }
 }
 
 template <class E>
 __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a, int segs)
 {
-    __shared__ Shared sh;
-    __shared__ int tokens[kThreads];
+    __shared__ Shared<kThreads / 64> sh;
     const int m = blockIdx.x;
-    RestPart p = {0.0, kNone};
+    RestPart p = {0.0, kNone, 0};
     if ((int)threadIdx.x < segs) p = ((const RestPart*)a.ws)[(int64_t)m * segs + threadIdx.x];
     const float biggest = group_max(p.biggest, sh);
     const bool some = p.sum > 0.0 || p.sum != p.sum;
-    p.sum = group_add(some ? p.sum * exp((double)below(p.biggest, biggest) / (double)a.temperature) : 0.0, sh);
+    double unused = 0.0;
+    p.sum = some ? p.sum * exp((double)below(p.biggest, biggest) / (double)a.temperature) : 0.0;
+    group_add(p.sum, unused, p.twice, sh);
     p.biggest = biggest;
-    finish_loss<E>(a, m, p, sh, tokens);
+    if (threadIdx.x < 64) finish_loss<E>(a, m, p);
 }
 
 template <class E>
 __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs a, int segs)
 {
     constexpr int W = kWide<E>;
-    __shared__ Shared sh;
-    __shared__ int tokens[kThreads];
+    __shared__ Shared<kThreads / 64> sh;
     const int m = (int)(blockIdx.x / segs), first = (int)(blockIdx.x % segs) * kSweep, end = min(first + kSweep, a.V);
     const typename E::T* const row = (const typename E::T*)a.logits + (int64_t)m * a.ld;
     typename E::T* const to = (typename E::T*)a.dlogits + (int64_t)m * a.dlogits_ld;
     const float* const stats = a.stats + 4 * (int64_t)m;
-    const float biggest = stats[0], per_sum = stats[1], factor = stats[2];
+    const float biggest = stats[0], factor = stats[2];
+    const double per_sum = fabs((double)stats[1]), per = 1.0 / (double)a.temperature;
     const float scale = a.dloss[m] * a.temperature;
-    const Listed w = listed(a, m, tokens);
-    const double per = 1.0 / (double)a.temperature;
-    const Exp e(per), one(1.0);
+    Listed w = listed(a, m, threadIdx.x);
+    if (stats[1] < 0.f) w.counts = w.counts && !again(a, m, threadIdx.x, w.token);
     // a word of the list that lies in this segment: its logit is read in front of all writes, which may be to the same place
     const bool here = w.counts && w.token >= first && w.token < end;
     float mine = 0.f;
     double log_t = w.logit;
-    if (a.teacher_lse) log_t -= a.teacher_lse[m];
-    else log_t -= (double)group_max_or_nan(w.counts ? (float)(w.logit * (double)a.temperature) : kNone, sh) * per + (double)stats[3];
+    if (a.teacher_lse) {
+        log_t -= a.teacher_lse[m];
+    } else {
+        const float z = w.counts ? (float)(w.logit * (double)a.temperature) : kNone;
+        const bool bad = __syncthreads_or(z != z);
+        const float most = group_max(z, sh);
+        log_t -= (bad ? (double)__builtin_nanf("") : (double)most * per) + (double)stats[3];
+    }
     if (here) {
-        const double s = exp((double)below(E::load(row + w.token), biggest) * per) * (double)per_sum;
+        const double s = exp((double)below(E::load(row + w.token), biggest) * per) * per_sum;
         mine = (float)((double)scale * (s - exp(log_t)));
     }
     __syncthreads();
-    const float kept = scale * (factor > 1.f ? 1.f : factor) * per_sum, fper = (float)per;
+    const Exponents x(kLog2e * per, biggest);
+    const bool far_rest = factor > 1.f || !x.usual;
+    const float kept = (float)((double)scale * (factor > 1.f ? 1.0 : (double)factor) * per_sum * (x.usual ? exp2(x.c) : 1.0)), fper = (float)per;
+    if (!far_rest) {
 #pragma unroll 2
-    for (int col = first + (int)threadIdx.x * W; col < end; col += kThreads * W) {
-        float v[W];
-        load_wide<E>(row, col, a.V, v);
+        for (int col = first + (int)threadIdx.x * W; col < end; col += kThreads * W) {
+            float v[W];
+            load_wide<E>(row, col, a.V, v);
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const float d = below(v[i], biggest);
-            v[i] = kept * e(d);
-            if (factor > 1.f) v[i] -= scale * one(fminf(fmaf(d, fper, factor), 0.f));
+            for (int i = 0; i < W; ++i) v[i] = kept * __builtin_amdgcn_exp2f(x.or_nan(v[i]));
+            store_wide<E>(to, col, a.V, v);
         }
-        store_wide<E>(to, col, a.V, v);
+    } else {
+        for (int col = first + (int)threadIdx.x * W; col < end; col += kThreads * W) {
+            float v[W];
+            load_wide<E>(row, col, a.V, v);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float d = below(v[i], biggest) * fper;
+                v[i] = (x.usual ? kept * __builtin_amdgcn_exp2f(x.or_nan(v[i])) : kept * expf(d)) - (factor > 1.f ? scale * expf(fminf(d + factor, 0.f)) : 0.f);
+            }
+            store_wide<E>(to, col, a.V, v);
+        }
     }
     __syncthreads();
     if (here) E::store(to + w.token, mine);
@@ -554,55 +732,85 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
 
 // ---- host
 
-int segments(int V, int per_thread) { return (V + per_thread * kThreads - 1) / (per_thread * kThreads); }
-// Logits of a thread: as few as keep 1024 workgroups busy, as many as leave a row 64 segments
-int per_thread(int M, int V)
+// How rows are laid over workgroups
+struct Lay {
+    int threads, per_thread, segs;
+};
+Lay lay_of(int M, int V)
 {
-    int n = 8;
-    while (n < 64 && ((int64_t)M * segments(V, n) > 1024 || segments(V, n) > kMostSegments) && segments(V, n) > 1) n *= 2;
-    return n;
+    // many short rows: four waves to one, whose barriers cost least; else sixteen waves, so that a row of up to 65 536 is one launch
+    Lay l;
+    l.threads = M >= 512 && V <= 16384 ? 256 : 1024;
+    l.per_thread = 8;
+    while (l.per_thread < 64 && l.threads * l.per_thread < V) l.per_thread *= 2;
+    // longer rows in segments: of few rows, shorter ones
+    l.segs = (V + l.threads * l.per_thread - 1) / (l.threads * l.per_thread);
+    if (l.segs > 1)
+        while (l.per_thread > 8 && (int64_t)M * l.segs < 256) {
+            l.per_thread /= 2;
+            l.segs = (V + l.threads * l.per_thread - 1) / (l.threads * l.per_thread);
+        }
+    return l;
 }
+static_assert(kSampleMaxVocabulary <= kMostSegments * 8 * 1024 && kMostSegments <= kThreads, "");
 
-template <class E, int VPT>
-hipError_t score(const ScoreArgs& a, hipStream_t s)
+template <class E, int VPT, int THREADS, bool TOP>
+hipError_t score(const ScoreArgs& a, int segs, hipStream_t s)
 {
-    const int segs = segments(a.V, VPT);
-    const dim3 grid((unsigned)((int64_t)a.M * segs)), block(kThreads);
-    if (a.top_n) hipLaunchKernelGGL((score_kernel<E, VPT, true>), grid, block, 0, s, a, segs);
-    else hipLaunchKernelGGL((score_kernel<E, VPT, false>), grid, block, 0, s, a, segs);
+    const dim3 grid((unsigned)((int64_t)a.M * segs));
+    const size_t lds = TOP ? sizeof(TopShared<kScoreMaxTop * THREADS / kGroups * VPT>) : 0;
+    const auto kernel = score_kernel<E, VPT, THREADS, TOP>;
+    hipError_t e = TOP ? allow_dynamic_lds((const void*)kernel, lds) : hipSuccess;
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, grid, dim3(THREADS), lds, s, a, segs);
     if (segs > 1) {
-        if (a.top_n) hipLaunchKernelGGL((score_join_kernel<E, true>), dim3(a.M), block, 0, s, a, segs);
-        else hipLaunchKernelGGL((score_join_kernel<E, false>), dim3(a.M), block, 0, s, a, segs);
+        const auto join = score_join_kernel<E, TOP>;
+        const size_t join_lds = TOP ? sizeof(TopShared<kJoinList>) : 0;
+        e = TOP ? allow_dynamic_lds((const void*)join, join_lds) : hipSuccess;
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(join, dim3(a.M), dim3(kThreads), join_lds, s, a, segs);
     }
     return hipGetLastError();
 }
-template <class E, int VPT>
-hipError_t distill(const DistillArgs& a, hipStream_t s)
+template <class E, int VPT, int THREADS>
+hipError_t distill(const DistillArgs& a, int segs, hipStream_t s)
 {
-    const int segs = segments(a.V, VPT);
-    hipLaunchKernelGGL((distill_kernel<E, VPT>), dim3((unsigned)((int64_t)a.M * segs)), dim3(kThreads), 0, s, a, segs);
+    hipLaunchKernelGGL((distill_kernel<E, VPT, THREADS>), dim3((unsigned)((int64_t)a.M * segs)), dim3(THREADS), 0, s, a, segs);
     if (segs > 1) hipLaunchKernelGGL((distill_join_kernel<E>), dim3(a.M), dim3(kThreads), 0, s, a, segs);
     return hipGetLastError();
+}
+template <class E, int THREADS, bool TOP>
+hipError_t score_by(const ScoreArgs& a, const Lay& l, hipStream_t s)
+{
+    switch (l.per_thread) {
+    case 8: return score<E, 8, THREADS, TOP>(a, l.segs, s);
+    case 16: return score<E, 16, THREADS, TOP>(a, l.segs, s);
+    case 32: return score<E, 32, THREADS, TOP>(a, l.segs, s);
+    default: return score<E, 64, THREADS, TOP>(a, l.segs, s);
+    }
 }
 template <class E>
 hipError_t score_of(const ScoreArgs& a, hipStream_t s)
 {
-    switch (per_thread(a.M, a.V)) {
-    case 8: return score<E, 8>(a, s);
-    case 16: return score<E, 16>(a, s);
-    case 32: return score<E, 32>(a, s);
-    default: return score<E, 64>(a, s);
+    Lay l = lay_of(a.M, a.V);
+    if (l.threads == 256) return a.top_n ? score_by<E, 256, true>(a, l, s) : score_by<E, 256, false>(a, l, s);
+    return a.top_n ? score_by<E, 1024, true>(a, l, s) : score_by<E, 1024, false>(a, l, s);
+}
+template <class E, int THREADS>
+hipError_t distill_by(const DistillArgs& a, const Lay& l, hipStream_t s)
+{
+    switch (l.per_thread) {
+    case 8: return distill<E, 8, THREADS>(a, l.segs, s);
+    case 16: return distill<E, 16, THREADS>(a, l.segs, s);
+    case 32: return distill<E, 32, THREADS>(a, l.segs, s);
+    default: return distill<E, 64, THREADS>(a, l.segs, s);
     }
 }
 template <class E>
 hipError_t distill_of(const DistillArgs& a, hipStream_t s)
 {
-    switch (per_thread(a.M, a.V)) {
-    case 8: return distill<E, 8>(a, s);
-    case 16: return distill<E, 16>(a, s);
-    case 32: return distill<E, 32>(a, s);
-    default: return distill<E, 64>(a, s);
-    }
+    const Lay l = lay_of(a.M, a.V);
+    return l.threads == 256 ? distill_by<E, 256>(a, l, s) : distill_by<E, 1024>(a, l, s);
 }
 
 }  // namespace
@@ -610,16 +818,17 @@ hipError_t distill_of(const DistillArgs& a, hipStream_t s)
 // a grid's threads have to stay under 2^32
 bool score_fits(int M, int V)
 {
-    return M >= 0 && V >= 1 && V <= kSampleMaxVocabulary && M < (1 << 22) && (int64_t)M * ((V + kSweep - 1) / kSweep) < (1 << 24);
+    return M >= 0 && V >= 1 && V <= kSampleMaxVocabulary && M < (1 << 22) && (int64_t)M * ((V + kSweep - 1) / kSweep) < (1 << 24) &&
+           (int64_t)M * lay_of(M, V).segs * lay_of(M, V).threads < ((int64_t)1 << 32);
 }
 size_t score_workspace_bytes(int M, int V, int top_n)
 {
-    const int segs = segments(V, per_thread(M, V));
+    const int segs = lay_of(M, V).segs;
     return std::max<size_t>(256, segs == 1 ? 0 : (size_t)M * segs * (sizeof(Part) + sizeof(u64) * top_n));
 }
 size_t distill_workspace_bytes(int M, int V)
 {
-    const int segs = segments(V, per_thread(M, V));
+    const int segs = lay_of(M, V).segs;
     return std::max<size_t>(256, segs == 1 ? 0 : (size_t)M * segs * sizeof(RestPart));
 }
 
