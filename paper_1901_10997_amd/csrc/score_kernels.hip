@@ -287,14 +287,14 @@ __global__ __launch_bounds__(THREADS) void score_kernel(ScoreArgs a, int segs)
     const int m = (int)(blockIdx.x / segs), seg = (int)(blockIdx.x % segs), first = seg * VPT * THREADS, tid = threadIdx.x;
     const typename E::T* const row = (const typename E::T*)a.logits + (int64_t)m * a.ld;
     const uint8_t* const allowed = a.allowed ? a.allowed + (int64_t)m * a.allowed_ld : nullptr;
-    const int token = a.token ? a.token[m] : -1;
-    const bool given = token >= 0 && token < a.V;
-    const float mine = given ? logit_of<E>(row, allowed, token) : kNone;
     const int chunks = min(kChunks, (a.V - first + kChunk - 1) / kChunk);       // that the row has; the same in all threads
     float v[VPT], biggest = kNone;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
         if (c < chunks) load_wide<E>(row, first + (c * THREADS + tid) * W, a.V, v + c * W);
+    const int token = a.token ? a.token[m] : -1;        // its logit is a second wait, behind the row's
+    const bool given = token >= 0 && token < a.V;
+    const float mine = given ? logit_of<E>(row, allowed, token) : kNone;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
         if (c < chunks) {
@@ -518,6 +518,7 @@ __device__ void finish_loss(const DistillArgs& a, int m, const RestPart& rest)
     int count = 0;
 #pragma unroll
     for (int i = 0; i < kOfLane; ++i) w[i] = listed(a, m, lane + 64 * i);
+    const int turns = (a.K + 63) / 64;          // the same in all lanes
     if (rest.twice)
 #pragma unroll
         for (int i = 0; i < kOfLane; ++i) w[i].counts = w[i].counts && !again(a, m, lane + 64 * i, w[i].token);
@@ -535,6 +536,7 @@ __device__ void finish_loss(const DistillArgs& a, int m, const RestPart& rest)
     double d[kOfLane], in_list = 0.0;
 #pragma unroll
     for (int i = 0; i < kOfLane; ++i) {
+        if (i >= turns) continue;
         d[i] = (double)below(l[i], biggest) * per;
         in_list += w[i].counts ? exp(d[i]) : 0.0;
     }
@@ -553,11 +555,13 @@ __device__ void finish_loss(const DistillArgs& a, int m, const RestPart& rest)
         norm = (double)wave_max_or_nan(most) * per;
         double z = 0.0;
 #pragma unroll
-        for (int i = 0; i < kOfLane; ++i) z += w[i].counts ? exp(w[i].logit - norm) : 0.0;
+        for (int i = 0; i < kOfLane; ++i)
+            if (i < turns) z += w[i].counts ? exp(w[i].logit - norm) : 0.0;
         log_norm = log(wave_add(z));
     }
 #pragma unroll
     for (int i = 0; i < kOfLane; ++i) {
+        if (i >= turns) continue;
         const double log_t = w[i].logit - norm - log_norm, t = w[i].counts ? exp(log_t) : 0.0;
         in_teacher += t;
         loss += w[i].counts && t != 0.0 ? t * (log_t - (d[i] - log_sum)) : 0.0;
