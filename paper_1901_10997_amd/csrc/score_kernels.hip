@@ -66,18 +66,60 @@ struct Exponents {
 // exp(scale d) for d <= 0, rows that are not usual; NaN stays
 __device__ __forceinline__ float far_weight(float d, float scale) { return expf(d * scale); }
 
+// Over the 64 lanes, in every lane, by moves between registers: neighbour, other pair of the quad, half-row mirror, row mirror, then
+// the two rows of a half and the two halves.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+}
+template <int CTRL, class T>
+__device__ __forceinline__ T moved_by(T v)
+{
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, moved<CTRL>(__builtin_bit_cast(uint32_t, v)));
+    } else {
+        const u32x2v w = __builtin_bit_cast(u32x2v, v);
+        return __builtin_bit_cast(T, (u32x2v){moved<CTRL>(w[0]), moved<CTRL>(w[1])});
+    }
+}
+// both of what lanes a row (ROWS) or a half apart hold
+template <bool ROWS, class T>
+__device__ __forceinline__ void both_of(T v, T& a, T& b)
+{
+    const auto swap = [](uint32_t x) { return ROWS ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false); };
+    if constexpr (sizeof(T) == 4) {
+        const auto s = swap(__builtin_bit_cast(uint32_t, v));
+        a = __builtin_bit_cast(T, (uint32_t)s[0]);
+        b = __builtin_bit_cast(T, (uint32_t)s[1]);
+    } else {
+        const u32x2v w = __builtin_bit_cast(u32x2v, v);
+        const auto lo = swap(w[0]), hi = swap(w[1]);
+        a = __builtin_bit_cast(T, (u32x2v){(uint32_t)lo[0], (uint32_t)hi[0]});
+        b = __builtin_bit_cast(T, (u32x2v){(uint32_t)lo[1], (uint32_t)hi[1]});
+    }
+}
+template <class T, class F>
+__device__ __forceinline__ T wave_join(T v, F join)
+{
+    v = join(v, moved_by<0xB1>(v));
+    v = join(v, moved_by<0x4E>(v));
+    v = join(v, moved_by<0x141>(v));
+    v = join(v, moved_by<0x140>(v));
+    T a, b;
+    both_of<true>(v, a, b);
+    v = join(a, b);
+    both_of<false>(v, a, b);
+    return join(a, b);
+}
 __device__ __forceinline__ float wave_max(float v)
 {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-    return v;
+    return wave_join(v, [](float a, float b) { return fmaxf(a, b); });
 }
 template <class T>
 __device__ __forceinline__ T wave_add(T v)
 {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
-    return v;
+    return wave_join(v, [](T a, T b) { return a + b; });
 }
 // over the workgroup, in every thread
 template <int WAVES>
@@ -341,20 +383,31 @@ __global__ __launch_bounds__(THREADS) void score_kernel(ScoreArgs a, int segs)
             if (c < chunks) mask[c].load(allowed, first + (c * THREADS + tid) * W, a.V);
     float v[VPT], biggest = kNone;
     const auto column = [&](int c) { return Piece<E>::column(first + (c * THREADS + tid) * W, a.V); };
-    const int token = a.token ? a.token[m] : -1;        // its logit is a second wait, behind the row's
+    const int token = a.token ? a.token[m] : -1;
     const bool given = token >= 0 && token < a.V;
-    const float mine = given ? logit_of<E>(row, allowed, token) : kNone;
+    // the given token's logit: from the thread that holds it, or where that is in another segment from memory
+    __shared__ float given_logit;
+    float mine = kNone;
+    if (given && (token < first || token >= first + kChunks * kChunk)) mine = logit_of<E>(row, allowed, token);
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
         if (c < chunks) {
             piece[c].take(first + (c * THREADS + tid) * W, a.V, first + (c + 1) * kChunk <= a.V, v + c * W);
             if (allowed) mask[c].apply(v + c * W);
+            const int place = token - first - (c * THREADS + tid) * W;
+            if (given && place >= 0 && place < W) {
+                const int shift = first + (c * THREADS + tid) * W - column(c);
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+                    if (i == place + shift) given_logit = v[c * W + i] == v[c * W + i] ? v[c * W + i] : kNone;
+            }
 #pragma unroll
             for (int i = 0; i < W; ++i) biggest = fmaxf(biggest, v[c * W + i]);
         }
     const float own = biggest;
     Part p;
     p.biggest = biggest = group_max(biggest, sh);
+    if (given && token >= first && token < first + kChunks * kChunk) mine = given_logit;
     p.sum = p.mean = 0.0;
     int front = 0;
     const Exponents x(kLog2e, biggest);
@@ -809,9 +862,10 @@ struct Lay {
 };
 Lay lay_of(int M, int V)
 {
-    // many short rows: four waves to one, whose barriers cost least; else sixteen waves, so that a row of up to 65 536 is one launch
+    // many rows: four waves to a row or a segment, whose waits others fill (2048 rows of 32 000 bf16 in two segments and joined 50 us, one to
+    // sixteen waves 65); else sixteen, so that a row of up to 65 536 is one launch
     Lay l;
-    l.threads = M >= 512 && V <= 16384 ? 256 : 1024;
+    l.threads = M >= 512 ? 256 : 1024;
     l.per_thread = 8;
     while (l.per_thread < 64 && l.threads * l.per_thread < V) l.per_thread *= 2;
     // longer rows in segments: of few rows, shorter ones
