@@ -273,6 +273,7 @@ __device__ __forceinline__ int token_of_key(u64 key) { return (int)~(uint32_t)ke
 template <int LIST>
 struct TopShared {
     u64 most[kGroups];
+    int front[kGroups];     // groups that are in front of each
     u64 list[LIST];
     u64 first[kScoreMaxTop];
     u64 border;
@@ -294,13 +295,20 @@ __device__ __forceinline__ void top_keys(int n, u64 most, TopShared<LIST>& sh, E
         sh.count = 0;
     }
     if (tid < n) sh.first[tid] = 0;
+    if (tid < kGroups) sh.front[tid] = 0;
     __syncthreads();
-    if (tid < kGroups) {
-        const u64 mine = sh.most[tid];
+    {       // each thread a part of the groups that may be in front of its own
+        const u64 mine = sh.most[tid % kGroups];
         int front = 0;
-#pragma unroll 8
-        for (int i = 0; i < kGroups; ++i) front += sh.most[i] > mine;
-        if (mine && front == n - 1) sh.border = mine;
+#pragma unroll 32
+        for (int i = 0; i < kGroups / kOf; ++i) front += sh.most[tid / kGroups * (kGroups / kOf) + i] > mine;
+        if constexpr (kOf == 1) {
+            if (mine && front == n - 1) sh.border = mine;
+        } else {
+            atomicAdd(sh.front + tid % kGroups, front);
+            __syncthreads();
+            if (tid < kGroups && mine && sh.front[tid] == n - 1) sh.border = mine;
+        }
     }
     __syncthreads();
     const u64 border = sh.border;
@@ -309,12 +317,14 @@ __device__ __forceinline__ void top_keys(int n, u64 most, TopShared<LIST>& sh, E
             if (key && key >= border) sh.list[atomicAdd(&sh.count, 1)] = key;
         });
     __syncthreads();
-    const int count = sh.count;
-    for (int i = tid; i < count; i += THREADS) {
+    // a wave counts for one key after another how many of the list are in front of it, 64 of them at a time
+    const int count = sh.count, lane = tid & 63;
+    const u64 near = lane < count ? sh.list[lane] : 0;
+    for (int i = tid >> 6; i < count; i += THREADS / 64) {
         const u64 key = sh.list[i];
-        int place = 0;
-        for (int j = 0; j < count; ++j) place += sh.list[j] > key;
-        if (place < n) sh.first[place] = key;
+        int place = __popcll(__ballot(near > key));
+        for (int j = 64; j < count && place < n; j += 64) place += __popcll(__ballot(j + lane < count && sh.list[j + lane] > key));
+        if (lane == 0 && place < n) sh.first[place] = key;
     }
     __syncthreads();
 }
