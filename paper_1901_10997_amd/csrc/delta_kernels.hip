@@ -145,6 +145,14 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" : : : "memory");
 }
 
+// 0 that the compiler does not know: what is worked out from it stays where it stands (addresses of a loop's end, worked out in front of
+// the loop, would hold a hundred registers through it).
+__device__ __forceinline__ int zero_here()
+{
+    int z = 0;
+    asm volatile("" : "+s"(z));
+    return z;
+}
 // Keeps the loads of a later turn of an unrolled loop out of the turns in front of it, where their registers would not be there.
 __device__ __forceinline__ void one_by_one() { asm volatile("" : : : "memory"); }
 
@@ -1248,12 +1256,13 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
                 }
                 dot += parts[3 * C];
             }
-        const u16 *const Q = at.Q(k), *const K = at.K(k);
+        const int late = zero_here();
+        const u16 *const Q = at.Q(k) + late, *const K = at.K(k) + late;
 #pragma unroll
         for (int m = 0; m < kParts; ++m) {
             if (kP > 1 || m % 2 == 0) one_by_one();
             const f32x4v q4 = dq[m].total(), s4 = from_dS[m].total(), r4 = from_dR[m].total();
-            const int d = key_column(m / kEach, m % kEach) + r;
+            const int d = key_column(m / kEach, m % kEach) + r + late;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float q = 0.f;
@@ -1354,13 +1363,14 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
                 *(float*)row_of<F32>(a.dbeta, a.dbeta_t, a.dbeta_b, t0 + lane, b, k.h) = lane < n ? dbs[0][lane] + dbs[1][lane] : 0.f;
             }
         }
-        const u16 *const KT = at.KT(k), *const QT = at.QT(k);
-        float* const shared = at.shared(k);
+        const u16 *const KT = at.KT(k) + late, *const QT = at.QT(k) + late;
+        float* const shared = at.shared(k) + late;
+        T *const dq0 = (T*)row_of<E>(a.dq, a.dq_t, a.dq_b, t0 + late, b, (int64_t)hk * a.Dk), *const dk0 = (T*)row_of<E>(a.dk, a.dk_t, a.dk_b, t0 + late, b, (int64_t)hk * a.Dk);
 #pragma unroll
         for (int m = 0; m < kParts; ++m) {
             if (kP > 1 || m % 4 == 0) one_by_one();
             Sum sq, sk;
-            const int first = key_column(m / kEach, m % kEach), d = first + r;
+            const int first = key_column(m / kEach, m % kEach), d = first + r + late;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 bf16x8 kt[kP], qt[kP];
@@ -1374,7 +1384,7 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (d >= a.Dk || row + i >= rows) continue;
-                float* const part = shared + (row + i) * a.Dk + d;
+                float* const part = shared + (row + i + late) * a.Dk + d;
                 float vq = row + i < n ? q4[i] : 0.f, vk = row + i < n ? k4[i] : 0.f;
                 if (hh > 0) {
                     vq += part[0];
@@ -1384,8 +1394,8 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
                     part[0] = vq;
                     part[C * a.Dk] = vk;
                 } else {
-                    E::store((T*)row_of<E>(a.dq, a.dq_t, a.dq_b, t0 + row + i, b, (int64_t)hk * a.Dk + d), vq);
-                    E::store((T*)row_of<E>(a.dk, a.dk_t, a.dk_b, t0 + row + i, b, (int64_t)hk * a.Dk + d), vk);
+                    E::store(dq0 + (row + i + late) * a.dq_t + d, vq);
+                    E::store(dk0 + (row + i + late) * a.dk_t + d, vk);
                 }
             }
         }
