@@ -270,9 +270,9 @@ struct Place {
     __host__ __device__ int64_t to_shared() const { return to_parts() + head_blocks * tiles() * kParts; }
     __device__ float* shared(const Block& k) const
     {
-        return floats() + to_shared() + (((int64_t)k.c * a.B + k.b) * a.key_heads + k.h / (a.heads / a.key_heads)) * 2 * C * a.Dk;
+        return floats() + to_shared() + (((int64_t)k.c * a.B + k.b) * a.key_heads + k.h / (a.heads / a.key_heads)) * 2 * C * DKP;
     }
-    __host__ __device__ int64_t to_sink() const { return BACK ? to_shared() + (a.heads > a.key_heads ? key_blocks * 2 * C * a.Dk : 0) : 0; }
+    __host__ __device__ int64_t to_sink() const { return BACK ? to_shared() + (a.heads > a.key_heads ? key_blocks * 2 * C * DKP : 0) : 0; }
     // where lanes write that have nothing to write: a store without a branch leaves the count of what is under way known, so that
     // nobody waits for more than it needs
     __device__ float* sink() const { return floats() + to_sink(); }
@@ -1363,39 +1363,64 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
                 *(float*)row_of<F32>(a.dbeta, a.dbeta_t, a.dbeta_b, t0 + lane, b, k.h) = lane < n ? dbs[0][lane] + dbs[1][lane] : 0.f;
             }
         }
+        // keys and queries by columns, and what the heads in front have left, a few tiles at a time
+        constexpr int kBatch = kP == 1 ? 2 : 1;
         const u16 *const KT = at.KT(k) + late, *const QT = at.QT(k) + late;
         float* const shared = at.shared(k) + late;
         T *const dq0 = (T*)row_of<E>(a.dq, a.dq_t, a.dq_b, t0 + late, b, (int64_t)hk * a.Dk), *const dk0 = (T*)row_of<E>(a.dk, a.dk_t, a.dk_b, t0 + late, b, (int64_t)hk * a.Dk);
+        const bool more = hh + 1 < group;
 #pragma unroll
-        for (int m = 0; m < kParts; ++m) {
-            if (kP > 1 || m % 4 == 0) one_by_one();
-            Sum sq, sk;
-            const int first = key_column(m / kEach, m % kEach), d = first + r + late;
+        for (int m0 = 0; m0 < kParts; m0 += kBatch) {
+            constexpr int kHere = kBatch < kParts ? kBatch : kParts;
+            one_by_one();
+            bf16x8 kt[kHere][2][kP], qt[kHere][2][kP];
+            f32x4v q4[kHere], k4[kHere];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                bf16x8 kt[kP], qt[kP];
-                fragment<kP>(kt, KT + fragment_at(first / 16, 2, s) + 8 * lane, C * DKP);
-                fragment<kP>(qt, QT + fragment_at(first / 16, 2, s) + 8 * lane, C * DKP);
-                multiply(sq, dPa[s], kt);
-                multiply(sk, both[s], kt);
-                multiply(sk, dPt[s], qt);
-            }
-            const f32x4v q4 = dq_sum[m] + sq.total(), k4 = dk_sum[m] + sk.total();
+            for (int m = 0; m < kHere; ++m) {
+                const int first = key_column((m0 + m) / kEach, (m0 + m) % kEach);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (d >= a.Dk || row + i >= rows) continue;
-                float* const part = shared + (row + i + late) * a.Dk + d;
-                float vq = row + i < n ? q4[i] : 0.f, vk = row + i < n ? k4[i] : 0.f;
-                if (hh > 0) {
-                    vq += part[0];
-                    vk += part[C * a.Dk];
+                for (int s = 0; s < 2; ++s) {
+                    fragment<kP>(kt[m][s], KT + fragment_at(first / 16, 2, s) + 8 * lane, C * DKP);
+                    fragment<kP>(qt[m][s], QT + fragment_at(first / 16, 2, s) + 8 * lane, C * DKP);
                 }
-                if (hh + 1 < group) {
-                    part[0] = vq;
-                    part[C * a.Dk] = vk;
-                } else {
-                    E::store(dq0 + (row + i + late) * a.dq_t + d, vq);
-                    E::store(dk0 + (row + i + late) * a.dk_t + d, vk);
+                q4[m] = k4[m] = kZero4;
+                if (hh > 0)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float* const part = shared + (row + i + late) * DKP + first + r;
+                        q4[m][i] = part[0];
+                        k4[m][i] = part[C * DKP];
+                    }
+            }
+#pragma unroll
+            for (int m = 0; m < kHere; ++m) {
+                Sum sq, sk;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    multiply(sq, dPa[s], kt[m][s]);
+                    multiply(sk, both[s], kt[m][s]);
+                    multiply(sk, dPt[s], qt[m][s]);
+                }
+                q4[m] += dq_sum[m0 + m] + sq.total();
+                k4[m] += dk_sum[m0 + m] + sk.total();
+            }
+#pragma unroll
+            for (int m = 0; m < kHere; ++m) {
+                const int d = key_column((m0 + m) / kEach, (m0 + m) % kEach) + r + late;
+                if (more) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float* const part = shared + (row + i + late) * DKP + d;
+                        part[0] = q4[m][i];
+                        part[C * DKP] = k4[m][i];
+                    }
+                } else if (d < a.Dk) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (row + i >= rows) continue;
+                        E::store(dq0 + (row + i + late) * a.dq_t + d, row + i < n ? q4[m][i] : 0.f);
+                        E::store(dk0 + (row + i + late) * a.dk_t + d, row + i < n ? k4[m][i] : 0.f);
+                    }
                 }
             }
         }
