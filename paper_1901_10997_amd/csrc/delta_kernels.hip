@@ -546,23 +546,25 @@ struct StateTile {
 
 // Four steps of one column in rows of [T, B]: for each block's four, addresses that need one addition.  Steps behind the sequence's end
 // stand for the last one, and are 0 when taken; no load has a branch, and nothing waits for one here.
-template <class E>
-struct FourSteps {
-    typename E::T raw[4];
+struct FourRows {
     int64_t whole[4], last[4];
     // n: steps of the last block
-    __device__ __forceinline__ void place(int row, int col, int64_t stride, int n)
+    __device__ __forceinline__ FourRows(int row, int64_t stride, int n)
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            whole[i] = (row + i) * stride + col;
-            last[i] = min(row + i, n - 1) * stride + col;
+            whole[i] = (row + i) * stride;
+            last[i] = min(row + i, n - 1) * stride;
         }
     }
-    __device__ __forceinline__ void load(const typename E::T* from, bool is_last)
+};
+template <class E>
+struct FourSteps {
+    typename E::T raw[4];
+    __device__ __forceinline__ void load(const typename E::T* from, const FourRows& rows, bool is_last)
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = from[is_last ? last[i] : whole[i]];
+        for (int i = 0; i < 4; ++i) raw[i] = from[is_last ? rows.last[i] : rows.whole[i]];
     }
     __device__ __forceinline__ f32x4v take(int row, int n) const
     {
@@ -572,27 +574,30 @@ struct FourSteps {
         return v;
     }
 };
-// Forward: the walk over the blocks of one sequence and head, 16 columns of S.  Keys, queries, X and P come from memory as the matrix
-// instruction takes them, those of the next block while this one is worked on; S, R and U pass through LDS in planes.
+
+// Forward: the walk over the blocks of one sequence and head, NT tiles of 16 columns of S.  Keys, queries, X and P come from memory as the
+// matrix instruction takes them, those of the next block while this one is worked on; S, R and U pass through LDS in planes.
 //
-// Bound: the chain S -> R -> U -> S of a block, three products with a barrier behind each, by one wave on a SIMD; what is not on it (Q S, P U,
-// O and all loads) stands where the chain waits: Q S behind R's barrier, P U behind the next block's first.
-template <class E, int DKP, bool STATES>
-__global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) void delta_walk_kernel(DeltaArgs a, int tiles)
+// Bound: with few workgroups the chain S -> R -> U -> S of a block, three products with a barrier behind each, by one wave on a SIMD; what is
+// not on it (Q S, P U, O and all loads) stands where the chain waits: Q S behind R's barrier, P U behind the next block's first.  With many, what
+// a tile takes of keys and queries from the caches, which two tiles halve.
+template <class E, int DKP, int NT, bool STATES>
+__global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)) void delta_walk_kernel(DeltaArgs a, int tiles)
 {
     using T = typename E::T;
-    constexpr int kP = kPlanes<E>, kR = kForResult<E>, LD = DKP + 8, kParts = DKP / 64, kK = DKP / 32;
-    __shared__ u16 Ss[3 * kTile * LD], Rs[3 * kTile * kSteps], Us[kR * kTile * kSteps], Es[3 * kTile * kSteps];
+    constexpr int kP = kPlanes<E>, kR = kForResult<E>, LD = DKP + 8, kParts = DKP / 64, kK = DKP / 32, kS = kTile * kSteps;
+    extern __shared__ u16 planes[];
+    u16 *const Ss = planes, *const Rs = Ss + NT * 3 * kTile * LD, *const Us = Rs + NT * 3 * kS, *const Es = Us + NT * kR * kS;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const unsigned id = by_xcd(blockIdx.x, gridDim.x);
     const int tile = (int)(id % tiles), h = (int)(id / tiles % a.heads), b = (int)(id / tiles / a.heads);
-    const int col = tile * kTile + r, row = 16 * w + 4 * g;             // the lane's column and the first of its four steps
-    const bool live = col < a.Dv;
+    const int col = tile * NT * kTile + r, row = 16 * w + 4 * g;        // the lane's first column and the first of its four steps
     const int len = length_of(a, b), blocks = (len + C - 1) / C;
     const int64_t state = ((int64_t)b * a.heads + h) * a.Dk * a.Dv, states_step = (int64_t)a.B * a.heads * a.Dk * a.Dv;
     const Place<E, DKP, false> at(a);
-    StateTile<DKP> S;
-    S.load(a.S0 ? a.S0 + state : nullptr, a.Dv, a, w, g, col);
+    StateTile<DKP> S[NT];
+#pragma unroll
+    for (int q = 0; q < NT; ++q) S[q].load(a.S0 ? a.S0 + state : nullptr, a.Dv, a, w, g, col + q * kTile);
     if (blocks > 0) {
         // addresses: the same for all lanes, and a lane's own 32 bits
         const Block first = {0, b, h, 0, 0, (int64_t)b * a.heads + h};
@@ -604,21 +609,21 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
         const float* beta0 = row_of<F32>(a.beta, a.beta_t, a.beta_b, 0, b, h);
         const T* v0 = row_of<E>(a.v, a.v_t, a.v_b, 0, b, (int64_t)h * a.Dv);
         T* const o0 = (T*)row_of<E>(a.o, a.o_t, a.o_b, 0, b, (int64_t)h * a.Dv);
-        const int64_t o_at[4] = {row * a.o_t + col, (row + 1) * a.o_t + col, (row + 2) * a.o_t + col, (row + 3) * a.o_t + col};
+        const int64_t o_at[4] = {row * a.o_t, (row + 1) * a.o_t, (row + 2) * a.o_t, (row + 3) * a.o_t};
         float* const sink = at.sink() + lane;
         bf16x8 K[kK][kP], Q[kK][kP], X[2][3], KT[kParts][2][kP], P[2][kR];
-        f32x4v y, e, O = kZero4;
-        FourSteps<E> v;
+        f32x4v y, e, O[NT];
+        FourSteps<E> v[NT];
         FourSteps<F32> beta;
         float last;
         const int rest = len - (blocks - 1) * C;        // steps of the last block
-        v.place(row, min(col, a.Dv - 1), a.v_t, rest);
-        beta.place(row, 0, a.beta_t, rest);
+        const FourRows v_rows(row, a.v_t, rest), beta_rows(row, a.beta_t, rest);
         const auto load_keys = [&](int c) {
 #pragma unroll
             for (int s = 0; s < kK; ++s) fragment<kP>(K[s], K0 + fragment_at(0, kK, s) + mine, C * DKP);
-            v.load(v0, c == blocks - 1);
-            beta.load(beta0, c == blocks - 1);
+#pragma unroll
+            for (int q = 0; q < NT; ++q) v[q].load(v0 + min(col + q * kTile, a.Dv - 1), v_rows, c == blocks - 1);
+            beta.load(beta0, beta_rows, c == blocks - 1);
         };
         const auto load_queries = [&]() {
 #pragma unroll
@@ -643,45 +648,60 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
         };
         // O of a block whose U is in LDS
         const auto finish = [&](int c) {
-            Sum pu;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                bf16x8 uf[kR];
-                fragment<kR>(uf, Us + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
-                multiply(pu, P[s], uf);
-            }
-            O += pu.total();
             const int n = len - c * C;
             T* const to = o0 + (int64_t)c * C * a.o_t;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) E::store(live && c >= 0 && row + i < n ? to + o_at[i] : (T*)sink, O[i]);
+            for (int q = 0; q < NT; ++q) {
+                Sum pu;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    bf16x8 uf[kR];
+                    fragment<kR>(uf, Us + q * kR * kS + r * kSteps + 32 * s + 8 * g, kS);
+                    multiply(pu, P[s], uf);
+                }
+                O[q] += pu.total();
+                const int at_col = col + q * kTile;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) E::store(at_col < a.Dv && c >= 0 && row + i < n ? to + o_at[i] + at_col : (T*)sink, O[q][i]);
+            }
         };
         load_keys(0);
         load_queries();
         load_inverse();
         load_columns();
         load_pairs();
-        S.publish(Ss, w, r, g);
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+            O[q] = kZero4;
+            S[q].publish(Ss + q * 3 * kTile * LD, w, r, g);
+        }
         // No branch in here: where one followed a matrix instruction the compiler has left out the wait in front of its result (two of the
         // eight instructions that lie between them elsewhere), and half of a result was what stood there before.
 #pragma unroll 1
         for (int c = 0; c < blocks; ++c) {
-            if constexpr (STATES) S.store_all(a.states + c * states_step + state, a.Dv, sink, a, w, g, col);
+            if constexpr (STATES)
+#pragma unroll
+                for (int q = 0; q < NT; ++q) S[q].store_all(a.states + c * states_step + state, a.Dv, sink, a, w, g, col + q * kTile);
             lds_barrier();
-            Sum ks, qs, u;
-            bf16x8 f[kK][3];
-#pragma unroll
-            for (int s = 0; s < kK; ++s) fragment<3>(f[s], Ss + r * LD + 32 * s + 8 * g, kTile * LD);
-#pragma unroll
-            for (int s = 0; s < kK; ++s) multiply(ks, K[s], f[s]);
             const int n = len - c * C;
             const bool more = c + 1 < blocks;
-            const f32x4v b4 = beta.take(row, n), v4 = v.take(row, n), found = ks.total(), decay = e, y4 = y;
+            Sum qs[NT];
+            bf16x8 f[NT][kK][3];
+            const f32x4v b4 = beta.take(row, n), decay = e, y4 = y;
             const float decayed = last;
-            f32x4v R;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) R[i] = b4[i] * (v4[i] - y4[i] * found[i]);
-            store_split<3>(R, Rs + r * kSteps + row, kTile * kSteps);
+            for (int q = 0; q < NT; ++q) {
+                Sum ks;
+#pragma unroll
+                for (int s = 0; s < kK; ++s) fragment<3>(f[q][s], Ss + q * 3 * kTile * LD + r * LD + 32 * s + 8 * g, kTile * LD);
+#pragma unroll
+                for (int s = 0; s < kK; ++s) multiply(ks, K[s], f[q][s]);
+                const f32x4v v4 = v[q].take(row, n), found = ks.total();
+                f32x4v R;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) R[i] = b4[i] * (v4[i] - y4[i] * found[i]);
+                store_split<3>(R, Rs + q * 3 * kS + r * kSteps + row, kS);
+            }
             finish(c - 1);                      // in front of the first block of nothing, to nowhere
             lds_barrier();
             // of the next block what this one has done with, each as soon as that is so
@@ -691,51 +711,62 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
             load_keys(more ? c + 1 : c);
             load_pairs();                       // of this block: taken behind the next one's first barrier
             P0 += more ? head_step : 0;
-            bf16x8 rf[2][3];
+            f32x4v U[NT];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) fragment<3>(rf[s], Rs + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
+            for (int q = 0; q < NT; ++q) {
+                Sum u;
+                bf16x8 rf[2][3];
 #pragma unroll
-            for (int s = 0; s < kK; ++s) {
-                if constexpr (kR == 2) {
-                    const bf16x8 two[2] = {f[s][0], f[s][1]};
-                    multiply(qs, Q[s], two);
-                } else {
-                    multiply(qs, Q[s], f[s]);
+                for (int s = 0; s < 2; ++s) fragment<3>(rf[s], Rs + q * 3 * kS + r * kSteps + 32 * s + 8 * g, kS);
+#pragma unroll
+                for (int s = 0; s < kK; ++s) {
+                    if constexpr (kR == 2) {
+                        const bf16x8 two[2] = {f[q][s][0], f[q][s][1]};
+                        multiply(qs[q], Q[s], two);
+                    } else {
+                        multiply(qs[q], Q[s], f[q][s]);
+                    }
                 }
+#pragma unroll
+                for (int s = 0; s < 2; ++s) multiply(u, X[s], rf[s]);
+                U[q] = u.total();
+                store_split<3>(times4(U[q], decay), Es + q * 3 * kS + r * kSteps + row, kS);
+                O[q] = times4(qs[q].total(), scaled4(y4, a.scale));
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) multiply(u, X[s], rf[s]);
-            const f32x4v U = u.total();
-            store_split<3>(times4(U, decay), Es + r * kSteps + row, kTile * kSteps);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) O[i] = qs.total()[i] * (a.scale * y4[i]);
             lds_barrier();
-            bf16x8 ef[2][3];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) fragment<3>(ef[s], Es + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
-            store_split<kR>(U, Us + r * kSteps + row, kTile * kSteps);
             Q0 += more ? keys_step : 0;
             X0 += more ? head_step : 0;
             y0 += more ? head_step / 2 : 0;
             load_queries();
             load_inverse();
 #pragma unroll
-            for (int m = 0; m < kParts; ++m) {
-                Sum sum;
+            for (int q = 0; q < NT; ++q) {
+                bf16x8 ef[2][3];
 #pragma unroll
-                for (int s = 0; s < 2; ++s) multiply(sum, KT[m][s], ef[s]);
-                S.v[m] = scaled4(S.v[m], decayed) + sum.total();
+                for (int s = 0; s < 2; ++s) fragment<3>(ef[s], Es + q * 3 * kS + r * kSteps + 32 * s + 8 * g, kS);
+                store_split<kR>(U[q], Us + q * kR * kS + r * kSteps + row, kS);
+#pragma unroll
+                for (int m = 0; m < kParts; ++m) {
+                    Sum sum;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) multiply(sum, KT[m][s], ef[s]);
+                    S[q].v[m] = scaled4(S[q].v[m], decayed) + sum.total();
+                }
+                S[q].publish(Ss + q * 3 * kTile * LD, w, r, g);
             }
-            S.publish(Ss, w, r, g);
             KT0 += more ? keys_step : 0;
             load_columns();
         }
         lds_barrier();
         finish(blocks - 1);
     }
-    if (a.ST) S.store(a.ST + state, a, w, g, col);
-    for (int64_t t = len + (threadIdx.x >> 4); t < a.T; t += 4 * kWaves)
-        if (live) E::store((T*)row_of<E>(a.o, a.o_t, a.o_b, t, b, (int64_t)h * a.Dv + col), 0.f);
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+        const int at_col = col + q * kTile;
+        if (a.ST) S[q].store(a.ST + state, a, w, g, at_col);
+        for (int64_t t = len + (threadIdx.x >> 4); t < a.T; t += 4 * kWaves)
+            if (at_col < a.Dv) E::store((T*)row_of<E>(a.o, a.o_t, a.o_b, t, b, (int64_t)h * a.Dv + at_col), 0.f);
+    }
 }
 
 // Few steps: a thread holds four columns of every 32nd row of S, eight threads 32 columns of a row; the sums over the rows of
@@ -826,24 +857,25 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a, int tiles)
             if (col + i < a.Dv) E::store((T*)row_of<E>(a.o, a.o_t, a.o_b, t, b, (int64_t)h * a.Dv) + col + i, 0.f);
 }
 
-// Gradient: the walk back over the blocks, 16 columns of dS.  Its chain is dS' -> dU -> dR -> dS; Q' (y dO) stands where dR is
+// Gradient: the walk back over the blocks, NT tiles of 16 columns of dS.  Its chain is dS' -> dU -> dR -> dS; Q' (y dO) stands where dR is
 // waited for.
-template <class E, int DKP>
-__global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) void delta_walk_back_kernel(DeltaArgs a, int tiles)
+template <class E, int DKP, int NT>
+__global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)) void delta_walk_back_kernel(DeltaArgs a, int tiles)
 {
     using T = typename E::T;
-    constexpr int kP = kPlanes<E>, LD = DKP + 8, kParts = DKP / 64, kK = DKP / 32;
-    __shared__ u16 Ds[3 * kTile * LD], Os[kP * kTile * kSteps], Us[3 * kTile * kSteps], Ys[3 * kTile * kSteps], Zs[3 * kTile * kSteps];
+    constexpr int kP = kPlanes<E>, LD = DKP + 8, kParts = DKP / 64, kK = DKP / 32, kS = kTile * kSteps;
+    extern __shared__ u16 planes[];
+    u16 *const Ds = planes, *const Os = Ds + NT * 3 * kTile * LD, *const Us = Os + NT * kP * kS, *const Ys = Us + NT * 3 * kS, *const Zs = Ys + NT * 3 * kS;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const unsigned id = by_xcd(blockIdx.x, gridDim.x);
     const int tile = (int)(id % tiles), h = (int)(id / tiles % a.heads), b = (int)(id / tiles / a.heads);
-    const int col = tile * kTile + r, row = 16 * w + 4 * g;
-    const bool live = col < a.Dv;
+    const int col = tile * NT * kTile + r, row = 16 * w + 4 * g;
     const int len = length_of(a, b), blocks = (len + C - 1) / C;
     const int64_t state = ((int64_t)b * a.heads + h) * a.Dk * a.Dv;
     const Place<E, DKP, true> at(a);
-    StateTile<DKP> dS;
-    dS.load(a.dST ? a.dST + state : nullptr, a.Dv, a, w, g, col);
+    StateTile<DKP> dS[NT];
+#pragma unroll
+    for (int q = 0; q < NT; ++q) dS[q].load(a.dST ? a.dST + state : nullptr, a.Dv, a, w, g, col + q * kTile);
     if (blocks > 0) {
         const Block behind = {blocks - 1, b, h, 0, 0, ((int64_t)(blocks - 1) * a.B + b) * a.heads + h};
         const int64_t keys_step = (int64_t)a.B * a.key_heads * at.kKeys, head_step = (int64_t)a.B * a.heads * at.kHead;
@@ -854,17 +886,16 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
         const float* beta0 = row_of<F32>(a.beta, a.beta_t, a.beta_b, (int64_t)behind.c * C, b, h);
         const T* dO0 = row_of<E>(a.dO, a.do_t, a.do_b, (int64_t)behind.c * C, b, (int64_t)h * a.Dv);
         T* const dv0 = (T*)row_of<E>(a.dv, a.dv_t, a.dv_b, 0, b, (int64_t)h * a.Dv);
-        const int64_t dv_at[4] = {row * a.dv_t + col, (row + 1) * a.dv_t + col, (row + 2) * a.dv_t + col, (row + 3) * a.dv_t + col};
+        const int64_t dv_at[4] = {row * a.dv_t, (row + 1) * a.dv_t, (row + 2) * a.dv_t, (row + 3) * a.dv_t};
         float* const sink = at.sink() + lane;
         const int ld = at.row();
         bf16x8 K[kK][kP], PT[2][3], XT[2][3], KT[kParts][2][kP], QT[kParts][2][kP];
-        f32x4v y, e, dO, b4;
-        FourSteps<E> raw;
+        f32x4v y, e, dO[NT], b4;
+        FourSteps<E> raw[NT];
         FourSteps<F32> beta;
         float last;
         const int rest = len - behind.c * C;
-        raw.place(row, min(col, a.Dv - 1), a.do_t, rest);
-        beta.place(row, 0, a.beta_t, rest);
+        const FourRows dO_rows(row, a.do_t, rest), beta_rows(row, a.beta_t, rest);
         const auto load_gates = [&]() {
             y = at4(y0 + row);
             e = at4(y0 + C + row);
@@ -877,8 +908,9 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
         const auto load_pairs = [&](bool is_last) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) fragment<3>(PT[s], PT0 + fragment_at(0, 2, s) + mine, C * C);
-            raw.load(dO0, is_last);
-            beta.load(beta0, is_last);
+#pragma unroll
+            for (int q = 0; q < NT; ++q) raw[q].load(dO0 + min(col + q * kTile, a.Dv - 1), dO_rows, is_last);
+            beta.load(beta0, beta_rows, is_last);
         };
         const auto load_inverse = [&]() {
 #pragma unroll
@@ -890,19 +922,12 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
 #pragma unroll
                 for (int m = 0; m < kParts; ++m) fragment<kP>(to[m][s], from + fragment_at(m, 2, s) + mine, C * DKP);
         };
-        Sum po;
         const auto take_pairs = [&](int n) {    // of the block that comes next; its dO in LDS
-            dO = raw.take(row, n);
             b4 = beta.take(row, n);
-            store_split<kP>(dO, Os + r * kSteps + row, kTile * kSteps);
-        };
-        const auto multiply_pairs = [&]() {
-            po = Sum();
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                bf16x8 f[kP];
-                fragment<kP>(f, Os + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
-                multiply(po, PT[s], f);
+            for (int q = 0; q < NT; ++q) {
+                dO[q] = raw[q].take(row, n);
+                store_split<kP>(dO[q], Os + q * kP * kS + r * kSteps + row, kS);
             }
         };
         load_pairs(true);
@@ -912,42 +937,42 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
         load_columns(QT, QT0);
         load_columns(KT, KT0);
         take_pairs(rest);
-        dS.publish(Ds, w, r, g);
+#pragma unroll
+        for (int q = 0; q < NT; ++q) dS[q].publish(Ds + q * 3 * kTile * LD, w, r, g);
         // no branch in here, as in the walk forward
 #pragma unroll 1
         for (int c = blocks - 1; c >= 0; --c) {
             const int n = len - c * C;
             Block k = behind;
             k.index = ((int64_t)c * a.B + b) * a.heads + h;
-            dS.store_all(at.dS(k), ld, sink, a, w, g, col);
-            const f32x4v dO4 = dO, beta4 = b4;
+#pragma unroll
+            for (int q = 0; q < NT; ++q) dS[q].store_all(at.dS(k), ld, sink, a, w, g, col + q * kTile);
+            const f32x4v beta4 = b4;
             const bool more = c > 0;
             lds_barrier();
-            bf16x8 f[kK][3];
-            Sum kd, dr;
-#pragma unroll
-            for (int s = 0; s < kK; ++s) fragment<3>(f[s], Ds + r * LD + 32 * s + 8 * g, kTile * LD);
-#pragma unroll
-            for (int s = 0; s < kK; ++s) multiply(kd, K[s], f[s]);
-            multiply_pairs();
-            const f32x4v found = times4(kd.total(), e), dU = found + po.total();
-            store_split<3>(dU, Us + r * kSteps + row, kTile * kSteps);
-            f32x4v yO, yb;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                yO[i] = a.scale * y[i] * dO4[i];
-                yb[i] = -y[i] * beta4[i];
-            }
+            f32x4v found[NT], yb;
             const float decayed = last;
-            store_split<3>(yO, Ys + r * kSteps + row, kTile * kSteps);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) yb[i] = -y[i] * beta4[i];
+#pragma unroll
+            for (int q = 0; q < NT; ++q) {
+                bf16x8 f[kK][3];
+                Sum kd, po;
+#pragma unroll
+                for (int s = 0; s < kK; ++s) fragment<3>(f[s], Ds + q * 3 * kTile * LD + r * LD + 32 * s + 8 * g, kTile * LD);
+#pragma unroll
+                for (int s = 0; s < kK; ++s) multiply(kd, K[s], f[s]);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    bf16x8 o[kP];
+                    fragment<kP>(o, Os + q * kP * kS + r * kSteps + 32 * s + 8 * g, kS);
+                    multiply(po, PT[s], o);
+                }
+                found[q] = times4(kd.total(), e);
+                store_split<3>(found[q] + po.total(), Us + q * 3 * kS + r * kSteps + row, kS);
+                store_split<3>(times4(scaled4(y, a.scale), dO[q]), Ys + q * 3 * kS + r * kSteps + row, kS);
+            }
             lds_barrier();
-            bf16x8 uf[2][3], yf[2][3], zf[2][3];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) fragment<3>(uf[s], Us + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) fragment<3>(yf[s], Ys + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) multiply(dr, XT[s], uf[s]);
             K0 -= more ? keys_step : 0;
             PT0 -= more ? head_step : 0;
             XT0 -= more ? head_step : 0;
@@ -957,41 +982,63 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> <= 2 ? 2 : 1)) voi
             load_pairs(!more && blocks == 1);   // all blocks but the last are whole
             load_gates();
             load_keys();
-            Sum sums[kParts];
+            Sum sums[NT][kParts];
+            f32x4v dR[NT];
 #pragma unroll
-            for (int m = 0; m < kParts; ++m)
+            for (int q = 0; q < NT; ++q) {
+                Sum dr;
+                bf16x8 uf[2][3], yf[2][3];
 #pragma unroll
-                for (int s = 0; s < 2; ++s) multiply(sums[m], QT[m][s], yf[s]);
-            const f32x4v dR = dr.total();
-            store_split<3>(times4(yb, dR), Zs + r * kSteps + row, kTile * kSteps);
+                for (int s = 0; s < 2; ++s) fragment<3>(uf[s], Us + q * 3 * kS + r * kSteps + 32 * s + 8 * g, kS);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) fragment<3>(yf[s], Ys + q * 3 * kS + r * kSteps + 32 * s + 8 * g, kS);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) multiply(dr, XT[s], uf[s]);
+#pragma unroll
+                for (int m = 0; m < kParts; ++m)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) multiply(sums[q][m], QT[m][s], yf[s]);
+                dR[q] = dr.total();
+                store_split<3>(times4(yb, dR[q]), Zs + q * 3 * kS + r * kSteps + row, kS);
+            }
             QT0 -= more ? keys_step : 0;
             load_columns(QT, QT0);
             load_inverse();
             lds_barrier();
 #pragma unroll
-            for (int s = 0; s < 2; ++s) fragment<3>(zf[s], Zs + r * kSteps + 32 * s + 8 * g, kTile * kSteps);
+            for (int q = 0; q < NT; ++q) {
+                bf16x8 zf[2][3];
 #pragma unroll
-            for (int m = 0; m < kParts; ++m) {
+                for (int s = 0; s < 2; ++s) fragment<3>(zf[s], Zs + q * 3 * kS + r * kSteps + 32 * s + 8 * g, kS);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) multiply(sums[m], KT[m][s], zf[s]);
-                dS.v[m] = scaled4(dS.v[m], decayed) + sums[m].total();
-            }
-            dS.publish(Ds, w, r, g);
-            float *const left = at.dR(k) + row * ld + col, *const f0 = at.found(k) + row * ld + col;     // a tile's columns are all there
+                for (int m = 0; m < kParts; ++m) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                left[i * ld] = dR[i];
-                f0[i * ld] = found[i];
-                E::store(live && row + i < n ? dv0 + (int64_t)c * C * a.dv_t + dv_at[i] : (T*)sink, beta4[i] * dR[i]);
+                    for (int s = 0; s < 2; ++s) multiply(sums[q][m], KT[m][s], zf[s]);
+                    dS[q].v[m] = scaled4(dS[q].v[m], decayed) + sums[q][m].total();
+                }
+                dS[q].publish(Ds + q * 3 * kTile * LD, w, r, g);
+                const int at_col = col + q * kTile;
+                // the workspace's rows hold a whole number of two tiles
+                float *const left = at.dR(k) + row * ld + at_col, *const f0 = at.found(k) + row * ld + at_col;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    left[i * ld] = dR[q][i];
+                    f0[i * ld] = found[q][i];
+                    E::store(at_col < a.Dv && row + i < n ? dv0 + (int64_t)c * C * a.dv_t + dv_at[i] + at_col : (T*)sink, beta4[i] * dR[q][i]);
+                }
             }
             KT0 -= more ? keys_step : 0;
             load_columns(KT, KT0);
             take_pairs(C);
         }
     }
-    if (a.dS0) dS.store(a.dS0 + state, a, w, g, col);
-    for (int64_t t = len + (threadIdx.x >> 4); t < a.T; t += 4 * kWaves)
-        if (live) E::store((T*)row_of<E>(a.dv, a.dv_t, a.dv_b, t, b, (int64_t)h * a.Dv + col), 0.f);
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+        const int at_col = col + q * kTile;
+        if (a.dS0) dS[q].store(a.dS0 + state, a, w, g, at_col);
+        for (int64_t t = len + (threadIdx.x >> 4); t < a.T; t += 4 * kWaves)
+            if (at_col < a.Dv) E::store((T*)row_of<E>(a.dv, a.dv_t, a.dv_b, t, b, (int64_t)h * a.Dv + at_col), 0.f);
+    }
 }
 
 // sum over the 16 lanes that hold the columns of a row
@@ -1026,12 +1073,11 @@ __global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int
     const int ld = at.row();
     FourSteps<E> raw;
     FourSteps<F32> raw_beta;
-    raw.place(row, min(col, a.Dv - 1), a.v_t, k.n);
-    raw_beta.place(row, 0, a.beta_t, k.n);
+    const FourRows v_rows(row, a.v_t, k.n), beta_rows(row, a.beta_t, k.n);
     S.load(a.states + k.index * a.Dk * a.Dv, a.Dv, a, w, g, col);
     dS.load(at.dS(k), ld, a, w, g, col);
-    raw.load(row_of<E>(a.v, a.v_t, a.v_b, k.t0, b, (int64_t)h * a.Dv), true);
-    raw_beta.load(row_of<F32>(a.beta, a.beta_t, a.beta_b, k.t0, b, h), true);
+    raw.load(row_of<E>(a.v, a.v_t, a.v_b, k.t0, b, (int64_t)h * a.Dv + min(col, a.Dv - 1)), v_rows, true);
+    raw_beta.load(row_of<F32>(a.beta, a.beta_t, a.beta_b, k.t0, b, h), beta_rows, true);
     float dot = 0.f, dR[4], found[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -1445,6 +1491,30 @@ hipError_t prepare(const DeltaArgs& a, hipStream_t s)
     return hipGetLastError();
 }
 
+// Two tiles of columns to a workgroup from as many as keep all compute units busy with half the workgroups
+bool two_tiles(const DeltaArgs& a) { return a.Dv > kTile && (int64_t)a.B * a.heads * ((a.Dv + 2 * kTile - 1) / (2 * kTile)) >= 256; }
+
+template <class Kernel>
+hipError_t walk_by(Kernel kernel, const DeltaArgs& a, int tiles, size_t lds, hipStream_t s)
+{
+    const hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)a.B * a.heads * tiles)), dim3(kThreads), lds, s, a, tiles);
+    return hipGetLastError();
+}
+template <class E, int DKP, int NT, bool STATES>
+hipError_t walk(const DeltaArgs& a, hipStream_t s)
+{
+    const size_t lds = NT * kTile * (3 * (DKP + 8) + (6 + kForResult<E>)*kSteps) * sizeof(u16);
+    return walk_by(delta_walk_kernel<E, DKP, NT, STATES>, a, (a.Dv + NT * kTile - 1) / (NT * kTile), lds, s);
+}
+template <class E, int DKP, int NT>
+hipError_t walk_back(const DeltaArgs& a, hipStream_t s)
+{
+    const size_t lds = NT * kTile * (3 * (DKP + 8) + (9 + kPlanes<E>)*kSteps) * sizeof(u16);
+    return walk_by(delta_walk_back_kernel<E, DKP, NT>, a, (a.Dv + NT * kTile - 1) / (NT * kTile), lds, s);
+}
+
 template <class E, int DKP>
 hipError_t forward(const DeltaArgs& a, hipStream_t s)
 {
@@ -1455,11 +1525,9 @@ hipError_t forward(const DeltaArgs& a, hipStream_t s)
     }
     const hipError_t e = prepare<E, DKP, false>(a, s);
     if (e != hipSuccess) return e;
-    const int tiles = (a.Dv + kTile - 1) / kTile;
-    const dim3 grid((unsigned)((int64_t)a.B * a.heads * tiles)), block(kThreads);
-    if (a.states) hipLaunchKernelGGL((delta_walk_kernel<E, DKP, true>), grid, block, 0, s, a, tiles);
-    else hipLaunchKernelGGL((delta_walk_kernel<E, DKP, false>), grid, block, 0, s, a, tiles);
-    return hipGetLastError();
+    if constexpr (DKP <= 128)
+        if (two_tiles(a)) return a.states ? walk<E, DKP, 2, true>(a, s) : walk<E, DKP, 2, false>(a, s);
+    return a.states ? walk<E, DKP, 1, true>(a, s) : walk<E, DKP, 1, false>(a, s);
 }
 
 template <class E, int DKP>
@@ -1468,8 +1536,8 @@ hipError_t backward(const DeltaArgs& a, hipStream_t s)
     hipError_t e = a.T > 0 ? prepare<E, DKP, true>(a, s) : hipSuccess;
     if (e != hipSuccess) return e;
     const int tiles = (a.Dv + kTile - 1) / kTile;
-    hipLaunchKernelGGL((delta_walk_back_kernel<E, DKP>), dim3((unsigned)((int64_t)a.B * a.heads * tiles)), dim3(kThreads), 0, s, a, tiles);
-    if (a.T == 0) return hipGetLastError();
+    e = DKP <= 128 && two_tiles(a) ? walk_back<E, DKP, DKP <= 128 ? 2 : 1>(a, s) : walk_back<E, DKP, 1>(a, s);
+    if (e != hipSuccess || a.T == 0) return e;
     hipLaunchKernelGGL((delta_update_kernel<E, DKP>), dim3((unsigned)(blocks(a.T) * a.B * a.heads * tiles)), dim3(kThreads), 0, s, a, tiles);
     constexpr int kRows = DKP < kRowsAtOnce ? DKP : kRowsAtOnce;
     const size_t lds = std::max<size_t>(((3 + kForResult<E>)*kRows + 3 * C) * kWideRow * sizeof(u16), 2 * C * kRow * sizeof(float));
