@@ -210,3 +210,61 @@ def test_a_step_too_many_sequences_for_one_round():
     """More workgroups than the device holds at once, several rounds of them."""
     c = D.make(12, 1, 600, 2, 2, 32, 64, "bf16")
     D.check_forward(c, *D.forward(c, D.buffers(c))[:2])
+
+
+# enough workgroups for two tiles of columns each: one tile and a part of one behind them, an odd one, key columns of both sizes
+@pytest.mark.parametrize("T,batch,heads,key_heads,Dk,Dv", [(130, 16, 16, 4, 40, 33), (70, 32, 8, 8, 100, 20), (65, 8, 8, 2, 128, 130), (66, 64, 8, 8, 16, 16)])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_many_sequences(name, T, batch, heads, key_heads, Dk, Dv):
+    r = np.random.default_rng(13)
+    c = D.make(13, T, batch, heads, key_heads, Dk, Dv, name, lengths=[T] + list(r.integers(0, T + 1, batch - 1)))
+    s = D.buffers(c)
+    o, ST, kept = D.forward(c, s, states=True)
+    D.check_forward(c, o, ST, kept)
+    D.check_backward(c, *D.backward(c, s, kept))
+    plain, ST2, _ = D.forward(c, s)             # the walk that keeps no states
+    assert bool((plain.t == o.t).all()) and bool((ST2 == ST).all())
+
+
+def test_a_walk_does_not_depend_on_its_company():
+    """The same sequence alone (one tile to a workgroup) and among many (two): the same bits."""
+    c = D.make(14, 130, 40, 8, 4, 64, 48, "bf16")
+    many = D.buffers(c)
+    o, ST, kept = D.forward(c, many, states=True)
+    out, dS0 = D.backward(c, many, kept)
+    one = {k: (v[:, 3:4] if k in ("q", "k", "v", "g", "beta", "dO") else v[3:4] if v is not None else None) for k, v in c.items()
+           if k in ("q", "k", "v", "g", "beta", "dO", "S0", "dST")}
+    alone = dict(c, batch=1, **one)
+    s = D.buffers(alone)
+    o1, ST1, kept1 = D.forward(alone, s, states=True)
+    out1, dS01 = D.backward(alone, s, kept1)
+    assert bool((o1.t[:, 0] == o.t[:, 3]).all()) and bool((ST1[0] == ST[3]).all()) and bool((dS01[0] == dS0[3]).all())
+    assert all(bool((out1[k].t[:, 0] == out[k].t[:, 3]).all()) for k in out)
+
+
+def test_keys_of_any_length():
+    """Keys are used as they are: short and long ones, whose states stay small, over a few blocks."""
+    c = D.make(15, 140, 2, 2, 2, 24, 20, "f32")
+    c["k"] = np.float32(c["k"] * 0.3).astype(np.float64)
+    c["q"] = np.float32(c["q"] * 50).astype(np.float64)
+    s = D.buffers(c)
+    o, ST, kept = D.forward(c, s, states=True)
+    D.check_forward(c, o, ST, kept)
+    D.check_backward(c, *D.backward(c, s, kept))
+
+
+def test_workspaces_of_their_own():
+    """Two calls on two streams at the same time."""
+    import torch
+    cases = [D.make(16 + i, 200, 2, 4, 2, 64, 64, "bf16") for i in range(2)]
+    held = [D.buffers(c) for c in cases]
+    want = [D.forward(c, s)[0].t.clone() for c, s in zip(cases, held)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for turn in range(4):
+        for c, s, st in zip(cases, held, streams):
+            with torch.cuda.stream(st):
+                got.append(D.forward(c, s, stream=st.cuda_stream)[0].t)
+    torch.cuda.synchronize()
+    assert all(bool((g == want[i % 2]).all()) for i, g in enumerate(got))
