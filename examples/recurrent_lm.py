@@ -7,12 +7,15 @@ writes on from it token by token, and learns.
                h = recurrence(P)                          the cell without W_h                      (lstm_scan_forward)
                r = quantize(h) W_out^T                    added in front of the next norm           (lstm_quantize_fp8, lstm_matmul_fp8)
     logits = norm(x + r) W_vocabulary^T                   token = draw(logits, u)                   (lstm_sample)
+                                                          log p of the given tokens                 (lstm_logprobs_forward)
 
-Learning goes back through the same operators: lstm_scan_backward, lstm_rmsnorm_backward, and each product's two gradients as
-products of transposed 8-bit operands.  torch holds the memory, gathers the embeddings, and computes the loss of the logits.
+Learning goes back through the same operators: lstm_logprobs_backward, lstm_scan_backward, lstm_rmsnorm_backward, and each product's two
+gradients as products of transposed 8-bit operands.  A smaller model learns from a larger one's likeliest words, which
+lstm_logprobs_forward lists and lstm_distill_forward / _backward compare with its own.  torch holds the memory and gathers the embeddings.
 
     python3 examples/recurrent_lm.py                          two blocks of 1500 units, 10 000 words
     python3 examples/recurrent_lm.py --train 50 --units 256 --words 500
+    python3 examples/recurrent_lm.py --train 50 --units 256 --words 500 --student 64
 """
 import argparse
 import os
@@ -118,6 +121,42 @@ def scan_gradient(P, states, dh):
     return dP
 
 
+def scores(logits, token, top=0, stats=None):
+    """log p of the tokens [M] and, of the `top` first words of every row, which they are and their log p"""
+    M, words = logits.shape
+    logprob = torch.empty(M, device="cuda")
+    first, first_logprob = torch.empty((M, top), dtype=torch.int32, device="cuda"), torch.empty((M, top), device="cuda")
+    ws = _workspace(B.lstm_logprobs_workspace_bytes(M, words, top))
+    B.lstm_logprobs_forward(M, words, TYPE[logits.dtype], logits.data_ptr(), logits.stride(0), None, 0, token.data_ptr(), logprob.data_ptr(), None, None,
+                            _ptr(stats), top, first.data_ptr() if top else None, first_logprob.data_ptr() if top else None, ws.data_ptr(), ws.numel(), _stream())
+    return logprob, first, first_logprob
+
+
+def likelihood_loss(logits, token):
+    """Mean of -log p of the tokens [M] and its gradient by the logits"""
+    M, words = logits.shape
+    stats, dlogits = torch.empty((M, 4), device="cuda"), torch.empty_like(logits)
+    logprob, _, _ = scores(logits, token, stats=stats)
+    each = torch.full((M,), -1.0 / M, device="cuda")
+    B.lstm_logprobs_backward(M, words, TYPE[logits.dtype], logits.data_ptr(), logits.stride(0), None, 0, token.data_ptr(), stats.data_ptr(), each.data_ptr(),
+                             None, dlogits.data_ptr(), words, _stream())
+    return -logprob.mean(), dlogits
+
+
+def teacher_loss(logits, teacher):
+    """Mean of the distance to a teacher's words [M, K] and their log probabilities, what they leave being one share for all others, and its gradient"""
+    (M, words), (first, first_logprob) = logits.shape, teacher
+    K = first.shape[1]
+    loss, stats, dlogits = torch.empty(M, device="cuda"), torch.empty((M, 4), device="cuda"), torch.empty_like(logits)
+    ws = _workspace(B.lstm_distill_workspace_bytes(M, words, K))
+    lse, each = torch.zeros(M, device="cuda"), torch.full((M,), 1.0 / M, device="cuda")      # log probabilities: their sum is 1
+    rows = (M, words, K, TYPE[logits.dtype], logits.data_ptr(), logits.stride(0), first.data_ptr(), first.stride(0), first_logprob.data_ptr(),
+            first_logprob.stride(0), lse.data_ptr(), 1.0)
+    B.lstm_distill_forward(*rows, loss.data_ptr(), stats.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+    B.lstm_distill_backward(*rows, stats.data_ptr(), each.data_ptr(), dlogits.data_ptr(), words, _stream())
+    return loss.mean(), dlogits
+
+
 class RecurrentLm:
     def __init__(self, words, units, blocks, seed=0):
         gen = torch.Generator(device="cuda")
@@ -169,17 +208,13 @@ class RecurrentLm:
             keep.append((sums, rstd))
         return product(y8, self.eight["vocabulary"], torch.empty((M, self.words), device="cuda")), new_state
 
-    def gradient(self, tokens, targets):
-        """Mean cross-entropy of `targets` [T, batch] and its gradient by every parameter."""
+    def gradient(self, tokens, targets, teacher=None):
+        """Mean cross-entropy of `targets` [T, batch] or, given a teacher's words for every position, mean distance to it, and its gradient by
+        every parameter."""
         keep, p, (T, batch), H = [], self.params, tokens.shape, self.units
         M, grad = T * batch, {}
         logits, _ = self.forward(tokens, keep=keep)
-        log_p = torch.log_softmax(logits, 1)
-        right = targets.reshape(-1, 1)
-        loss = -log_p.gather(1, right).mean()
-        dlogits = log_p.exp_()
-        dlogits.scatter_add_(1, right, torch.full_like(right, -1, dtype=torch.float32))
-        dlogits /= M
+        loss, dlogits = likelihood_loss(logits, targets.reshape(-1).to(torch.int32)) if teacher is None else teacher_loss(logits, teacher)
 
         def through(name, d, inputs, dtype):
             """dW into `grad`, and the gradient of the inputs [M, columns of W]"""
@@ -269,12 +304,12 @@ class Writer:
         return out
 
 
-def train(model, tokens, steps, rate):
+def train(model, tokens, steps, rate, teacher=None):
     """`steps` steps of Adam on one batch tokens [T + 1, batch]; the losses."""
     moments = {k: (torch.zeros_like(v), torch.zeros_like(v)) for k, v in model.params.items()}
     losses = []
     for n in range(1, steps + 1):
-        loss, grad = model.gradient(tokens[:-1], tokens[1:])
+        loss, grad = model.gradient(tokens[:-1], tokens[1:], teacher)
         for k, v in model.params.items():
             m1, m2 = moments[k]
             m1.mul_(0.9).add_(grad[k], alpha=0.1)
@@ -294,6 +329,7 @@ def main():
     a.add_argument("--prompt", type=int, default=64, help="tokens of the longest prompt")
     a.add_argument("--generate", type=int, default=64)
     a.add_argument("--train", type=int, default=0, help="steps on one synthetic batch first")
+    a.add_argument("--student", type=int, default=0, help="units of a model that then learns the same number of steps from this one's likeliest words")
     a = a.parse_args()
     model = RecurrentLm(a.words, a.units, a.blocks)
     gen = torch.Generator(device="cuda")
@@ -308,6 +344,13 @@ def main():
     if a.train:
         losses = train(model, tokens, a.train, 2e-3)
         print(f"loss {losses[0]:.3f} -> {losses[-1]:.3f} in {a.train} steps")
+    if a.student:
+        target = tokens[1:].reshape(-1).to(torch.int32)
+        logprob, *teacher = scores(model.forward(tokens[:-1])[0], target, min(32, a.words))
+        student = RecurrentLm(a.words, a.student, a.blocks, seed=2)
+        losses = train(student, tokens, a.train, 2e-3, teacher)
+        print(f"student: from the teacher {losses[0]:.3f} -> {losses[-1]:.3f}" if losses else "student: no steps",
+              f"; log p of the text {scores(student.forward(tokens[:-1])[0], target)[0].mean():.3f}, the teacher's {logprob.mean():.3f}", sep="")
     lengths = torch.randint(a.prompt // 2, a.prompt + 1, (a.batch,), generator=gen, device="cuda", dtype=torch.int32)
     logits, state = model.forward(tokens[:a.prompt], lengths, last_only=True)
     writer = Writer(model, logits.argmax(1), state, temperature=0.8, top_k=50, top_p=0.95)
