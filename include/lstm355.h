@@ -436,8 +436,8 @@ int lstm_bench_group_exchange(int slots, int members, int groups, int placed, in
 
 /* ---- operators around the cells -----------------------------------------------------------------------------------------
  * What a recurrent language model runs beside the stacks above: a recurrence that is linear in its state (for long sequences
- * and for training), the norm between layers, products of 8-bit operands and the draw of the next token.  They have no
- * handle.  All data pointers are DEVICE and the caller's, `dtype` and `out_dtype` are LSTM_F32 or LSTM_BF16 (raw 16-bit
+ * and for training) and one whose state is a matrix, the norm between layers, products of 8-bit operands, the draw of the next token,
+ * scores of given tokens and the loss against a teacher.  They have no handle.  All data pointers are DEVICE and the caller's, `dtype` and `out_dtype` are LSTM_F32 or LSTM_BF16 (raw 16-bit
  * patterns), lengths `*_ld` and strides are in elements.  Every call is asynchronous on `stream`, allocates nothing, keeps
  * nothing and may be recorded into a graph; two calls may run at the same time if their outputs and workspaces are different
  * ones.  A workspace is 16-byte aligned and need not be initialised; every call that has the argument checks it, also
@@ -578,7 +578,8 @@ int lstm_sample(int M, int V, int dtype, const void* logits, int64_t ld, const u
  *     query.  key_dim <= 256, value_dim <= 65536.  Keys are used as they are; they are meant to have length 1 (lstm_rmsnorm_forward over rows
  *     of key_dim columns with weight key_dim^-1/2).
  *   log_decay fp32 [T, B, heads] or NULL = 0 (the delta rule without gates), meant to be <= 0; what is below -10000, minus infinity too,
- *     forgets all.  beta fp32 [T, B, heads].
+ *     forgets all; where its sum within LSTM_DELTA_STEPS steps passes 88 the growth leaves fp32 and results are not finite.  beta fp32
+ *     [T, B, heads].
  *   lengths [B] int32 or NULL (all T): steps of each sequence, taken into [0, T].  What the inputs hold behind a sequence's end is not
  *     read; o is 0 there, and the state is that of the last step (S0 for length 0).
  *   S0 [B, heads, key_dim, value_dim] fp32 or NULL = zeros; ST the same, or NULL: the final state; it may be S0 itself.
@@ -626,6 +627,7 @@ int lstm_delta_backward(int T, int B, int heads, int key_heads, int key_dim, int
  *     where there are fewer.
  *   stats fp32 [M, 4] or NULL: what lstm_logprobs_backward needs (largest logit, log of the sum over exp(l - largest), entropy, 1 over the sum).
  *   workspace: at least lstm_logprobs_workspace_bytes(M, V, top_n) bytes.
+ * Tokens whose share of the largest one's is below 2^-126 count as 0 in entropy and sums; their log p is what it is.
  */
 size_t lstm_logprobs_workspace_bytes(int M, int V, int top_n);
 int lstm_logprobs_forward(int M, int V, int dtype, const void* logits, int64_t ld, const uint8_t* allowed, int64_t allowed_ld,
@@ -654,7 +656,8 @@ int lstm_logprobs_backward(int M, int V, int dtype, const void* logits, int64_t 
  *     there is, t is softmax(z / temperature) over it and t_r = 0; a row whose list has no words then has loss 0 and no gradient.
  *   temperature 2^-20 .. 2^20.  loss [M] or NULL.  stats fp32 [M, 4] or NULL: what lstm_distill_backward needs.
  *   workspace: at least lstm_distill_workspace_bytes(M, V, K) bytes.
- * A student's logit may be minus infinity (its s_j is 0; the loss is infinite where t_j is not).  A NaN in a row makes its results NaN.
+ * A student's logit may be minus infinity (its s_j is 0; the loss is infinite where t_j is not); a row of nothing else has loss and gradient
+ * NaN, and so have a list of minus infinities alone without teacher_lse and its words.  A NaN in a row makes its results NaN.
  */
 size_t lstm_distill_workspace_bytes(int M, int V, int K);
 int lstm_distill_forward(int M, int V, int K, int dtype, const void* logits, int64_t ld, const int32_t* top_token, int64_t top_token_ld,

@@ -388,6 +388,10 @@ __device__ __forceinline__ void write_square(const float* from, u16* to)
 
 // X, P, y and e of every block, and the planes of keys and queries.  X is built of blocks of 16: those on the diagonal by substitution, a
 // column to a lane; then X_ij = -X_ii sum_k L_ik X_kj, those one off the diagonal first.
+//
+// Measured, one key head of 128 for two of 16 heads: 8 x 1024 steps bf16 53 us without and 61 with what the gradient needs, which is 132 and 214 MB written,
+// 2.5 and 3.5 TB/s; 16 x 300 steps of 8 heads of 100 fp32 46 and 49 us, where the fp32 instruction's products and the chain of the inverse, four
+// barriers long, bound it.
 template <class E, int DKP, bool BACK, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a)
 {
@@ -581,6 +585,10 @@ struct FourSteps {
 // Bound: with few workgroups the chain S -> R -> U -> S of a block, three products with a barrier behind each, by one wave on a SIMD; what is
 // not on it (Q S, P U, O and all loads) stands where the chain waits: Q S behind R's barrier, P U behind the next block's first.  With many, what
 // a tile takes of keys and queries from the caches, which two tiles halve.
+//
+// Measured: 8192 steps of 16 heads of 128 x 128, bf16, 260 us, 2.0 us a block on 128 workgroups (on the fp32 instruction, without planes, 1564 with the
+// preparation, 317 now); 8 x 1024 steps 146 us with the states kept; 16 x 300 steps of 8 heads of 100 x 100, fp32, 65 us.  The matrix units are 17 to 18 %
+// busy while a workgroup has a compute unit.
 template <class E, int DKP, int NT, bool STATES>
 __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)) void delta_walk_kernel(DeltaArgs a, int tiles)
 {
@@ -772,6 +780,9 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
 // Few steps: a thread holds four columns of every 32nd row of S, eight threads 32 columns of a row; the sums over the rows of
 // what key and query find meet in LDS once a step, and
 //     u = b (v - a S'k)     o = scale (a S'q + (q.k) u)     S <- a S + k u'
+//
+// A single step is bound by moving the state once each way: 64 sequences of 16 heads of 128 x 128 34 us for 135 MB, 3.9 TB/s; one sequence of 12 heads of
+// 125 x 125 6.1 us, a launch and three trips to memory one after the other.
 template <class E, int RP>
 __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a, int tiles)
 {
@@ -858,7 +869,8 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a, int tiles)
 }
 
 // Gradient: the walk back over the blocks, NT tiles of 16 columns of dS.  Its chain is dS' -> dU -> dR -> dS; Q' (y dO) stands where dR is
-// waited for.
+// waited for.  Measured: 8 x 1024 steps of 16 heads of 128 x 128, bf16, 197 us, 303 MB of it written (dS', dR and e K dS' in fp32, dv); 16 x 300 steps of 8 heads of
+// 100 x 100, fp32, 67 us.  The matrix units are 14 to 16 % busy: the chain, by two workgroups on a compute unit.
 template <class E, int DKP, int NT>
 __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)) void delta_walk_back_kernel(DeltaArgs a, int tiles)
 {
@@ -1054,7 +1066,10 @@ template <int N>
 __device__ __forceinline__ float row16_shifted(float v) { return dpp_move<0x110 + N>(v); }
 
 // U of every block again, from the state in front of it, 16 columns to a workgroup, and the columns' part of what sums over a
-// step's columns: dR.(v - y K S), -y b dR.(K S), U.(e K dS'); and of S.dS'.
+// step's columns: dR.(v - y K S), -y b dR.(K S), U.(e K dS'); and of S.dS'.  One tile to a workgroup, several workgroups to a compute unit: each is loads, two
+// products and a sum one after the other, and the others fill its waits.  (Eight tiles one after the other, K and X kept and the next tile on its way,
+// took registers for the addresses and halved the workgroups: 163 us against 164.)  Measured: 8 x 1024 steps of 16 heads of 128 x 128, bf16, 164 us for 325 MB from and
+// to memory, 2.0 TB/s; 16 x 300 steps of 8 heads of 100 x 100, fp32, 42 us.
 template <class E, int DKP>
 __global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int tiles)
 {
@@ -1156,7 +1171,11 @@ __global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int
 // (each decay's own terms; as differences of what reaches two neighbouring G, what a strong decay leaves of dg would be lost).
 // A workgroup of eight waves takes a block of one sequence and key head and goes through the heads that share it, 32 columns of S at a time,
 // whose planes its threads make together while the next ones are on their way.  Waves w and w + 4 hold the results of the same 16 steps, each
-// for every other 64 key columns' half; of the pairs of steps the first makes dP, the second dA.
+// for half of a tile's key columns; of the pairs of steps the first makes dP, the second dA.
+//
+// One workgroup has a compute unit, its results 128 registers of each lane: what bounds it is that nobody works while it waits, at the tiles' barriers and
+// in the end of a block, which is a third of it.  Measured: 8 x 1024 steps of 16 heads of 128 x 128, bf16, 260 us for 500 MB, matrix units 13 % busy; 16 x 300
+// steps of 8 heads of 100 x 100, fp32, 151 us, 16 %.
 constexpr int kGradientWaves = 8, kGradientThreads = 64 * kGradientWaves;
 constexpr int kWide = 32, kWideRow = kWide + 8;         // columns of a tile, and its row in LDS
 constexpr int kRowsAtOnce = 128;                        // of S and dS' in LDS
@@ -1476,6 +1495,9 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
 
 // ---- host
 
+// Steps one by one up to here, in blocks from there on.  Blocks of any T up to 32, one by one of 4 / 8 / 12 / 16 steps, us: one sequence of 16 heads of 128 x 128 bf16
+// 17 and 11.4 / 17.2 / 23.8 / 30.2; 16 of them 45.5 and 21.4 / 34.0 / 45.9 / 58.2; 64 of them 152 and 56.8 / 94.8 / 133.6 / 171.6; four of 8 heads of 100 x 100 fp32
+// 24.7 and 11.1 / 14.8 / 20.3 / 25.4.
 constexpr int kFewSteps = 8;
 
 int64_t blocks(int T) { return (T + C - 1) / C; }
@@ -1491,7 +1513,10 @@ hipError_t prepare(const DeltaArgs& a, hipStream_t s)
     return hipGetLastError();
 }
 
-// Two tiles of columns to a workgroup from as many as keep all compute units busy with half the workgroups
+// Two tiles of columns to a workgroup from as many as keep all compute units busy with half the workgroups.  One and two tiles, us, 1024 steps of 16 heads of
+// 128 x 128 bf16: one sequence (64 workgroups of two) 48.5 and 65.3, two 53.3 and 69.5, three 71.3 and 73.7, four (256) 92.8 and 91.3, in fp32 194 and 156;
+// with the gradient 469 and 449.  300 steps of 8 heads of 100 x 100, fp32, with the gradient: four sequences (128) 148 and 165, eight (256) 273 and 252.
+// Keys of more than 128 columns leave no registers for two.
 bool two_tiles(const DeltaArgs& a) { return a.Dv > kTile && (int64_t)a.B * a.heads * ((a.Dv + 2 * kTile - 1) / (2 * kTile)) >= 256; }
 
 template <class Kernel>

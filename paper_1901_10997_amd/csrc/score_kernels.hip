@@ -372,6 +372,9 @@ __device__ __forceinline__ float just_below(float v)
     return v == kNone ? v : __uint_as_float(u >> 31 ? u + 1 : u - 1);
 }
 
+// Measured: 4096 rows of 10 000 bf16 24.5 us, 3.3 TB/s, the vector units 77 % of the busy cycles (an exponential a logit at a quarter of
+// the rate); 700 rows of 10 000 fp32 12 us; with 20 alternatives 256 rows of 32 000 bf16 and a mask 16 us, one row of 10 000 with 5 alternatives
+// 9.1, where the row's eight barriers and the choice of alternatives follow each other on one compute unit.
 template <class E, int VPT, int THREADS, bool TOP>
 __global__ __launch_bounds__(THREADS) void score_kernel(ScoreArgs a, int segs)
 {
@@ -528,6 +531,7 @@ __global__ __launch_bounds__(kThreads) void score_join_kernel(ScoreArgs a, int s
     finish_row(a, m, p, given, mine, TOP ? top.first : nullptr);
 }
 
+// Bound by memory: 700 rows of 10 000 fp32 12 us for 56 MB, 4.7 TB/s.  Nothing is shared between threads, so a workgroup is a stretch of a row.
 template <class E>
 __global__ __launch_bounds__(kThreads) void score_gradient_kernel(ScoreArgs a, int segs)
 {
@@ -713,6 +717,8 @@ __device__ void finish_loss(const DistillArgs& a, int m, const RestPart& rest)
     }
 }
 
+// The words of the list leave the sum over the others by a bit each in LDS, so that the share of all others is a sum and not 1 less what the list has.
+// Measured: 2048 rows of 32 000 bf16 39 us, 3.3 TB/s, vector units 83 % of the busy cycles; 700 rows of 10 000 fp32 14 us.
 template <class E, int VPT, int THREADS>
 __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int segs)
 {
@@ -785,6 +791,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int seg
     }
 }
 
+// 2048 rows of two segments 8.7 us: the loss's chain of logarithms and exponentials in 64 bits, a wave a row.
 template <class E>
 __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a, int segs)
 {
@@ -801,6 +808,7 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a, i
     if (threadIdx.x < 64) finish_loss<E>(a, m, p);
 }
 
+// Bound by memory: 2048 rows of 32 000 bf16 46 us for 262 MB, 5.7 TB/s (some of it from the last-level cache); 700 rows of 10 000 fp32 13 us.
 template <class E>
 __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs a, int segs)
 {

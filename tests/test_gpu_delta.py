@@ -268,3 +268,21 @@ def test_workspaces_of_their_own():
                 got.append(D.forward(c, s, stream=st.cuda_stream)[0].t)
     torch.cuda.synchronize()
     assert all(bool((g == want[i % 2]).all()) for i, g in enumerate(got))
+
+
+@pytest.mark.parametrize("T", [8, 60, 150])
+def test_growth(T):
+    """A gate above 0: with beta = 0 the state only grows, o = scale e^(sum of g) S0'q, up to a sum of 80 in a block."""
+    c = D.make(17, T, 2, 2, 1, 40, 24, "f32")
+    c["beta"] = np.zeros_like(c["beta"])
+    c["g"] = np.full_like(c["g"], 0.5)
+    c["g"][64:] = 0.125
+    o, ST, _ = D.forward(c, D.buffers(c))
+    grown = np.exp(np.cumsum(c["g"], 0))[..., None]                     # [T, batch, heads, 1]
+    q = c["q"].reshape(T, 2, 40)
+    want = c["scale"] * np.einsum("tbd,bhdv->tbhv", q, c["S0"]) * grown
+    # an exponential of up to 47: its argument's rounding 47 u, and that of up to three blocks or of the single steps; sums over 40 terms, relative to their magnitudes
+    size = c["scale"] * np.einsum("tbd,bhdv->tbhv", np.abs(q), np.abs(c["S0"])) * grown
+    assert (np.abs(D.host(o.t).reshape(T, 2, 2, 24) - want) <= 3 * (47 + 40 + 8) * 2.0 ** -24 * size).all()
+    size = np.abs(c["S0"]) * grown[-1][..., None]
+    assert (np.abs(D.host(ST) - c["S0"] * grown[-1][..., None]) <= 3 * (47 + 40 + 8) * 2.0 ** -24 * size).all()

@@ -294,6 +294,18 @@ def test_nan_stays_in_its_row():
         assert got[0][m] == clean[0][m] and np.array_equal(got[1][m], clean[1][m])
 
 
+@pytest.mark.parametrize("V", [50, 40000])
+def test_rows_and_lists_of_minus_infinities(V):
+    l, _, r = make(9, 4, V, "f32")
+    l[1] = -np.inf
+    words, z, _ = teacher(l, r, 6, 1.0, False)
+    z[2] = -np.inf
+    loss, grad = distill(l, "f32", words, z, 1.0, None, np.ones(4))
+    assert np.isnan(loss[1]) and np.isnan(grad[1]).all()
+    assert np.isnan(loss[2]) and np.isnan(grad[2][words[2]]).all()
+    assert np.isfinite(loss[[0, 3]]).all() and np.isfinite(grad[[0, 3]]).all()
+
+
 def test_lists_shared_by_all_rows():
     """A row length of 0: one list for all."""
     import torch
