@@ -43,11 +43,14 @@ static_assert(C == 64 && kWaves * 16 == C, "");
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint16_t u16;
 
-// planes of keys, queries and other operands of type E, and of what a result of that type is made from
+// planes of keys, queries and other operands of type E, and of what a result of that type is made from; whether a walk has registers to keep what
+// it could also work out or read again
 template <class E>
 constexpr int kPlanes = E::kBytes == 2 ? 1 : 3;
 template <class E>
 constexpr int kForResult = E::kBytes == 2 ? 2 : 3;
+template <class E, int DKP, int NT>
+constexpr bool kRoom = NT == 1 && DKP / 64 * kPlanes<E> <= 6;
 
 constexpr f32x4v kZero4 = {0.f, 0.f, 0.f, 0.f};
 __device__ __forceinline__ f32x4v at4(const float* p) { return *(const f32x4v*)p; }
@@ -548,27 +551,36 @@ struct StateTile {
     }
 };
 
-// Four steps of one column in rows of [T, B]: for each block's four, addresses that need one addition.  Steps behind the sequence's end
-// stand for the last one, and are 0 when taken; no load has a branch, and nothing waits for one here.
+// Four steps of one column in rows of [T, B], from `row` of a block on.  Steps behind the sequence's end, `rest` of the last block, stand for the last one,
+// and are 0 when taken; no load has a branch, and nothing waits for one here.  KEPT: the rows' places are worked out once, in sixteen registers (8192
+// steps on one tile to a workgroup 260 us, worked out each time 269); without registers to spare each time.
+template <bool KEPT>
 struct FourRows {
-    int64_t whole[4], last[4];
-    // n: steps of the last block
-    __device__ __forceinline__ FourRows(int row, int64_t stride, int n)
+    int row, rest;
+    int64_t stride, whole[4], last[4];
+    __device__ __forceinline__ FourRows(int row, int64_t stride, int rest) : row(row), rest(rest), stride(stride)
     {
+        if constexpr (KEPT)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            whole[i] = (row + i) * stride;
-            last[i] = min(row + i, n - 1) * stride;
-        }
+            for (int i = 0; i < 4; ++i) {
+                whole[i] = (row + i) * stride;
+                last[i] = min(row + i, rest - 1) * stride;
+            }
+    }
+    __device__ __forceinline__ int64_t at(int i, bool is_last) const
+    {
+        if constexpr (KEPT) return is_last ? last[i] : whole[i];
+        else return min(row + i, (is_last ? rest : C) + zero_here() - 1) * stride;
     }
 };
 template <class E>
 struct FourSteps {
     typename E::T raw[4];
-    __device__ __forceinline__ void load(const typename E::T* from, const FourRows& rows, bool is_last)
+    template <bool KEPT>
+    __device__ __forceinline__ void load(const typename E::T* from, const FourRows<KEPT>& rows, bool is_last)
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = from[is_last ? rows.last[i] : rows.whole[i]];
+        for (int i = 0; i < 4; ++i) raw[i] = from[rows.at(i, is_last)];
     }
     __device__ __forceinline__ f32x4v take(int row, int n) const
     {
@@ -587,10 +599,10 @@ struct FourSteps {
 // a tile takes of keys and queries from the caches, which two tiles halve.
 //
 // Measured: 8192 steps of 16 heads of 128 x 128, bf16, 260 us, 2.0 us a block on 128 workgroups (on the fp32 instruction, without planes, 1564 with the
-// preparation, 317 now); 8 x 1024 steps 146 us with the states kept; 16 x 300 steps of 8 heads of 100 x 100, fp32, 65 us.  The matrix units are 17 to 18 %
-// busy while a workgroup has a compute unit.
+// preparation, 317 now); 8 x 1024 steps 127 us with the states kept, on two workgroups a compute unit (146 on one, as when what could be read again or worked
+// out again was kept in 290 registers); 16 x 300 steps of 8 heads of 100 x 100, fp32, 66 us, one workgroup a compute unit.  The matrix units are 17 to 21 % busy.
 template <class E, int DKP, int NT, bool STATES>
-__global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)) void delta_walk_kernel(DeltaArgs a, int tiles)
+__global__ __launch_bounds__(kThreads, (DKP <= 128 && DKP / 64 * kPlanes<E> * NT <= 4 ? 2 : 1)) void delta_walk_kernel(DeltaArgs a, int tiles)
 {
     using T = typename E::T;
     constexpr int kP = kPlanes<E>, kR = kForResult<E>, LD = DKP + 8, kParts = DKP / 64, kK = DKP / 32, kS = kTile * kSteps;
@@ -617,7 +629,6 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
         const float* beta0 = row_of<F32>(a.beta, a.beta_t, a.beta_b, 0, b, h);
         const T* v0 = row_of<E>(a.v, a.v_t, a.v_b, 0, b, (int64_t)h * a.Dv);
         T* const o0 = (T*)row_of<E>(a.o, a.o_t, a.o_b, 0, b, (int64_t)h * a.Dv);
-        const int64_t o_at[4] = {row * a.o_t, (row + 1) * a.o_t, (row + 2) * a.o_t, (row + 3) * a.o_t};
         float* const sink = at.sink() + lane;
         bf16x8 K[kK][kP], Q[kK][kP], X[2][3], KT[kParts][2][kP], P[2][kR];
         f32x4v y, e, O[NT];
@@ -625,7 +636,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
         FourSteps<F32> beta;
         float last;
         const int rest = len - (blocks - 1) * C;        // steps of the last block
-        const FourRows v_rows(row, a.v_t, rest), beta_rows(row, a.beta_t, rest);
+        const FourRows<kRoom<E, DKP, NT>> v_rows(row, a.v_t, rest), beta_rows(row, a.beta_t, rest);
         const auto load_keys = [&](int c) {
 #pragma unroll
             for (int s = 0; s < kK; ++s) fragment<kP>(K[s], K0 + fragment_at(0, kK, s) + mine, C * DKP);
@@ -656,7 +667,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
         };
         // O of a block whose U is in LDS
         const auto finish = [&](int c) {
-            const int n = len - c * C;
+            const int n = len - c * C, late = row + (kRoom<E, DKP, NT> ? 0 : zero_here());
             T* const to = o0 + (int64_t)c * C * a.o_t;
 #pragma unroll
             for (int q = 0; q < NT; ++q) {
@@ -670,7 +681,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
                 O[q] += pu.total();
                 const int at_col = col + q * kTile;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) E::store(at_col < a.Dv && c >= 0 && row + i < n ? to + o_at[i] + at_col : (T*)sink, O[q][i]);
+                for (int i = 0; i < 4; ++i) E::store(at_col < a.Dv && c >= 0 && row + i < n ? to + (late + i) * a.o_t + at_col : (T*)sink, O[q][i]);
             }
         };
         load_keys(0);
@@ -694,16 +705,16 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
             const int n = len - c * C;
             const bool more = c + 1 < blocks;
             Sum qs[NT];
-            bf16x8 f[NT][kK][3];
             const f32x4v b4 = beta.take(row, n), decay = e, y4 = y;
             const float decayed = last;
+            bf16x8 f[kK][3];
 #pragma unroll
             for (int q = 0; q < NT; ++q) {
                 Sum ks;
 #pragma unroll
-                for (int s = 0; s < kK; ++s) fragment<3>(f[q][s], Ss + q * 3 * kTile * LD + r * LD + 32 * s + 8 * g, kTile * LD);
+                for (int s = 0; s < kK; ++s) fragment<3>(f[s], Ss + q * 3 * kTile * LD + r * LD + 32 * s + 8 * g, kTile * LD);
 #pragma unroll
-                for (int s = 0; s < kK; ++s) multiply(ks, K[s], f[q][s]);
+                for (int s = 0; s < kK; ++s) multiply(ks, K[s], f[s]);
                 const f32x4v v4 = v[q].take(row, n), found = ks.total();
                 f32x4v R;
 #pragma unroll
@@ -728,12 +739,11 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
                 for (int s = 0; s < 2; ++s) fragment<3>(rf[s], Rs + q * 3 * kS + r * kSteps + 32 * s + 8 * g, kS);
 #pragma unroll
                 for (int s = 0; s < kK; ++s) {
-                    if constexpr (kR == 2) {
-                        const bf16x8 two[2] = {f[q][s][0], f[q][s][1]};
-                        multiply(qs[q], Q[s], two);
-                    } else {
-                        multiply(qs[q], Q[s], f[q][s]);
-                    }
+                    bf16x8 again[kR];       // without room S once more: of two tiles it would take a hundred registers from the first product to here
+#pragma unroll
+                    for (int i = 0; i < kR; ++i) again[i] = f[s][i];
+                    if constexpr (!kRoom<E, DKP, NT>) fragment<kR>(again, Ss + q * 3 * kTile * LD + r * LD + 32 * s + 8 * g, kTile * LD);
+                    multiply(qs[q], Q[s], again);
                 }
 #pragma unroll
                 for (int s = 0; s < 2; ++s) multiply(u, X[s], rf[s]);
@@ -869,10 +879,11 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a, int tiles)
 }
 
 // Gradient: the walk back over the blocks, NT tiles of 16 columns of dS.  Its chain is dS' -> dU -> dR -> dS; Q' (y dO) stands where dR is
-// waited for.  Measured: 8 x 1024 steps of 16 heads of 128 x 128, bf16, 197 us, 303 MB of it written (dS', dR and e K dS' in fp32, dv); 16 x 300 steps of 8 heads of
-// 100 x 100, fp32, 67 us.  The matrix units are 14 to 16 % busy: the chain, by two workgroups on a compute unit.
+// waited for.  Measured: 8 x 1024 steps of 16 heads of 128 x 128, bf16, 166 us, two workgroups a compute unit (197 with one, whose 355 registers held
+// results until the block's end; they leave now as soon as they are there), 303 MB written (dS', dR and e K dS' in fp32, dv); 16 x 300 steps of 8 heads of 100 x 100,
+// fp32, 68 us, one workgroup a compute unit.  The matrix units are 16 % busy.
 template <class E, int DKP, int NT>
-__global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)) void delta_walk_back_kernel(DeltaArgs a, int tiles)
+__global__ __launch_bounds__(kThreads, (DKP <= 128 && DKP / 64 * kPlanes<E> * NT <= 4 ? 2 : 1)) void delta_walk_back_kernel(DeltaArgs a, int tiles)
 {
     using T = typename E::T;
     constexpr int kP = kPlanes<E>, LD = DKP + 8, kParts = DKP / 64, kK = DKP / 32, kS = kTile * kSteps;
@@ -898,7 +909,6 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
         const float* beta0 = row_of<F32>(a.beta, a.beta_t, a.beta_b, (int64_t)behind.c * C, b, h);
         const T* dO0 = row_of<E>(a.dO, a.do_t, a.do_b, (int64_t)behind.c * C, b, (int64_t)h * a.Dv);
         T* const dv0 = (T*)row_of<E>(a.dv, a.dv_t, a.dv_b, 0, b, (int64_t)h * a.Dv);
-        const int64_t dv_at[4] = {row * a.dv_t, (row + 1) * a.dv_t, (row + 2) * a.dv_t, (row + 3) * a.dv_t};
         float* const sink = at.sink() + lane;
         const int ld = at.row();
         bf16x8 K[kK][kP], PT[2][3], XT[2][3], KT[kParts][2][kP], QT[kParts][2][kP];
@@ -907,7 +917,6 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
         FourSteps<F32> beta;
         float last;
         const int rest = len - behind.c * C;
-        const FourRows dO_rows(row, a.do_t, rest), beta_rows(row, a.beta_t, rest);
         const auto load_gates = [&]() {
             y = at4(y0 + row);
             e = at4(y0 + C + row);
@@ -917,6 +926,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
 #pragma unroll
             for (int s = 0; s < kK; ++s) fragment<kP>(K[s], K0 + fragment_at(0, kK, s) + mine, C * DKP);
         };
+        const FourRows<kRoom<E, DKP, NT>> dO_rows(row, a.do_t, rest), beta_rows(row, a.beta_t, rest);
         const auto load_pairs = [&](bool is_last) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) fragment<3>(PT[s], PT0 + fragment_at(0, 2, s) + mine, C * C);
@@ -962,7 +972,7 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
             const f32x4v beta4 = b4;
             const bool more = c > 0;
             lds_barrier();
-            f32x4v found[NT], yb;
+            f32x4v yb;
             const float decayed = last;
 #pragma unroll
             for (int i = 0; i < 4; ++i) yb[i] = -y[i] * beta4[i];
@@ -980,8 +990,12 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
                     fragment<kP>(o, Os + q * kP * kS + r * kSteps + 32 * s + 8 * g, kS);
                     multiply(po, PT[s], o);
                 }
-                found[q] = times4(kd.total(), e);
-                store_split<3>(found[q] + po.total(), Us + q * 3 * kS + r * kSteps + row, kS);
+                const f32x4v found = times4(kd.total(), e);
+                store_split<3>(found + po.total(), Us + q * 3 * kS + r * kSteps + row, kS);
+                // the workspace's rows hold a whole number of two tiles
+                float* const f0 = at.found(k) + (row + zero_here()) * ld + col + q * kTile;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f0[i * ld] = found[i];
                 store_split<3>(times4(scaled4(y, a.scale), dO[q]), Ys + q * 3 * kS + r * kSteps + row, kS);
             }
             lds_barrier();
@@ -995,9 +1009,9 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
             load_gates();
             load_keys();
             Sum sums[NT][kParts];
-            f32x4v dR[NT];
 #pragma unroll
             for (int q = 0; q < NT; ++q) {
+                if (q > 0) one_by_one();
                 Sum dr;
                 bf16x8 uf[2][3], yf[2][3];
 #pragma unroll
@@ -1010,8 +1024,15 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
                 for (int m = 0; m < kParts; ++m)
 #pragma unroll
                     for (int s = 0; s < 2; ++s) multiply(sums[q][m], QT[m][s], yf[s]);
-                dR[q] = dr.total();
-                store_split<3>(times4(yb, dR[q]), Zs + q * 3 * kS + r * kSteps + row, kS);
+                const f32x4v dR = dr.total();
+                store_split<3>(times4(yb, dR), Zs + q * 3 * kS + r * kSteps + row, kS);
+                const int at_col = col + q * kTile, late = row + zero_here();
+                float* const left = at.dR(k) + late * ld + at_col;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    left[i * ld] = dR[i];
+                    E::store(at_col < a.Dv && row + i < n ? dv0 + (int64_t)c * C * a.dv_t + (late + i) * a.dv_t + at_col : (T*)sink, beta4[i] * dR[i]);
+                }
             }
             QT0 -= more ? keys_step : 0;
             load_columns(QT, QT0);
@@ -1029,15 +1050,6 @@ __global__ __launch_bounds__(kThreads, (DKP / 64 * kPlanes<E> * NT <= 2 ? 2 : 1)
                     dS[q].v[m] = scaled4(dS[q].v[m], decayed) + sums[q][m].total();
                 }
                 dS[q].publish(Ds + q * 3 * kTile * LD, w, r, g);
-                const int at_col = col + q * kTile;
-                // the workspace's rows hold a whole number of two tiles
-                float *const left = at.dR(k) + row * ld + at_col, *const f0 = at.found(k) + row * ld + at_col;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    left[i * ld] = dR[q][i];
-                    f0[i * ld] = found[q][i];
-                    E::store(at_col < a.Dv && row + i < n ? dv0 + (int64_t)c * C * a.dv_t + dv_at[i] + at_col : (T*)sink, beta4[i] * dR[q][i]);
-                }
             }
             KT0 -= more ? keys_step : 0;
             load_columns(KT, KT0);
@@ -1086,9 +1098,9 @@ __global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int
     const Place<E, DKP, true> at(a);
     StateTile<DKP> S, dS;
     const int ld = at.row();
+    const FourRows<false> v_rows(row, a.v_t, k.n), beta_rows(row, a.beta_t, k.n);
     FourSteps<E> raw;
     FourSteps<F32> raw_beta;
-    const FourRows v_rows(row, a.v_t, k.n), beta_rows(row, a.beta_t, k.n);
     S.load(a.states + k.index * a.Dk * a.Dv, a.Dv, a, w, g, col);
     dS.load(at.dS(k), ld, a, w, g, col);
     raw.load(row_of<E>(a.v, a.v_t, a.v_b, k.t0, b, (int64_t)h * a.Dv + min(col, a.Dv - 1)), v_rows, true);
@@ -1496,7 +1508,7 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
 // ---- host
 
 // Steps one by one up to here, in blocks from there on.  Blocks of any T up to 32, one by one of 4 / 8 / 12 / 16 steps, us: one sequence of 16 heads of 128 x 128 bf16
-// 17 and 11.4 / 17.2 / 23.8 / 30.2; 16 of them 45.5 and 21.4 / 34.0 / 45.9 / 58.2; 64 of them 152 and 56.8 / 94.8 / 133.6 / 171.6; four of 8 heads of 100 x 100 fp32
+// 17 and 11.4 / 17.2 / 23.8 / 30.2; 16 of them 40 and 21.4 / 34.0 / 45.9 / 58.2; 64 of them 121 and 56.8 / 94.8 / 133.6 / 171.6; four of 8 heads of 100 x 100 fp32
 // 24.7 and 11.1 / 14.8 / 20.3 / 25.4.
 constexpr int kFewSteps = 8;
 
@@ -1514,8 +1526,8 @@ hipError_t prepare(const DeltaArgs& a, hipStream_t s)
 }
 
 // Two tiles of columns to a workgroup from as many as keep all compute units busy with half the workgroups.  One and two tiles, us, 1024 steps of 16 heads of
-// 128 x 128 bf16: one sequence (64 workgroups of two) 48.5 and 65.3, two 53.3 and 69.5, three 71.3 and 73.7, four (256) 92.8 and 91.3, in fp32 194 and 156;
-// with the gradient 469 and 449.  300 steps of 8 heads of 100 x 100, fp32, with the gradient: four sequences (128) 148 and 165, eight (256) 273 and 252.
+// 128 x 128 bf16: one sequence (64 workgroups of two) 48 and 72, two 54 and 75, three 73 and 79, four (256) 94 and 93, in fp32 196 and 160;
+// with the gradient 467 and 453.  300 steps of 8 heads of 100 x 100, fp32, with the gradient: four sequences (128) 149 and 169, eight (256) 274 and 254.
 // Keys of more than 128 columns leave no registers for two.
 bool two_tiles(const DeltaArgs& a) { return a.Dv > kTile && (int64_t)a.B * a.heads * ((a.Dv + 2 * kTile - 1) / (2 * kTile)) >= 256; }
 
