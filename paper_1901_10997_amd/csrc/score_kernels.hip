@@ -17,7 +17,8 @@
 // 2^c (sum + e ln 2 mean), mean being the sum of weight times exponent.  (An exponential of the difference in fp32, with what its product loses put
 // in, and every sum in 64 bits took 62.7 us for 4096 rows of 10 000 bf16.)  Rows whose o is 2^20 or more take the differences.
 // A clamp of the exponent at -200, whose weight is 0, takes in minus infinity and, where such tokens do not exist, NaN.
-// Up to eight weights are added in fp32, those sums in fp64.
+// Up to eight weights are added in fp32, those sums in fp64; the largest logit's own, which is 1, and those of its equals are counted beside them, so that
+// the log p of a token that has nearly all mass is as exact as the sum over the others.
 //
 // Top alternatives: threads in groups; the n-th largest of the groups' own largest logits is a border that n logits reach, and only n groups
 // hold logits that reach it; these are put in order by counting who is in front of whom.  A logit and its index make one key, so
@@ -372,7 +373,7 @@ __device__ __forceinline__ float just_below(float v)
     return v == kNone ? v : __uint_as_float(u >> 31 ? u + 1 : u - 1);
 }
 
-// Measured: 4096 rows of 10 000 bf16 24.5 us, 3.3 TB/s, the vector units 77 % of the busy cycles (an exponential a logit at a quarter of
+// Measured: 4096 rows of 10 000 bf16 27 us (24.4 without the count of the largest), 3.0 TB/s, the vector units 77 % of the busy cycles (an exponential a logit at a quarter of
 // the rate); 700 rows of 10 000 fp32 12 us; with 20 alternatives 256 rows of 32 000 bf16 and a mask 16 us, one row of 10 000 with 5 alternatives
 // 9.1, where the row's eight barriers and the choice of alternatives follow each other on one compute unit.
 template <class E, int VPT, int THREADS, bool TOP>
@@ -394,7 +395,7 @@ __global__ __launch_bounds__(THREADS) void score_kernel(ScoreArgs a, int segs)
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
             if (c < chunks) mask[c].load(allowed, first + (c * THREADS + tid) * W, a.V);
-    float v[VPT], biggest = kNone;
+    float v[VPT], most[kChunks], biggest = kNone;
     const auto column = [&](int c) { return Piece<E>::column(first + (c * THREADS + tid) * W, a.V); };
     const int token = a.token ? a.token[m] : -1;
     const bool given = token >= 0 && token < a.V;
@@ -414,15 +415,17 @@ __global__ __launch_bounds__(THREADS) void score_kernel(ScoreArgs a, int segs)
                 for (int i = 0; i < W; ++i)
                     if (i == place + shift) given_logit = v[c * W + i] == v[c * W + i] ? v[c * W + i] : kNone;
             }
+            most[c] = kNone;
 #pragma unroll
-            for (int i = 0; i < W; ++i) biggest = fmaxf(biggest, v[c * W + i]);
+            for (int i = 0; i < W; ++i) most[c] = fmaxf(most[c], v[c * W + i]);
+            biggest = fmaxf(biggest, most[c]);
         }
     const float own = biggest;
     Part p;
     p.biggest = biggest = group_max(biggest, sh);
     if (given && token >= first && token < first + kChunks * kChunk) mine = given_logit;
     p.sum = p.mean = 0.0;
-    int front = 0;
+    int front = 0, ones = 0;
     const Exponents x(kLog2e, biggest);
     if (x.usual) {
 #pragma unroll
@@ -435,11 +438,21 @@ __global__ __launch_bounds__(THREADS) void score_kernel(ScoreArgs a, int segs)
                     sum += w;
                     mean = fmaf(w, t, mean);
                 }
+                if (most[c] == biggest) {       // a row's largest is here: the others once more
+                    sum = mean = 0.f;
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        const float t = x.of(v[c * W + i]), w = v[c * W + i] == biggest ? 0.f : __builtin_amdgcn_exp2f(t);
+                        sum += w;
+                        mean = fmaf(w, t, mean);
+                        ones += v[c * W + i] == biggest;
+                    }
+                }
                 p.sum += sum;
                 p.mean += mean;
             }
         const double scale = exp2(x.c), s = p.sum, t = p.mean;
-        p.sum = scale * (s + x.e * kLn2 * t);
+        p.sum = scale * (s + x.e * kLn2 * t) + ones;
         p.mean = scale * kLn2 * (t * (1.0 + x.e) + x.c * s);
     } else if (biggest > kNone) {
 #pragma unroll
@@ -577,7 +590,10 @@ __global__ __launch_bounds__(kThreads) void score_gradient_kernel(ScoreArgs a, i
             if (at <= token && token < at + W)
 #pragma unroll
                 for (int i = 0; i < W; ++i)
-                    if (at + i == token && v[i] > kNone) g[i] += dlogprob;
+                    if (at + i == token && v[i] > kNone) {      // 1 - p as such: little is left of it where the token is nearly sure
+                        const float t = x.of(v[i]);
+                        g[i] = -(__builtin_amdgcn_exp2f(t) * per_sum) * fmaf(t, slope, constant - dlogprob) - dlogprob * expm1f(below(v[i], biggest) - log_sum);
+                    }
         } else {
 #pragma unroll
             for (int i = 0; i < W; ++i) {

@@ -278,6 +278,34 @@ def test_distill_of_far_logits(name):
         check_distill(l, name, words, z, 1.0, lse, dloss, distill(l, name, words, z, 1.0, lse, dloss))
 
 
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V", [(1, 10000), (600, 3000), (2, 70000)])
+def test_nearly_sure_tokens(M, V, name):
+    """log p, entropy and 1 - p of a token that leaves 1e-2 to 1e-12 to all others, to a few steps of fp32 of themselves."""
+    r = np.random.default_rng(10)
+    l = r.normal(size=(M, V))
+    token = r.integers(0, V, M)
+    l[np.arange(M), token] = np.log(V) + np.linspace(5, 28, M) if M > 1 else 24.0
+    l = rounded(l, name)
+    d = l - l.max(1, keepdims=True)
+    others = np.where(np.arange(V) == token[:, None], 0, np.exp(d))
+    rest = others.sum(1)
+    log_p, entropy = -np.log1p(rest), np.log1p(rest) - (others * d).sum(1) / (1 + rest)
+    got, _, _ = score(l, name, token, top_n=1)
+    logprob, h, top_logprob = (got[k].double().cpu().numpy() for k in ("logprob", "entropy", "top_logprob"))
+    # a weight 2^-t is off by its argument's rounding, t up to 52: half a step of it is 2^-19, times ln 2; the exponential's own and the sums' a few 2^-24; the sum over
+    # thousands of others takes the mean of the first.  One of it all as a bound, and the result's own rounding.  The sum, 1 and the others, is in
+    # 64 bits: behind the 1 come one addition in its thread, six in its wave, up to fifteen of waves, and as many again where segments are joined, each half a step: 2^-53
+    sums = 2 * (1 + 6 + 15) * 2.0 ** -53
+    tol = 2.0 ** -19 * np.log(2) + 8 * 2.0 ** -24
+    assert (logprob <= 0).all() and (np.abs(logprob - log_p) <= tol * -log_p + sums).all() and (top_logprob[:, 0] == logprob).all()
+    assert (np.abs(h - entropy) <= 2 * tol * entropy + sums).all()
+    if name == "f32":
+        grad = score_gradient(l, name, token, np.ones(M), np.zeros(M))
+        grad = np.asarray(grad, np.float64)[np.arange(M), token]
+        assert (np.abs(grad - rest / (1 + rest)) <= (tol + 8 * 2.0 ** -24) * rest + sums).all()
+
+
 def test_nan_stays_in_its_row():
     l, _, r = make(7, 5, 3000, "f32")
     words, z, lse = teacher(l, r, 8, 1.0, True)
