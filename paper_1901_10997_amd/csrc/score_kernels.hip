@@ -373,9 +373,9 @@ __device__ __forceinline__ float just_below(float v)
     return v == kNone ? v : __uint_as_float(u >> 31 ? u + 1 : u - 1);
 }
 
-// Measured: 4096 rows of 10 000 bf16 27 us (24.4 without the count of the largest), 3.0 TB/s, the vector units 77 % of the busy cycles (an exponential a logit at a quarter of
-// the rate); 700 rows of 10 000 fp32 12 us; with 20 alternatives 256 rows of 32 000 bf16 and a mask 16 us, one row of 10 000 with 5 alternatives
-// 9.1, where the row's eight barriers and the choice of alternatives follow each other on one compute unit.
+// Measured: 4096 rows of 10 000 bf16 27 us (24.4 without the count of the largest), 3.0 TB/s, the vector units 73 % of the busy cycles (an exponential a logit at a quarter of
+// the rate); 700 rows of 10 000 fp32 13 us; with 20 alternatives 256 rows of 32 000 bf16 and a mask 16 us, one row of 10 000 with 5 alternatives
+// 9.2, where the row's eight barriers and the choice of alternatives follow each other on one compute unit.
 template <class E, int VPT, int THREADS, bool TOP>
 __global__ __launch_bounds__(THREADS) void score_kernel(ScoreArgs a, int segs)
 {
