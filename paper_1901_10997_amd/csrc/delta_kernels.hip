@@ -20,8 +20,9 @@
 //
 // Products.  The matrix instruction of bf16 is sixteen times as fast as that of fp32, so fp32 values are split into planes, each the
 // nearest bf16 to what those in front of it leave: three hold all 24 bits.  The product of planes i and j counts where i + j is below the
-// larger number of planes; what is left out is below 2^-24 (three planes) or 2^-16 (two) of the product.  Keys and queries in bf16 are one
-// plane.  Everything that reaches a state or an fp32 result has three; where a result is rounded to bf16 (2^-9) two do.
+// larger number of planes; what is left out is below 2^-24 of the product.  Keys, queries and dO in bf16 are one plane, everything else is three, also where
+// the result is rounded to bf16: a sum may be far smaller than its terms.  (Two there were off by 2^-17 of a term; 8192 steps of 16 heads of 128 x 128 bf16
+// took 307 us so and take 330, a training step of 8 x 1024 805 and 844.)
 #include "common.h"
 #include "elem.h"
 #include "lm_ops.h"
@@ -43,12 +44,9 @@ static_assert(C == 64 && kWaves * 16 == C, "");
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint16_t u16;
 
-// planes of keys, queries and other operands of type E, and of what a result of that type is made from; whether a walk has registers to keep what
-// it could also work out or read again
+// planes of keys, queries and other operands of type E; whether a walk has registers to keep what it could also work out or read again
 template <class E>
 constexpr int kPlanes = E::kBytes == 2 ? 1 : 3;
-template <class E>
-constexpr int kForResult = E::kBytes == 2 ? 2 : 3;
 template <class E, int DKP, int NT>
 constexpr bool kRoom = NT == 1 && DKP / 64 * kPlanes<E> <= 6;
 
@@ -235,9 +233,9 @@ __device__ __forceinline__ const typename E::T* row_of(const void* p, int64_t t_
 // tiles of columns add to sums over a step's columns, and dq and dk of heads that share a key.
 template <class E, int DKP, bool BACK>
 struct Place {
-    static constexpr int kP = kPlanes<E>, kR = kForResult<E>;
+    static constexpr int kP = kPlanes<E>;
     static constexpr int64_t kMatrix = (int64_t)kP * C * DKP, kKeys = (BACK ? 4 : 3) * kMatrix;
-    static constexpr int64_t kHead = (BACK ? 9 : 3 + kR) * C * C + 4 * C;
+    static constexpr int64_t kHead = (BACK ? 9 : 6) * C * C + 4 * C;
     static constexpr int kParts = 256;      // sums of a tile of columns: 64 each of three, and one
     const DeltaArgs& a;
     const int64_t key_blocks, head_blocks;
@@ -482,7 +480,7 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a)
         }
     }
     if constexpr (BACK) write_square<3, true>(Ps, at.PT(k));
-    else write_square<kForResult<E>, false>(Ps, at.P(k));
+    else write_square<3, false>(Ps, at.P(k));
 #pragma unroll
     for (int off = 1; off < 4; ++off) {
         __syncthreads();
@@ -605,9 +603,9 @@ template <class E, int DKP, int NT, bool STATES>
 __global__ __launch_bounds__(kThreads, (DKP <= 128 && DKP / 64 * kPlanes<E> * NT <= 4 ? 2 : 1)) void delta_walk_kernel(DeltaArgs a, int tiles)
 {
     using T = typename E::T;
-    constexpr int kP = kPlanes<E>, kR = kForResult<E>, LD = DKP + 8, kParts = DKP / 64, kK = DKP / 32, kS = kTile * kSteps;
+    constexpr int kP = kPlanes<E>, LD = DKP + 8, kParts = DKP / 64, kK = DKP / 32, kS = kTile * kSteps;
     extern __shared__ u16 planes[];
-    u16 *const Ss = planes, *const Rs = Ss + NT * 3 * kTile * LD, *const Us = Rs + NT * 3 * kS, *const Es = Us + NT * kR * kS;
+    u16 *const Ss = planes, *const Rs = Ss + NT * 3 * kTile * LD, *const Us = Rs + NT * 3 * kS, *const Es = Us + NT * 3 * kS;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const unsigned id = by_xcd(blockIdx.x, gridDim.x);
     const int tile = (int)(id % tiles), h = (int)(id / tiles % a.heads), b = (int)(id / tiles / a.heads);
@@ -630,7 +628,7 @@ __global__ __launch_bounds__(kThreads, (DKP <= 128 && DKP / 64 * kPlanes<E> * NT
         const T* v0 = row_of<E>(a.v, a.v_t, a.v_b, 0, b, (int64_t)h * a.Dv);
         T* const o0 = (T*)row_of<E>(a.o, a.o_t, a.o_b, 0, b, (int64_t)h * a.Dv);
         float* const sink = at.sink() + lane;
-        bf16x8 K[kK][kP], Q[kK][kP], X[2][3], KT[kParts][2][kP], P[2][kR];
+        bf16x8 K[kK][kP], Q[kK][kP], X[2][3], KT[kParts][2][kP], P[2][3];
         f32x4v y, e, O[NT];
         FourSteps<E> v[NT];
         FourSteps<F32> beta;
@@ -663,7 +661,7 @@ __global__ __launch_bounds__(kThreads, (DKP <= 128 && DKP / 64 * kPlanes<E> * NT
         };
         const auto load_pairs = [&]() {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) fragment<kR>(P[s], P0 + fragment_at(0, 2, s) + mine, C * C);
+            for (int s = 0; s < 2; ++s) fragment<3>(P[s], P0 + fragment_at(0, 2, s) + mine, C * C);
         };
         // O of a block whose U is in LDS
         const auto finish = [&](int c) {
@@ -674,8 +672,8 @@ __global__ __launch_bounds__(kThreads, (DKP <= 128 && DKP / 64 * kPlanes<E> * NT
                 Sum pu;
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    bf16x8 uf[kR];
-                    fragment<kR>(uf, Us + q * kR * kS + r * kSteps + 32 * s + 8 * g, kS);
+                    bf16x8 uf[3];
+                    fragment<3>(uf, Us + q * 3 * kS + r * kSteps + 32 * s + 8 * g, kS);
                     multiply(pu, P[s], uf);
                 }
                 O[q] += pu.total();
@@ -739,11 +737,9 @@ __global__ __launch_bounds__(kThreads, (DKP <= 128 && DKP / 64 * kPlanes<E> * NT
                 for (int s = 0; s < 2; ++s) fragment<3>(rf[s], Rs + q * 3 * kS + r * kSteps + 32 * s + 8 * g, kS);
 #pragma unroll
                 for (int s = 0; s < kK; ++s) {
-                    bf16x8 again[kR];       // without room S once more: of two tiles it would take a hundred registers from the first product to here
-#pragma unroll
-                    for (int i = 0; i < kR; ++i) again[i] = f[s][i];
-                    if constexpr (!kRoom<E, DKP, NT>) fragment<kR>(again, Ss + q * 3 * kTile * LD + r * LD + 32 * s + 8 * g, kTile * LD);
-                    multiply(qs[q], Q[s], again);
+                    // without room S once more: of two tiles it would take a hundred registers from the first product to here
+                    if constexpr (!kRoom<E, DKP, NT>) fragment<3>(f[s], Ss + q * 3 * kTile * LD + r * LD + 32 * s + 8 * g, kTile * LD);
+                    multiply(qs[q], Q[s], f[s]);
                 }
 #pragma unroll
                 for (int s = 0; s < 2; ++s) multiply(u, X[s], rf[s]);
@@ -762,7 +758,7 @@ __global__ __launch_bounds__(kThreads, (DKP <= 128 && DKP / 64 * kPlanes<E> * NT
                 bf16x8 ef[2][3];
 #pragma unroll
                 for (int s = 0; s < 2; ++s) fragment<3>(ef[s], Es + q * 3 * kS + r * kSteps + 32 * s + 8 * g, kS);
-                store_split<kR>(U[q], Us + q * kR * kS + r * kSteps + row, kS);
+                store_split<3>(U[q], Us + q * 3 * kS + r * kSteps + row, kS);
 #pragma unroll
                 for (int m = 0; m < kParts; ++m) {
                     Sum sum;
@@ -1196,11 +1192,11 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
 {
     using T = typename E::T;
     extern __shared__ float lds[];
-    constexpr int kP = kPlanes<E>, kR = kForResult<E>, kRows = DKP < kRowsAtOnce ? DKP : kRowsAtOnce, kTurns = DKP / kRows;
+    constexpr int kP = kPlanes<E>, kRows = DKP < kRowsAtOnce ? DKP : kRowsAtOnce, kTurns = DKP / kRows;
     constexpr int kParts = DKP / 32, kEach = kRows / 32;        // tiles of 16 key columns of a wave, those of a turn
     constexpr int kLoads = kRows * kWide / 4 / kGradientThreads;
-    // S (three planes), dS' and U of a tile of columns; in their place later dP and dA
-    u16 *const Ss = (u16*)lds, *const Ds = Ss + 3 * kRows * kWideRow, *const Us = Ds + kR * kRows * kWideRow;
+    // S, dS' and U of a tile of columns, three planes each; in their place later dP and dA
+    u16 *const Ss = (u16*)lds, *const Ds = Ss + 3 * kRows * kWideRow, *const Us = Ds + 3 * kRows * kWideRow;
     float *const Ps = lds, *const As = Ps + C * kRow;
     __shared__ double Gs[C];
     __shared__ float ys[C], es[C], betas[C], overs[kGradientWaves][C], fronts[2][C], backs[C], dbs[2][C];
@@ -1260,7 +1256,7 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
         fetch_states(0);
         fetch_rows(0);
         for (int wide = 0; wide < wides; ++wide) {
-            bf16x8 dO[kP], dR[3], U[kR];
+            bf16x8 dO[kP], dR[3], U[3];
 #pragma unroll
             for (int turn = 0; turn < kTurns; ++turn) {
                 lds_barrier();
@@ -1275,13 +1271,13 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
                     const int p = threadIdx.x + i * kGradientThreads, d = p / (kWide / 4), from = p % (kWide / 4) * 4;
                     const bool there = turn * kRows + d < a.Dk;
                     store_split<3>(if4(there, s4[i].take(wide * kWide + from, a.Dv)), Ss + d * kWideRow + from, kRows * kWideRow);
-                    store_split<kR>(if4(there, within4(ds4[i], wide * kWide + from, a.Dv)), Ds + d * kWideRow + from, kRows * kWideRow);
+                    store_split<3>(if4(there, within4(ds4[i], wide * kWide + from, a.Dv)), Ds + d * kWideRow + from, kRows * kWideRow);
                 }
                 fetch_states(min(wide * kTurns + turn + 1, wides * kTurns - 1));
                 if (turn == 0) fetch_rows(min(wide + 1, wides - 1));
                 lds_barrier();
                 if (turn == 0) {
-                    fragment<kR>(U, Us + mine * kWideRow + 8 * g, C * kWideRow);
+                    fragment<3>(U, Us + mine * kWideRow + 8 * g, C * kWideRow);
                     const auto multiply_pairs = [&](const auto& first) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
@@ -1293,19 +1289,14 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
                     if (half == 0) multiply_pairs(dO);
                     else multiply_pairs(dR);
                 }
-                bf16x8 Rr[kR];
-#pragma unroll
-                for (int i = 0; i < kR; ++i) Rr[i] = dR[i];
 #pragma unroll
                 for (int m = 0; m < kEach; ++m) {
-                    bf16x8 s[3], ds[kR], sr[kR];
+                    bf16x8 s[3], ds[3];
                     const int at_row = (16 * (half * kEach + m) + r) * kWideRow + 8 * g;
                     fragment<3>(s, Ss + at_row, kRows * kWideRow);
-                    fragment<kR>(ds, Ds + at_row, kRows * kWideRow);
-#pragma unroll
-                    for (int i = 0; i < kR; ++i) sr[i] = s[i];
+                    fragment<3>(ds, Ds + at_row, kRows * kWideRow);
                     multiply(dq[turn * kEach + m], dO, s);
-                    multiply(from_dR[turn * kEach + m], Rr, sr);
+                    multiply(from_dR[turn * kEach + m], dR, s);
                     multiply(from_dS[turn * kEach + m], U, ds);
                 }
             }
@@ -1415,13 +1406,13 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
         }
         const float last = ys[C - 1];
         __syncthreads();
-        bf16x8 both[2][kR], dPa[2][kR], dPt[2][kR];
+        bf16x8 both[2][3], dPa[2][3], dPt[2][3];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int from = 32 * s + 8 * g;
-            split8<kR>(at4(As + mine * kRow + from) + down4(As + from * kRow + mine, kRow), at4(As + mine * kRow + from + 4) + down4(As + (from + 4) * kRow + mine, kRow), both[s]);
-            split8<kR>(at4(Ps + mine * kRow + from), at4(Ps + mine * kRow + from + 4), dPa[s]);
-            split8<kR>(down4(Ps + from * kRow + mine, kRow), down4(Ps + (from + 4) * kRow + mine, kRow), dPt[s]);
+            split8<3>(at4(As + mine * kRow + from) + down4(As + from * kRow + mine, kRow), at4(As + mine * kRow + from + 4) + down4(As + (from + 4) * kRow + mine, kRow), both[s]);
+            split8<3>(at4(Ps + mine * kRow + from), at4(Ps + mine * kRow + from + 4), dPa[s]);
+            split8<3>(down4(Ps + from * kRow + mine, kRow), down4(Ps + (from + 4) * kRow + mine, kRow), dPt[s]);
         }
         if (wave == 0) {
             double from = (double)fronts[0][lane] + fronts[1][lane], to = backs[lane], dg = 0.0;
@@ -1542,7 +1533,7 @@ hipError_t walk_by(Kernel kernel, const DeltaArgs& a, int tiles, size_t lds, hip
 template <class E, int DKP, int NT, bool STATES>
 hipError_t walk(const DeltaArgs& a, hipStream_t s)
 {
-    const size_t lds = NT * kTile * (3 * (DKP + 8) + (6 + kForResult<E>)*kSteps) * sizeof(u16);
+    const size_t lds = NT * kTile * (3 * (DKP + 8) + 9 * kSteps) * sizeof(u16);
     return walk_by(delta_walk_kernel<E, DKP, NT, STATES>, a, (a.Dv + NT * kTile - 1) / (NT * kTile), lds, s);
 }
 template <class E, int DKP, int NT>
@@ -1577,7 +1568,7 @@ hipError_t backward(const DeltaArgs& a, hipStream_t s)
     if (e != hipSuccess || a.T == 0) return e;
     hipLaunchKernelGGL((delta_update_kernel<E, DKP>), dim3((unsigned)(blocks(a.T) * a.B * a.heads * tiles)), dim3(kThreads), 0, s, a, tiles);
     constexpr int kRows = DKP < kRowsAtOnce ? DKP : kRowsAtOnce;
-    const size_t lds = std::max<size_t>(((3 + kForResult<E>)*kRows + 3 * C) * kWideRow * sizeof(u16), 2 * C * kRow * sizeof(float));
+    const size_t lds = std::max<size_t>((6 * kRows + 3 * C) * kWideRow * sizeof(u16), 2 * C * kRow * sizeof(float));
     const auto kernel = a.Dv % 4 == 0 ? delta_gradient_kernel<E, DKP, true> : delta_gradient_kernel<E, DKP, false>;
     e = allow_dynamic_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
