@@ -652,8 +652,9 @@ int lstm_logprobs_backward(int M, int V, int dtype, const void* logits, int64_t 
  *   top_token [M, K] int32, top_logit [M, K] fp32 (z): the teacher's words, in any order, K 1 .. 256; row lengths >= 0 (0: one list for
  *     all).  A word outside 0 .. V - 1 (padding) or one that stands in the list before does not count.  Minus infinity is a share of 0.
  *   teacher_lse [M] fp32: the log of the teacher's sum of exp(z / temperature) over its whole vocabulary (0 where top_logit are log
- *     probabilities and temperature is 1); what the list leaves of 1 is one share t_r for all other words together.  NULL: the list is all
- *     there is, t is softmax(z / temperature) over it and t_r = 0; a row whose list has no words then has loss 0 and no gradient.
+ *     probabilities and temperature is 1); what the list leaves of 1 is one share t_r for all other words together, 0 where the list is
+ *     the whole vocabulary.  NULL: the list is all there is, t is softmax(z / temperature) over it and t_r = 0; a row whose list has no words then
+ *     has loss 0 and no gradient.
  *   temperature 2^-20 .. 2^20.  loss [M] or NULL.  stats fp32 [M, 4] or NULL: what lstm_distill_backward needs.
  *   workspace: at least lstm_distill_workspace_bytes(M, V, K) bytes.
  * A student's logit may be minus infinity (its s_j is 0; the loss is infinite where t_j is not); a row of nothing else has loss and gradient

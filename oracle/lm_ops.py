@@ -320,6 +320,8 @@ def distill(logits, top_token, top_logit, temperature, teacher_lse=None, dloss=N
         log_s = _log_shares(l[m] / heat)
         outside = np.ones(V, bool)
         outside[words] = False
+        if not outside.any():       # nobody is left to have what rounding leaves of 1
+            t_rest = 0.0
         with np.errstate(divide="ignore", invalid="ignore"):
             used = t > 0
             total = (t[used] * (np.log(t[used]) - log_s[words[used]])).sum()

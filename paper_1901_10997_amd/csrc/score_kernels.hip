@@ -710,7 +710,7 @@ __device__ void finish_loss(const DistillArgs& a, int m, const RestPart& rest)
     loss = wave_add(loss);
     if (a.teacher_lse) {
         const double left = 1.0 - wave_add(in_teacher);
-        t_rest = left < 0.0 ? 0.0 : left;
+        t_rest = left < 0.0 || count == a.V ? 0.0 : left;       // a list of all words leaves nobody to have what rounding leaves of 1
     }
     if (lane != 0) return;
     // what a word outside the list gets, as a factor of its s; where that would leave the range of fp32 the logarithm of what is
