@@ -721,7 +721,8 @@ __device__ void finish_loss(const DistillArgs& a, int m, const RestPart& rest)
     } else if (t_rest != 0.0) {
         const double r = log(t_rest) - (log_rest - log_sum);
         loss += t_rest * r;
-        factor = r < 40.0 ? 1.0 - exp(r) : r != r ? r : log(t_rest) - log_rest;
+        // (words that are all minus infinity have no s to take it from)
+        if (some_rest) factor = r < 40.0 ? 1.0 - exp(r) : r != r ? r : log(t_rest) - log_rest;
     }
     if (a.loss) a.loss[m] = (float)(loss * heat * heat);
     if (a.stats) {
