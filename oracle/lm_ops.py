@@ -322,6 +322,9 @@ def distill(logits, top_token, top_logit, temperature, teacher_lse=None, dloss=N
         outside[words] = False
         if not outside.any():       # nobody is left to have what rounding leaves of 1
             t_rest = 0.0
+        elif teacher_lse is not None and (l[m, outside] == -np.inf).all():
+            size = (t[t > 0] * abs(z[t > 0])).sum() + abs(float(teacher_lse[m])) + 1
+            t_rest = t_rest if t_rest > 2.0 ** -22 * size else 0.0
         with np.errstate(divide="ignore", invalid="ignore"):
             used = t > 0
             total = (t[used] * (np.log(t[used]) - log_s[words[used]])).sum()

@@ -711,6 +711,17 @@ __device__ void finish_loss(const DistillArgs& a, int m, const RestPart& rest)
     if (a.teacher_lse) {
         const double left = 1.0 - wave_add(in_teacher);
         t_rest = left < 0.0 || count == a.V ? 0.0 : left;       // a list of all words leaves nobody to have what rounding leaves of 1
+        if (t_rest > 0.0 && !some_rest) {
+            // Nor does a student to whom all others are minus infinity.  A share t_j is off by its logit's and lse's half steps of 2^-24, their sum by those
+            // weighed; four times that, for an lse that was worked out in fp32.
+            double size = 0.0;
+#pragma unroll
+            for (int i = 0; i < kOfLane; ++i) {
+                const double t = w[i].counts ? exp(w[i].logit - norm) : 0.0;
+                size += t != 0.0 ? t * fabs(w[i].logit) : 0.0;
+            }
+            if (t_rest <= 0x1p-22 * (wave_add(size) + fabs(norm) + 1.0)) t_rest = 0.0;
+        }
     }
     if (lane != 0) return;
     // what a word outside the list gets, as a factor of its s; where that would leave the range of fp32 the logarithm of what is

@@ -1,4 +1,5 @@
-"""Distillation of a student whose words outside the list are all minus infinity: they get no gradient, whatever the teacher leaves them."""
+"""Distillation of a student whose words outside the list are all minus infinity: they get no gradient, whatever the teacher leaves them.  What
+it leaves is a share that nobody has (an infinite loss), or no more than the rounding of the teacher's numbers (no share)."""
 import numpy as np
 import pytest
 
@@ -41,3 +42,24 @@ def test_nobody_has_the_share(M, V, K, name):
         check_distill(l, name, words, z, 1.0, lse, dloss, got)
         assert (got[1][:-1][l[:-1] == -np.inf] == 0).all()
         assert (np.isposinf(got[0][:-1]) == (off > 0)).all() and np.isfinite(got[0][-1])
+
+
+def test_oracle_takes_rounding_for_no_share():
+    l, words, z, r = student(1, 200, 50, 6)
+    loss, grad = O.distill(l, words, z, 1.0, own_lse(z), np.ones(200))
+    assert np.isfinite(loss).all() and (grad[:-1][l[:-1] == -np.inf] == 0).all()
+    loss, _ = O.distill(l, words, z, 1.0, own_lse(z) + 1e-5, np.ones(200))     # more than rounding
+    assert (loss[:-1] == np.inf).all() and np.isfinite(loss[-1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("heat", [1.0, 0.5, 3.0])
+def test_rounding_is_no_share(heat, name):
+    l, words, z, r = student(3, 300, 50, 6, name)
+    dloss = np.float32(r.normal(size=300)).astype(np.float64)
+    lse = own_lse(z, heat)
+    got = distill(l, name, words, z, heat, lse, dloss)
+    assert np.isfinite(got[0]).all() and np.isfinite(got[1]).all()
+    rows = slice(0, 299)        # the last one has others, whose share is as good as its rounding
+    check_distill(l[rows], name, words[rows], z[rows], heat, lse[rows], dloss[rows], (got[0][rows], got[1][rows]))
