@@ -884,7 +884,10 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
         const bool whole = first + (c + 1) * kChunk <= a.V;
         float v[W];
         piece[c].take(col, a.V, whole, v);
-        if (!far_rest) {
+        if (factor == 0.f) {        // nothing to anybody outside the list: no teacher, whatever the row holds, or the others have what is theirs
+#pragma unroll
+            for (int i = 0; i < W; ++i) v[i] = 0.f;
+        } else if (!far_rest) {
 #pragma unroll
             for (int i = 0; i < W; ++i) v[i] = kept * __builtin_amdgcn_exp2f(x.or_nan(v[i]));
         } else {
