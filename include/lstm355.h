@@ -655,7 +655,8 @@ int lstm_logprobs_backward(int M, int V, int dtype, const void* logits, int64_t 
  *     probabilities and temperature is 1); what the list leaves of 1 is one share t_r for all other words together, 0 where the list is
  *     the whole vocabulary.  NULL: the list is all there is, t is softmax(z / temperature) over it and t_r = 0; a row whose list has no words then
  *     has loss 0 and no gradient.
- *   temperature 2^-20 .. 2^20.  loss [M] or NULL.  stats fp32 [M, 4] or NULL: what lstm_distill_backward needs.
+ *   temperature 2^-20 .. 2^20, in 64 bits: t_r is a difference that takes what rounding does to it in full, so it has to be the one that teacher_lse
+ *     was made with.  loss [M] or NULL.  stats fp32 [M, 4] or NULL: what lstm_distill_backward needs.
  *   workspace: at least lstm_distill_workspace_bytes(M, V, K) bytes.
  * A student's logit may be minus infinity (its s_j is 0, and so is its gradient outside the list; the loss is infinite where t_j, or t_r of words that
  * are all so, is not; such a t_r of no more than 2^-22 (|teacher_lse| + sum_j t_j |z_j| / temperature + 1) is what rounding leaves, and counts as 0); a row
@@ -664,7 +665,7 @@ int lstm_logprobs_backward(int M, int V, int dtype, const void* logits, int64_t 
  */
 size_t lstm_distill_workspace_bytes(int M, int V, int K);
 int lstm_distill_forward(int M, int V, int K, int dtype, const void* logits, int64_t ld, const int32_t* top_token, int64_t top_token_ld,
-                         const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, float temperature, float* loss,
+                         const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, double temperature, float* loss,
                          float* stats, void* workspace, size_t workspace_bytes, void* stream);
 /*
  * Its gradient by the student's logits, rounded to dtype:  dl_j = dloss temperature (s_j - t_j) in the list, dloss temperature
@@ -672,7 +673,7 @@ int lstm_distill_forward(int M, int V, int K, int dtype, const void* logits, int
  * itself.
  */
 int lstm_distill_backward(int M, int V, int K, int dtype, const void* logits, int64_t ld, const int32_t* top_token, int64_t top_token_ld,
-                          const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, float temperature,
+                          const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, double temperature,
                           const float* stats, const float* dloss, void* dlogits, int64_t dlogits_ld, void* stream);
 
 #ifdef __cplusplus

@@ -141,8 +141,8 @@ def load(build_if_missing: bool = True):
             ("lstm_delta_backward", [ci] * 7 + [vp, i64, i64] * 5 + [vp, c.c_float, vp, vp, i64, i64, vp] + [vp, i64, i64] * 5 + [vp, vp, sz, vp]),
             ("lstm_logprobs_forward", [ci] * 3 + [vp, i64, vp, i64] + [vp] * 5 + [ci] + [vp] * 3 + [sz, vp]),
             ("lstm_logprobs_backward", [ci] * 3 + [vp, i64, vp, i64] + [vp] * 5 + [i64, vp]),
-            ("lstm_distill_forward", [ci] * 4 + [vp, i64] * 3 + [vp, c.c_float] + [vp] * 3 + [sz, vp]),
-            ("lstm_distill_backward", [ci] * 4 + [vp, i64] * 3 + [vp, c.c_float] + [vp] * 3 + [i64, vp])):
+            ("lstm_distill_forward", [ci] * 4 + [vp, i64] * 3 + [vp, c.c_double] + [vp] * 3 + [sz, vp]),
+            ("lstm_distill_backward", [ci] * 4 + [vp, i64] * 3 + [vp, c.c_double] + [vp] * 3 + [i64, vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = ci, types
     _lib = lib

@@ -421,7 +421,7 @@ static int check_distill(const char* entry, const DistillArgs& a, int dtype)
     if (!score_fits(a.M, a.V)) return bad(entry, "V outside 1 .. 2^20, M outside 0 .. 2^22 - 1, or more than 2^24 pieces of 8192 logits");
     if (a.K < 1 || a.K > kDistillMaxTop) return bad(entry, "K outside 1 .. 256");
     if (!is_type(dtype)) return bad(entry, kType);
-    if (!(a.temperature >= 0x1p-20f && a.temperature <= 0x1p20f)) return bad(entry, "temperature outside 2^-20 .. 2^20");
+    if (!(a.temperature >= 0x1p-20 && a.temperature <= 0x1p20)) return bad(entry, "temperature outside 2^-20 .. 2^20");
     if (a.M > 0 && (!a.logits || !a.top_token || !a.top_logit)) return bad(entry, kNull);
     if (!matrix_ok(a.logits, a.ld, a.M, a.V, dtype) || !floats({a.top_token, a.top_logit, a.teacher_lse, a.loss, a.stats, a.dloss}))
         return bad(entry, "rows overlap, or a pointer is not aligned to its element type");
@@ -435,7 +435,7 @@ size_t lstm_distill_workspace_bytes(int M, int V, int K)
 }
 
 int lstm_distill_forward(int M, int V, int K, int dtype, const void* logits, int64_t ld, const int32_t* top_token, int64_t top_token_ld,
-                         const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, float temperature, float* loss,
+                         const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, double temperature, float* loss,
                          float* stats, void* workspace, size_t workspace_bytes, void* stream)
 {
     static const char entry[] = "lstm_distill_forward";
@@ -450,7 +450,7 @@ int lstm_distill_forward(int M, int V, int K, int dtype, const void* logits, int
 }
 
 int lstm_distill_backward(int M, int V, int K, int dtype, const void* logits, int64_t ld, const int32_t* top_token, int64_t top_token_ld,
-                          const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, float temperature,
+                          const float* top_logit, int64_t top_logit_ld, const float* teacher_lse, double temperature,
                           const float* stats, const float* dloss, void* dlogits, int64_t dlogits_ld, void* stream)
 {
     static const char entry[] = "lstm_distill_backward";

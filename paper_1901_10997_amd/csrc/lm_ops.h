@@ -191,7 +191,7 @@ struct DistillArgs {
     const float* top_logit;
     int64_t top_logit_ld;
     const float* teacher_lse;
-    float temperature;
+    double temperature;
     float* loss;
     float* stats;                           // [M, 4]; written by the forward, read by the backward
     const float* dloss;                     // backward

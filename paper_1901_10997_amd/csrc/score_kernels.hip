@@ -65,7 +65,8 @@ struct Exponents {
     }
 };
 // exp(scale d) for d <= 0, rows that are not usual; NaN stays
-__device__ __forceinline__ float far_weight(float d, float scale) { return expf(d * scale); }
+__device__ __forceinline__ float far_weight(float d) { return expf(d); }
+__device__ __forceinline__ float far_weight(float d, double scale) { return expf((float)(d * scale)); }
 
 // Over the 64 lanes, in every lane, by moves between registers: neighbour, other pair of the quad, half-row mirror, row mirror, then
 // the two rows of a half and the two halves.
@@ -460,7 +461,7 @@ __global__ __launch_bounds__(THREADS) void score_kernel(ScoreArgs a, int segs)
             if (c < chunks)
 #pragma unroll
                 for (int i = 0; i < W; ++i) {
-                    const float d = below(v[c * W + i], biggest), w = v[c * W + i] > kNone ? far_weight(d, 1.f) : 0.f;
+                    const float d = below(v[c * W + i], biggest), w = v[c * W + i] > kNone ? far_weight(d) : 0.f;
                     p.sum += w;
                     p.mean += w > 0.f ? w * d : 0.f;
                 }
@@ -598,7 +599,7 @@ __global__ __launch_bounds__(kThreads) void score_gradient_kernel(ScoreArgs a, i
 #pragma unroll
             for (int i = 0; i < W; ++i) {
                 const bool exists = v[i] > kNone;
-                const float d = exists ? below(v[i], biggest) : kNone, p = exists ? far_weight(d, 1.f) * stats[3] : 0.f;
+                const float d = exists ? below(v[i], biggest) : kNone, p = exists ? far_weight(d) * stats[3] : 0.f;
                 const float bracket = p > 0.f ? fmaf(dentropy, d - log_sum + entropy, dlogprob) : 0.f;
                 g[i] = exists ? (at + i == token ? dlogprob : 0.f) - p * bracket : 0.f;
             }
@@ -628,7 +629,7 @@ __device__ __forceinline__ Listed listed(const DistillArgs& a, int m, int j)
     if (j < a.K) {
         w.token = a.top_token[m * a.top_token_ld + j];
         w.counts = w.token >= 0 && w.token < a.V;
-        w.logit = (double)a.top_logit[m * a.top_logit_ld + j] / (double)a.temperature;
+        w.logit = (double)a.top_logit[m * a.top_logit_ld + j] / a.temperature;
     }
     return w;
 }
@@ -786,7 +787,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int seg
     RestPart p = {0.0, group_max(biggest, sh), twice};
     double unused = 0.0;
     int none = 0;
-    const Exponents x(kLog2e / (double)a.temperature, p.biggest);
+    const Exponents x(kLog2e / a.temperature, p.biggest);
     if (x.usual) {
         double mean = 0.0;
 #pragma unroll
@@ -804,7 +805,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int seg
             }
         p.sum = exp2(x.c) * (p.sum + x.e * kLn2 * mean);
     } else {
-        const float per = 1.f / a.temperature;
+        const double per = 1.0 / a.temperature;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
             if (c < chunks)
@@ -830,7 +831,7 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a, i
     const float biggest = group_max(p.biggest, sh);
     const bool some = p.sum > 0.0 || p.sum != p.sum;
     double unused = 0.0;
-    p.sum = some ? p.sum * exp((double)below(p.biggest, biggest) / (double)a.temperature) : 0.0;
+    p.sum = some ? p.sum * exp((double)below(p.biggest, biggest) / a.temperature) : 0.0;
     group_add(p.sum, unused, p.twice, sh);
     p.biggest = biggest;
     if (threadIdx.x < 64) finish_loss<E>(a, m, p);
@@ -853,8 +854,8 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
     for (int c = 0; c < kChunks; ++c)
         if (c < chunks) piece[c].load(row, first + (c * kThreads + (int)threadIdx.x) * W, a.V);
     const float biggest = stats[0], factor = stats[2];
-    const double per_sum = fabs((double)stats[1]), per = 1.0 / (double)a.temperature;
-    const float scale = a.dloss[m] * a.temperature;
+    const double per_sum = fabs((double)stats[1]), per = 1.0 / a.temperature;
+    const float scale = (float)(a.dloss[m] * a.temperature);
     Listed w = listed(a, m, threadIdx.x);
     if (stats[1] < 0.f) w.counts = w.counts && !again(a, m, threadIdx.x, w.token);
     // a word of the list that lies in this segment: its logit is read in front of all writes, which may be to the same place
@@ -864,7 +865,7 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
     if (a.teacher_lse) {
         log_t -= a.teacher_lse[m];
     } else {
-        const float z = w.counts ? (float)(w.logit * (double)a.temperature) : kNone;
+        const float z = w.counts ? (float)(w.logit * a.temperature) : kNone;
         const bool bad = __syncthreads_or(z != z);
         const float most = group_max(z, sh);
         log_t -= (bad ? (double)__builtin_nanf("") : (double)most * per) + (double)stats[3];
@@ -876,7 +877,13 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
     __syncthreads();
     const Exponents x(kLog2e * per, biggest);
     const bool far_rest = factor > 1.f || !x.usual;
-    const float kept = (float)((double)scale * (factor > 1.f ? 1.0 : (double)factor) * per_sum * (x.usual ? exp2(x.c) : 1.0)), fper = (float)per;
+    const float kept = (float)((double)scale * (factor > 1.f ? 1.0 : (double)factor) * per_sum * (x.usual ? exp2(x.c) : 1.0));
+    // a weight 2^t is off by e ln 2 t of itself, e being what k has been rounded by, and that is as much as its argument's rounding may be
+    const float off = (float)(x.e * kLn2);
+    const auto weight = [&](float l) {
+        const float t = x.or_nan(l), w = __builtin_amdgcn_exp2f(t);
+        return fmaf(w * t, off, w);
+    };
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
         if (c >= chunks) continue;
@@ -889,12 +896,12 @@ __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs 
             for (int i = 0; i < W; ++i) v[i] = 0.f;
         } else if (!far_rest) {
 #pragma unroll
-            for (int i = 0; i < W; ++i) v[i] = kept * __builtin_amdgcn_exp2f(x.or_nan(v[i]));
+            for (int i = 0; i < W; ++i) v[i] = kept * weight(v[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                const float d = below(v[i], biggest) * fper;
-                v[i] = (x.usual ? kept * __builtin_amdgcn_exp2f(x.or_nan(v[i])) : kept * expf(d)) - (factor > 1.f ? scale * expf(fminf(d + factor, 0.f)) : 0.f);
+                const double d = (double)below(v[i], biggest) * per;
+                v[i] = kept * (x.usual ? weight(v[i]) : expf((float)d)) - (factor > 1.f ? scale * expf(fminf((float)(d + (double)factor), 0.f)) : 0.f);
             }
         }
         store_piece<E>(to, col, a.V, whole, v);
