@@ -563,6 +563,12 @@ __global__ __launch_bounds__(kThreads) void score_gradient_kernel(ScoreArgs a, i
     // log p = ln 2 (t + c) - log S up to e t, which is below a step of it; p = 2^t 2^c / S; bracket = constant + t slope
     const float per_sum = (float)(exp2(x.c) * (double)stats[3]);
     const float slope = dentropy * (float)kLn2, constant = dlogprob + dentropy * (float)(kLn2 * x.c - (double)log_sum + (double)entropy);
+    // the given token's, with 1 - p and log p + entropy as such: of both little is left where it is nearly sure, and neither may be what rounding leaves
+    // of dlogprob
+    const auto of_given = [&](float l, float p) {
+        const float log_p = below(l, biggest) - log_sum;
+        return (p > 0.f ? -p * (dentropy * (log_p + entropy)) : 0.f) - dlogprob * expm1f(log_p);
+    };
     constexpr int kChunks = kSweep / kThreads / W, kChunk = kThreads * W;
     const int chunks = (end - first + kChunk - 1) / kChunk;
     Piece<E> piece[kChunks];
@@ -591,17 +597,14 @@ __global__ __launch_bounds__(kThreads) void score_gradient_kernel(ScoreArgs a, i
             if (at <= token && token < at + W)
 #pragma unroll
                 for (int i = 0; i < W; ++i)
-                    if (at + i == token && v[i] > kNone) {      // 1 - p as such: little is left of it where the token is nearly sure
-                        const float t = x.of(v[i]);
-                        g[i] = -(__builtin_amdgcn_exp2f(t) * per_sum) * fmaf(t, slope, constant - dlogprob) - dlogprob * expm1f(below(v[i], biggest) - log_sum);
-                    }
+                    if (at + i == token && v[i] > kNone) g[i] = of_given(v[i], __builtin_amdgcn_exp2f(x.of(v[i])) * per_sum);
         } else {
 #pragma unroll
             for (int i = 0; i < W; ++i) {
                 const bool exists = v[i] > kNone;
                 const float d = exists ? below(v[i], biggest) : kNone, p = exists ? far_weight(d) * stats[3] : 0.f;
                 const float bracket = p > 0.f ? fmaf(dentropy, d - log_sum + entropy, dlogprob) : 0.f;
-                g[i] = exists ? (at + i == token ? dlogprob : 0.f) - p * bracket : 0.f;
+                g[i] = !exists ? 0.f : at + i == token ? of_given(v[i], p) : -p * bracket;
             }
         }
         store_piece<E>(to, col, a.V, whole, g);
