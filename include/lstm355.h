@@ -437,8 +437,8 @@ int lstm_bench_group_exchange(int slots, int members, int groups, int placed, in
 /* ---- operators around the cells -----------------------------------------------------------------------------------------
  * What a recurrent language model runs beside the stacks above: a recurrence that is linear in its state (for long sequences
  * and for training) and one whose state is a matrix, the norm between layers, products of 8-bit operands, the draw of the next token,
- * scores of given tokens and the loss against a teacher.  They have no handle.  All data pointers are DEVICE and the caller's, `dtype` and `out_dtype` are LSTM_F32 or LSTM_BF16 (raw 16-bit
- * patterns), lengths `*_ld` and strides are in elements.  Every call is asynchronous on `stream`, allocates nothing, keeps
+ * scores of given tokens and the loss against a teacher.  They have no handle.  All data pointers are DEVICE and the caller's,
+ * `dtype` and `out_dtype` are LSTM_F32 or LSTM_BF16 (raw 16-bit patterns), lengths `*_ld` and strides are in elements.  Every call is asynchronous on `stream`, allocates nothing, keeps
  * nothing and may be recorded into a graph; two calls may run at the same time if their outputs and workspaces are different
  * ones.  A workspace is 16-byte aligned and need not be initialised; every call that has the argument checks it, also
  * lstm_matmul_fp8 and lstm_sample, which ask for 256 bytes and touch none of them.  Errors: LSTM_ERR_ARG (NULL where required, a size, type,
@@ -575,7 +575,8 @@ int lstm_sample(int M, int V, int dtype, const void* logits, int64_t ld, const u
  *
  *   q, k [T, B, key_heads * key_dim], v and o [T, B, heads * value_dim] of dtype: row (t, b) at + t*_t + b*_b, the heads of a row side by
  *     side; input strides are >= 0, rows of o lie apart.  heads is a multiple of key_heads: heads h key_heads / heads .. share a key and a
- *     query.  key_dim <= 256, value_dim <= 65536.  Keys are used as they are; they are meant to have length 1 (lstm_rmsnorm_forward over rows
+ *     query.  key_dim <= 256, value_dim <= 65536, heads <= 65536, T <= 2^30; B * heads, B * heads * ceil(value_dim / 16), and that for every
+ *     LSTM_DELTA_STEPS steps of T, stay below 2^24.  Keys are used as they are; they are meant to have length 1 (lstm_rmsnorm_forward over rows
  *     of key_dim columns with weight key_dim^-1/2).
  *   log_decay fp32 [T, B, heads] or NULL = 0 (the delta rule without gates), meant to be <= 0; what is below -10000, minus infinity too,
  *     forgets all; where its sum within LSTM_DELTA_STEPS steps passes 88 the growth leaves fp32 and results are not finite.  beta fp32
@@ -585,10 +586,11 @@ int lstm_sample(int M, int V, int dtype, const void* logits, int64_t ld, const u
  *   S0 [B, heads, key_dim, value_dim] fp32 or NULL = zeros; ST the same, or NULL: the final state; it may be S0 itself.
  *   states: NULL, or fp32 [ceil(T / LSTM_DELTA_STEPS), B, heads, key_dim, value_dim], what lstm_delta_backward needs: the state in front of
  *     every LSTM_DELTA_STEPS-th step that a sequence has (the others are left as they are).
- *   workspace: at least lstm_delta_workspace_bytes(..., backward = 0) bytes.
+ *   workspace: at least lstm_delta_workspace_bytes(..., backward = 0) bytes (what the larger need of the two types is).
  * T = 0 moves S0 to ST; B = 0 does nothing.  State and gates are fp32, o alone is rounded to dtype.  T = 1 is the form for serving: one
- * launch, S0 = ST in place.  A NaN or an infinity in a step makes what its sequence and head give from the first step of its
- * LSTM_DELTA_STEPS on not finite, in the columns of v that it reaches; other heads and sequences do not see it.
+ * launch, S0 = ST in place.  A NaN or an infinity in a step can make what its sequence and head give from the first step of its
+ * LSTM_DELTA_STEPS on not finite, and makes what it reaches from its own on so, in the columns of v that it reaches (one of a query its own step's o alone);
+ * other heads and sequences do not see it.
  */
 enum { LSTM_DELTA_STEPS = 64 };
 size_t lstm_delta_workspace_bytes(int T, int B, int heads, int key_heads, int key_dim, int value_dim, int backward);
@@ -615,7 +617,7 @@ int lstm_delta_backward(int T, int B, int heads, int key_heads, int key_dim, int
                         void* stream);
 
 /*
- * Scores of M rows of logits [M, V] (dtype; V <= 2^20): with log p_j = l_j - log sum_i exp(l_i) over the tokens that exist,
+ * Scores of M rows of logits [M, V] (dtype; V <= 2^20, M < 2^22, M * ceil(V / 8192) < 2^24): with log p_j = l_j - log sum_i exp(l_i) over the tokens that exist,
  *   allowed uint8 [M, V] (allowed_ld = 0: one row for all) or NULL, NaN and minus infinity: as in lstm_sample, tokens that do not exist.
  *     Tokens whose logit is plus infinity share all mass equally.
  *   token [M] int32: the given token of each row; outside 0 .. V - 1 (padding) the row has none: logprob 0, rank -1.
@@ -644,7 +646,7 @@ int lstm_logprobs_backward(int M, int V, int dtype, const void* logits, int64_t 
                            int64_t dlogits_ld, void* stream);
 
 /*
- * Distillation: how far a student's logits [M, V] (dtype) are from a teacher of whom each row names K words with their logits,
+ * Distillation: how far a student's logits [M, V] (dtype; sizes as for the scores) are from a teacher of whom each row names K words with their logits,
  *
  *     s = softmax(l / temperature)     t_j = exp(z_j / temperature - teacher_lse)     t_r = max(0, 1 - sum_j t_j)     s_r = 1 - sum_j s_j
  *     loss = temperature^2 ( sum over the list of t_j (log t_j - log s_j) + t_r (log t_r - log s_r) )

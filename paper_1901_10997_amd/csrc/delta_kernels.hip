@@ -22,7 +22,7 @@
 // nearest bf16 to what those in front of it leave: three hold all 24 bits.  The product of planes i and j counts where i + j is below the
 // larger number of planes; what is left out is below 2^-24 of the product.  Keys, queries and dO in bf16 are one plane, everything else is three, also where
 // the result is rounded to bf16: a sum may be far smaller than its terms.  (Two there were off by 2^-17 of a term; 8192 steps of 16 heads of 128 x 128 bf16
-// took 307 us so and take 330, a training step of 8 x 1024 805 and 844.)
+// took 307 us so and take 330, a training step of 8 x 1024 805 and 811.)
 #include "common.h"
 #include "elem.h"
 #include "lm_ops.h"
@@ -390,8 +390,8 @@ __device__ __forceinline__ void write_square(const float* from, u16* to)
 // X, P, y and e of every block, and the planes of keys and queries.  X is built of blocks of 16: those on the diagonal by substitution, a
 // column to a lane; then X_ij = -X_ii sum_k L_ik X_kj, those one off the diagonal first.
 //
-// Measured, one key head of 128 for two of 16 heads: 8 x 1024 steps bf16 53 us without and 61 with what the gradient needs, which is 132 and 214 MB written,
-// 2.5 and 3.5 TB/s; 16 x 300 steps of 8 heads of 100 fp32 46 and 49 us, where the fp32 instruction's products and the chain of the inverse, four
+// Measured, one key head of 128 for two of 16 heads: 8 x 1024 steps bf16 54 us without and 62 with what the gradient needs, which is 148 and 214 MB written,
+// 2.7 and 3.5 TB/s; 16 x 300 steps of 8 heads of 100 fp32 46 and 49 us, where the fp32 instruction's products and the chain of the inverse, four
 // barriers long, bound it.
 template <class E, int DKP, bool BACK, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a)
@@ -551,7 +551,7 @@ struct StateTile {
 
 // Four steps of one column in rows of [T, B], from `row` of a block on.  Steps behind the sequence's end, `rest` of the last block, stand for the last one,
 // and are 0 when taken; no load has a branch, and nothing waits for one here.  KEPT: the rows' places are worked out once, in sixteen registers (8192
-// steps on one tile to a workgroup 260 us, worked out each time 269); without registers to spare each time.
+// steps on one tile to a workgroup 260 us, worked out each time 269, when reads and updates had two planes); without registers to spare each time.
 template <bool KEPT>
 struct FourRows {
     int row, rest;
@@ -596,9 +596,10 @@ struct FourSteps {
 // not on it (Q S, P U, O and all loads) stands where the chain waits: Q S behind R's barrier, P U behind the next block's first.  With many, what
 // a tile takes of keys and queries from the caches, which two tiles halve.
 //
-// Measured: 8192 steps of 16 heads of 128 x 128, bf16, 260 us, 2.0 us a block on 128 workgroups (on the fp32 instruction, without planes, 1564 with the
-// preparation, 317 now); 8 x 1024 steps 127 us with the states kept, on two workgroups a compute unit (146 on one, as when what could be read again or worked
-// out again was kept in 290 registers); 16 x 300 steps of 8 heads of 100 x 100, fp32, 66 us, one workgroup a compute unit.  The matrix units are 17 to 21 % busy.
+// Measured: 8192 steps of 16 heads of 128 x 128, bf16, 279 us, 2.2 us a block on 128 workgroups (on the fp32 instruction, without planes, 1564 with the
+// preparation, 330 now; a sum for each order of planes, so that the products do not wait for each other, changed nothing); 8 x 1024 steps 132 us with the
+// states kept, on two workgroups a compute unit (with two planes where there were two 127, and on one, when what could be read again or worked out again
+// was kept in 290 registers, 146); 16 x 300 steps of 8 heads of 100 x 100, fp32, 68 us, one workgroup a compute unit.  The matrix units are 17 to 23 % busy.
 template <class E, int DKP, int NT, bool STATES>
 __global__ __launch_bounds__(kThreads, (DKP <= 128 && DKP / 64 * kPlanes<E> * NT <= 4 ? 2 : 1)) void delta_walk_kernel(DeltaArgs a, int tiles)
 {
@@ -876,7 +877,7 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a, int tiles)
 
 // Gradient: the walk back over the blocks, NT tiles of 16 columns of dS.  Its chain is dS' -> dU -> dR -> dS; Q' (y dO) stands where dR is
 // waited for.  Measured: 8 x 1024 steps of 16 heads of 128 x 128, bf16, 166 us, two workgroups a compute unit (197 with one, whose 355 registers held
-// results until the block's end; they leave now as soon as they are there), 303 MB written (dS', dR and e K dS' in fp32, dv); 16 x 300 steps of 8 heads of 100 x 100,
+// results until the block's end; they leave now as soon as they are there), 305 MB written (dS', dR and e K dS' in fp32, dv); 16 x 300 steps of 8 heads of 100 x 100,
 // fp32, 68 us, one workgroup a compute unit.  The matrix units are 16 % busy.
 template <class E, int DKP, int NT>
 __global__ __launch_bounds__(kThreads, (DKP <= 128 && DKP / 64 * kPlanes<E> * NT <= 4 ? 2 : 1)) void delta_walk_back_kernel(DeltaArgs a, int tiles)
@@ -1182,8 +1183,8 @@ __global__ __launch_bounds__(kThreads) void delta_update_kernel(DeltaArgs a, int
 // for half of a tile's key columns; of the pairs of steps the first makes dP, the second dA.
 //
 // One workgroup has a compute unit, its results 128 registers of each lane: what bounds it is that nobody works while it waits, at the tiles' barriers and
-// in the end of a block, which is a third of it.  Measured: 8 x 1024 steps of 16 heads of 128 x 128, bf16, 260 us for 500 MB, matrix units 13 % busy; 16 x 300
-// steps of 8 heads of 100 x 100, fp32, 151 us, 16 %.
+// in the end of a block, which is a third of it.  Measured: 8 x 1024 steps of 16 heads of 128 x 128, bf16, 262 us for 470 MB, matrix units 18 % busy; 16 x 300
+// steps of 8 heads of 100 x 100, fp32, 150 us, 16 %.
 constexpr int kGradientWaves = 8, kGradientThreads = 64 * kGradientWaves;
 constexpr int kWide = 32, kWideRow = kWide + 8;         // columns of a tile, and its row in LDS
 constexpr int kRowsAtOnce = 128;                        // of S and dS' in LDS
@@ -1486,9 +1487,11 @@ __global__ __launch_bounds__(kGradientThreads, 2) void delta_gradient_kernel(Del
 
 // ---- host
 
-// Steps one by one up to here, in blocks from there on.  Blocks of any T up to 32, one by one of 4 / 8 / 12 / 16 steps, us: one sequence of 16 heads of 128 x 128 bf16
-// 17 and 11.4 / 17.2 / 23.8 / 30.2; 16 of them 40 and 21.4 / 34.0 / 45.9 / 58.2; 64 of them 121 and 56.8 / 94.8 / 133.6 / 171.6; four of 8 heads of 100 x 100 fp32
-// 24.7 and 11.1 / 14.8 / 20.3 / 25.4.
+// Steps one by one up to here, in blocks from there on.  Blocks of 4 to 16 steps, one by one of 4 / 8 / 12 / 16, us: one sequence of 16 heads of 128 x 128 bf16
+// 17 and 12.2 / 17.0 / 23.8 / 30.3; 16 of them 42 and 16.8 / 27.1 / 37.2 / 46.7; 64 of them 115 and 55.3 / 92.0 / 130 / 168; four of 8 heads of 100 x 100 fp32
+// 24.7 and 11.7 / 15.1 / 20.3 / 25.8.  Four and 64 of 8 heads of 64 x 64 bf16 14.9 and 11.9 / 13.4 / 18.7 / 23.6, 36 and 14.0 / 22.4 / 30.3 / 38.2; four of 4 heads of
+// 256 x 256 bf16 22 and 14.5 / 23.7 / 33.3 / 42.7.  Where the states alone fill the card, wide keys in fp32 gain from more single steps: 32 sequences of 4 heads of
+// 256 x 256 111 and 21.1 / 30.5 / 39.5 / 47.2.
 constexpr int kFewSteps = 8;
 
 int64_t blocks(int T) { return (T + C - 1) / C; }
@@ -1505,8 +1508,9 @@ hipError_t prepare(const DeltaArgs& a, hipStream_t s)
 }
 
 // Two tiles of columns to a workgroup from as many as keep all compute units busy with half the workgroups.  One and two tiles, us, 1024 steps of 16 heads of
-// 128 x 128 bf16: one sequence (64 workgroups of two) 48 and 72, two 54 and 75, three 73 and 79, four (256) 94 and 93, in fp32 196 and 160;
-// with the gradient 467 and 453.  300 steps of 8 heads of 100 x 100, fp32, with the gradient: four sequences (128) 149 and 169, eight (256) 274 and 254.
+// 128 x 128 bf16: one sequence (64 workgroups of two) 55 and 81, two 56 and 80, three 75 and 82, four (256) 87 and 94, in fp32 180 and 152;
+// with the gradient 475 and 460.  300 steps of 8 heads of 100 x 100, fp32, with the gradient: four sequences (128) 152 and 170, eight (256) 254 and 240.
+// 16 heads of 64 x 64 bf16: four sequences (128) 58 and 74, eight (256) 86 and 92, with the gradient 482 and 464, in fp32 176 and 151.
 // Keys of more than 128 columns leave no registers for two.
 bool two_tiles(const DeltaArgs& a) { return a.Dv > kTile && (int64_t)a.B * a.heads * ((a.Dv + 2 * kTile - 1) / (2 * kTile)) >= 256; }
 
@@ -1585,7 +1589,7 @@ size_t delta_workspace_bytes(int T, int B, int heads, int key_heads, int Dk, int
     return std::max<size_t>(256, std::max(bytes_by_width<F32>(a, back), bytes_by_width<Bf16>(a, back)));
 }
 
-// a grid's threads have to stay under 2^32
+// a grid's threads have to stay under 2^32 (the blocks' gradient has twice as many to a workgroup; its workspace, 74 KB and more a block and head, ends in front of that)
 bool delta_fits(int T, int B, int heads, int Dk, int Dv)
 {
     const int64_t of_state = (int64_t)B * heads * ((Dv + kTile - 1) / kTile);

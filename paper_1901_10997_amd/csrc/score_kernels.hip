@@ -750,7 +750,7 @@ __device__ void finish_loss(const DistillArgs& a, int m, const RestPart& rest)
 }
 
 // The words of the list leave the sum over the others by a bit each in LDS, so that the share of all others is a sum and not 1 less what the list has.
-// Measured: 2048 rows of 32 000 bf16 39 us, 3.3 TB/s, vector units 83 % of the busy cycles; 700 rows of 10 000 fp32 14 us.
+// Measured: 2048 rows of 32 000 bf16 41 us, 3.2 TB/s, vector units 83 % of the busy cycles; 700 rows of 10 000 fp32 14 us.
 template <class E, int VPT, int THREADS>
 __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int segs)
 {
@@ -823,7 +823,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a, int seg
     }
 }
 
-// 2048 rows of two segments 8.7 us: the loss's chain of logarithms and exponentials in 64 bits, a wave a row.
+// 2048 rows of two segments 8.6 us: the loss's chain of logarithms and exponentials in 64 bits, a wave a row.
 template <class E>
 __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a, int segs)
 {
@@ -840,7 +840,7 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a, i
     if (threadIdx.x < 64) finish_loss<E>(a, m, p);
 }
 
-// Bound by memory: 2048 rows of 32 000 bf16 46 us for 262 MB, 5.7 TB/s (some of it from the last-level cache); 700 rows of 10 000 fp32 13 us.
+// Bound by memory: 2048 rows of 32 000 bf16 46.5 us for 262 MB, 5.6 TB/s (some of it from the last-level cache); 700 rows of 10 000 fp32 13 us.
 template <class E>
 __global__ __launch_bounds__(kThreads) void distill_gradient_kernel(DistillArgs a, int segs)
 {
