@@ -660,10 +660,11 @@ int lstm_logprobs_backward(int M, int V, int dtype, const void* logits, int64_t 
  *   temperature 2^-20 .. 2^20, in 64 bits: t_r is a difference that takes what rounding does to it in full, so it has to be the one that teacher_lse
  *     was made with.  loss [M] or NULL.  stats fp32 [M, 4] or NULL: what lstm_distill_backward needs.
  *   workspace: at least lstm_distill_workspace_bytes(M, V, K) bytes.
- * A student's logit may be minus infinity (its s_j is 0, and so is its gradient outside the list; the loss is infinite where t_j, or t_r of words that
- * are all so, is not; such a t_r of no more than 2^-22 (|teacher_lse| + sum_j t_j |z_j| / temperature + 1) is what rounding leaves, and counts as 0); a row
- * of nothing else has loss and gradient NaN, and so have a list of minus infinities alone without teacher_lse and its words.  A NaN in a row makes its results NaN,
- * except in one without a teacher.
+ * A student's logit may be minus infinity (its s_j is 0, and so is its gradient outside the list; the loss is infinite where t_j, or t_r
+ * of words that are all so, is not; such a t_r of no more than 2^-22 (|teacher_lse| + sum_j t_j |z_j| / temperature + 1) is what rounding
+ * leaves, and counts as 0); a row of nothing else has loss and gradient NaN, and so have a list of minus infinities alone without
+ * teacher_lse and its words.  A NaN in a row makes its results NaN, except in one without a teacher.  A word whose share of the student's
+ * largest one's is below 2^-126 counts as one of 0 in the gradient outside the list, unless t_r / s_r is above e^40.
  */
 size_t lstm_distill_workspace_bytes(int M, int V, int K);
 int lstm_distill_forward(int M, int V, int K, int dtype, const void* logits, int64_t ld, const int32_t* top_token, int64_t top_token_ld,
